@@ -290,6 +290,80 @@ int nvfp4_osci_suppress_sparse(float *W, int64_t C, int64_t D, const uint32_t *i
                                const float *dist_q_s, float tau, unsigned long long *n_reset, void *stream);
 
 /*
+ * What a transformer block has around its quantized linears: norms, the nonlinearity of the MLP, 8-bit checkpoints of activations
+ * for the backward pass, and the linear of single tokens on packed weights (bf16 activations, not quantized).
+ *
+ * Arrays of these calls are strided: ldx is the number of elements from one row of X to the next, at least the row's
+ * length (SHAPE otherwise); the elements of a row are contiguous.  Unlike the other calls' arrays they may start at any element (2 bytes
+ * for bf16, 4 for binary32).  Sources are NVFP4_SRC_BF16, NVFP4_SRC_F32 or, where a checkpoint is taken, NVFP4_SRC_CKPT8: then
+ * the pointer is a HOST pointer to an nvfp4_ckpt8 and its ld is not read.  Outputs are NVFP4_OUT_BF16 or NVFP4_OUT_F32, independently of the
+ * sources.  An output must not overlap an input.  Sums and statistics are binary32, each output is rounded once.
+ * Arrays have at most 2^33 elements and span at most 2^46 (SHAPE).  A NaN or infinity stays in the row (norms), the element or the token that it is in;
+ * in the norm's backward pass it reaches dgamma and dbeta in its columns.
+ */
+enum { NVFP4_SRC_F32 = 2, NVFP4_SRC_CKPT8 = 3 };
+enum { NVFP4_NORM_LAYER = 0, NVFP4_NORM_RMS = 1 };
+enum { NVFP4_ACT_SWIGLU = 0, NVFP4_ACT_GELU = 1 };
+
+/* An 8-bit checkpoint of a [rows x K] array.  Every 128 consecutive elements of a row (the last group may be shorter) share a power of two 2^e:
+ * with a = max |x| over the group's finite elements, e is the least integer with a <= 448 * 2^e and -126 <= e <= 120 (-126 for a = 0).
+ *   codes [rows][K]              E4M3 (bias 7, no infinity, max 448) of x * 2^-e, nearest, ties to even
+ *   exps  [rows][ceil(K / 128)]  e + 127
+ * value = code * 2^e; elements that are not finite become NaN (0x7F) and leave the rest of their group as it is.  Device memory of the
+ * caller, no alignment; the saving call fills rows and K. */
+typedef struct nvfp4_ckpt8 {
+    uint8_t *codes;
+    uint8_t *exps;
+    int64_t rows, K;
+} nvfp4_ckpt8;
+
+/*
+ * Norm of every row of X [N x D]: mu = mean(x) (NVFP4_NORM_RMS: 0), r = 1 / sqrt(mean((x - mu)^2) + eps), Y = (x - mu) r gamma + beta.
+ * gamma, beta: binary32 [D], 16-byte aligned, optional (NULL: 1 and 0).  stats: [N][2] binary32 (mu, r), 8-byte aligned, optional; the
+ * backward pass needs it.  ckpt: optional; receives X in 8 bits from the same read.  D <= 2^22.
+ * Errors: NULL, SHAPE, ENUM (also eps < 0 or NaN), ALIGN.
+ */
+int nvfp4_norm_fwd(const void *X, int src_kind, int64_t ldx, int64_t N, int64_t D, const float *gamma, const float *beta, float eps,
+                   int norm, void *Y, int out_dtype, int64_t ldy, float *stats, nvfp4_ckpt8 *ckpt, void *stream);
+
+/*
+ * Gradients of nvfp4_norm_fwd from dY (NVFP4_SRC_BF16 or NVFP4_SRC_F32), X (as it was, or its 8-bit checkpoint) and the forward call's stats.
+ * With h = (x - mu) r and g = dY gamma: dX = r (g - mean(g) - h mean(g h)) (NVFP4_NORM_RMS: without mean(g)), dgamma = sum over rows of dY h,
+ * dbeta = sum over rows of dY (binary32 [D], 16-byte aligned, each optional; zeros for N = 0).  The sums over rows are taken
+ * in an order that depends on N and D alone: the same inputs give the same bits.  ws: nvfp4_norm_workspace_bytes(N, D) bytes where dgamma or dbeta is wanted.
+ * Errors: NULL, SHAPE, ENUM, ALIGN, MISMATCH (checkpoint of another shape), WORKSPACE.
+ */
+int nvfp4_norm_bwd(const void *dY, int dy_kind, int64_t lddy, const void *X, int src_kind, int64_t ldx, const float *stats,
+                   const float *gamma, int64_t N, int64_t D, int norm, void *dX, int out_dtype, int64_t lddx, float *dgamma,
+                   float *dbeta, void *ws, size_t ws_bytes, void *stream);
+size_t nvfp4_norm_workspace_bytes(int64_t N, int64_t D);
+
+/*
+ * The nonlinearity between the linears of an MLP.  NVFP4_ACT_SWIGLU: H [N x 2F] holds F gates g, then F up values u; A = g s(g) u.
+ * NVFP4_ACT_GELU: H [N x F], A = x s(2 sqrt(2 / pi) (x + 0.044715 x^3)) (the tanh form).  s(z) = 1 / (1 + exp(-z)).  A [N x F].
+ * ckpt: optional; receives H in 8 bits from the same read, as [2N x F] (SWIGLU: row 2n the gates, 2n + 1 the up values of token n, so
+ * that no group has both) or [N x F].
+ * nvfp4_act_bwd: dH (the shape of H) from dA [N x F] (NVFP4_SRC_BF16 or NVFP4_SRC_F32) and H as it was or its checkpoint.
+ * Errors: NULL, SHAPE, ENUM, ALIGN, MISMATCH (checkpoint of another shape).
+ */
+int nvfp4_act_fwd(const void *H, int src_kind, int64_t ldh, int64_t N, int64_t F, int act, void *A, int out_dtype, int64_t lda,
+                  nvfp4_ckpt8 *ckpt, void *stream);
+int nvfp4_act_bwd(const void *dA, int da_kind, int64_t ldda, const void *H, int src_kind, int64_t ldh, int64_t N, int64_t F, int act,
+                  void *dH, int out_dtype, int64_t lddh, void *stream);
+
+/* Any other activation [N x D] in 8 bits and back.  Errors: NULL, SHAPE, ENUM, ALIGN. */
+int nvfp4_ckpt8_save(const void *X, int src_kind, int64_t ldx, int64_t N, int64_t D, nvfp4_ckpt8 *out, void *stream);
+int nvfp4_ckpt8_load(const nvfp4_ckpt8 *src, void *Y, int out_dtype, int64_t ldy, void *stream);
+
+/*
+ * Y [M x C] = X [M x K] * W^T for the few tokens of a decoding step: X bf16 as it is, W [C x K] an operand in either outer mode
+ * (nvfp4_linear_fwd's Wq_ctx, or what nvfp4_quantize gives of axis 0).  The products are exact, the sums binary32.  Meant for M up to some
+ * dozens (the weights are read once per 64 tokens); M <= 2^20, C <= 2^26, K <= 2^22.  No workspace: may be captured in a graph.
+ * Errors: NULL, SHAPE, ENUM, ALIGN.
+ */
+int nvfp4_gemv(const void *X, int64_t ldx, int64_t M, const nvfp4_tensor *W, void *Y, int out_dtype, int64_t ldy, void *stream);
+
+/*
  * Scratch bytes an operation needs.  op = NVFP4_OP_*.  QUANTIZE: (N, D) = (R, C) of the source, C ignored.
  * GEMM: Out is [N x C] with reduction length D.  LINEAR_*: as in the calls above.  Returns 0 for a bad op.
  *

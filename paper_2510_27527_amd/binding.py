@@ -20,11 +20,15 @@ LIB_PATH = os.path.join(_HERE, "libtjnvfp4.so")
 ROUND_RTN, ROUND_SR = 0, 1
 SCALE_DEFAULT, SCALE_NE, SCALE_UP = 0, 1, 2
 OUTER_TENSOR, OUTER_BLOCK128 = 0, 1
-SRC_BF16, SRC_NVFP4 = 0, 1
+SRC_BF16, SRC_NVFP4, SRC_F32, SRC_CKPT8 = 0, 1, 2, 3
 OUT_BF16, OUT_F32 = 0, 1
 OP_QUANTIZE, OP_GEMM, OP_LINEAR_FWD, OP_LINEAR_BWD_DX, OP_LINEAR_BWD_DW, OP_LINEAR_BWD = 0, 1, 2, 3, 4, 5
+NORM_LAYER, NORM_RMS = 0, 1
+ACT_SWIGLU, ACT_GELU = 0, 1
+CKPT_GROUP = 128               # elements of a row that share a power of two in an 8-bit checkpoint
 
 EXPORTS = ["nvfp4_quantize", "nvfp4_quantize_dual", "nvfp4_gemm_nt", "nvfp4_gemm_nt_static", "nvfp4_linear_fwd", "nvfp4_linear_bwd_dx", "nvfp4_linear_bwd_dw", "nvfp4_linear_bwd", "nvfp4_osci_update", "nvfp4_osci_suppress", "nvfp4_osci_select", "nvfp4_osci_update_sparse", "nvfp4_osci_suppress_sparse", "nvfp4_osci_select_workspace_bytes", "nvfp4_outctl_fwd", "nvfp4_outctl_bwd", "nvfp4_outctl_workspace_bytes", "nvfp4_outctl_dw_plan", "nvfp4_backward_plan", "nvfp4_backward_product_plan",
+           "nvfp4_norm_fwd", "nvfp4_norm_bwd", "nvfp4_norm_workspace_bytes", "nvfp4_act_fwd", "nvfp4_act_bwd", "nvfp4_ckpt8_save", "nvfp4_ckpt8_load", "nvfp4_gemv",
            "nvfp4_workspace_bytes", "nvfp4_gemm_plan", "nvfp4_gemm_plan_kernel", "nvfp4_amax_bf16", "nvfp4_stream_key", "nvfp4_strerror", "nvfp4_version"]
 
 
@@ -43,6 +47,10 @@ class CQcfg(C.Structure):
     _fields_ = [("rounding", C.c_int32), ("scale_round", C.c_int32), ("outer_mode", C.c_int32),
                 ("tensor_id", C.c_uint32), ("seed", C.c_uint64), ("amax_in", C.c_void_p), ("rht", C.c_int32),
                 ("rht_id", C.c_uint32)]
+
+
+class CCkpt8(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("exps", C.c_void_p), ("rows", C.c_int64), ("K", C.c_int64)]
 
 
 class CProductPlan(C.Structure):
@@ -110,6 +118,22 @@ def lib():
         L.nvfp4_osci_update_sparse.argtypes = [vp, i64, i64, vp, i64, vp, vp, vp, vp, vp]
         L.nvfp4_osci_suppress_sparse.restype = i32
         L.nvfp4_osci_suppress_sparse.argtypes = [vp, i64, i64, vp, i64, vp, vp, C.c_float, vp, vp]
+        L.nvfp4_norm_fwd.restype = i32
+        L.nvfp4_norm_fwd.argtypes = [vp, i32, i64, i64, i64, vp, vp, C.c_float, i32, vp, i32, i64, vp, vp, vp]
+        L.nvfp4_norm_bwd.restype = i32
+        L.nvfp4_norm_bwd.argtypes = [vp, i32, i64, vp, i32, i64, vp, vp, i64, i64, i32, vp, i32, i64, vp, vp, vp, sz, vp]
+        L.nvfp4_norm_workspace_bytes.restype = sz
+        L.nvfp4_norm_workspace_bytes.argtypes = [i64, i64]
+        L.nvfp4_act_fwd.restype = i32
+        L.nvfp4_act_fwd.argtypes = [vp, i32, i64, i64, i64, i32, vp, i32, i64, vp, vp]
+        L.nvfp4_act_bwd.restype = i32
+        L.nvfp4_act_bwd.argtypes = [vp, i32, i64, vp, i32, i64, i64, i64, i32, vp, i32, i64, vp]
+        L.nvfp4_ckpt8_save.restype = i32
+        L.nvfp4_ckpt8_save.argtypes = [vp, i32, i64, i64, i64, vp, vp]
+        L.nvfp4_ckpt8_load.restype = i32
+        L.nvfp4_ckpt8_load.argtypes = [vp, vp, i32, i64, vp]
+        L.nvfp4_gemv.restype = i32
+        L.nvfp4_gemv.argtypes = [vp, i64, i64, vp, vp, i32, i64, vp]
         L.nvfp4_workspace_bytes.restype = sz
         L.nvfp4_workspace_bytes.argtypes = [i32, i64, i64, i64, i32]
         L.nvfp4_gemm_plan.restype = i32
@@ -511,3 +535,178 @@ def outctl_bwd(dY, Xq: NVFP4Tensor, Wq: NVFP4Tensor, X_hp, W_hp, seed: int, laye
                                 ws.numel(), _stream())
     _check(rc, "nvfp4_outctl_bwd")
     return tuple(outs)
+
+
+# ---- operators around the linears: norms, nonlinearities, 8-bit checkpoints, the linear of single tokens ----
+
+@dataclass
+class Ckpt8:
+    """Device buffers of an 8-bit checkpoint of a [rows, K] array."""
+    codes: torch.Tensor      # uint8 [rows, K]: E4M3 codes
+    exps: torch.Tensor       # uint8 [rows, ceil(K / 128)]: 127 + e, the values being code * 2^e
+    rows: int
+    K: int
+
+    def c_struct(self) -> CCkpt8:
+        return CCkpt8(_ptr(self.codes), _ptr(self.exps), self.rows, self.K)
+
+
+def alloc_ckpt8(rows: int, K: int, device="cuda") -> Ckpt8:
+    return Ckpt8(torch.empty((rows, K), dtype=torch.uint8, device=device),
+                 torch.empty((rows, -(-K // CKPT_GROUP)), dtype=torch.uint8, device=device), rows, K)
+
+
+def alloc_act_ckpt8(N: int, F: int, act: int, device="cuda") -> Ckpt8:
+    """The checkpoint of a nonlinearity's input: the gates and the up values of a token are rows of their own (SwiGLU)."""
+    return alloc_ckpt8(2 * N if act == ACT_SWIGLU else N, F, device)
+
+
+def alloc_stats(N: int, device="cuda") -> torch.Tensor:
+    """The statistics of a norm's rows (mean, 1 / deviation) that its backward pass reads."""
+    return torch.empty((N, 2), dtype=torch.float32, device=device)
+
+
+def _rows(t: torch.Tensor, what: str):
+    """(kind, row stride) of a bf16 or float32 matrix whose rows are contiguous; the rows may be any distance apart."""
+    assert t.dim() == 2 and t.is_cuda, what + ": 2-D, on the GPU"
+    assert t.dtype == torch.bfloat16 or t.dtype == torch.float32, what + ": bf16 or float32"
+    n = t.shape[1]
+    s0, s1 = t.stride()
+    assert s1 == 1 or n <= 1, what + ": rows of contiguous elements"
+    return (SRC_BF16 if t.dtype == torch.bfloat16 else SRC_F32), (s0 if t.shape[0] > 1 else n)
+
+
+def _out_rows(t: Optional[torch.Tensor], shape, out_dtype: int, device, what: str):
+    """The output matrix, allocated where none is given, and its row stride."""
+    if t is None:
+        return _out_tensor(*shape, out_dtype, device), shape[1]
+    kind, ld = _rows(t, what)
+    assert tuple(t.shape) == tuple(shape) and kind == (SRC_BF16 if out_dtype == OUT_BF16 else SRC_F32), what
+    return t, ld
+
+
+def _param(t: Optional[torch.Tensor], D: int, what: str):
+    assert t is None or (t.dtype == torch.float32 and t.dim() == 1 and t.numel() == D and t.is_contiguous() and t.is_cuda), what + ": float32 [D]"
+    return _ptr(t)
+
+
+def _check_ckpt(c: Ckpt8, rows: int, K: int):
+    assert c.rows == rows and c.K == K, "checkpoint of another shape"
+    for t, shape in ((c.codes, (rows, K)), (c.exps, (rows, -(-K // CKPT_GROUP)))):
+        assert t.dtype == torch.uint8 and tuple(t.shape) == shape and t.is_contiguous() and t.is_cuda, "checkpoint buffers"
+
+
+def _check_stats(t: torch.Tensor, N: int):
+    assert t.dtype == torch.float32 and tuple(t.shape) == (N, 2) and t.is_contiguous() and t.is_cuda, "stats: float32 [N, 2]"
+
+
+def norm_fwd(X: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None, *, eps: float = 1e-5,
+             norm: int = NORM_LAYER, out_dtype: int = OUT_BF16, Y: Optional[torch.Tensor] = None, stats: Optional[torch.Tensor] = None,
+             ckpt: Optional[Ckpt8] = None) -> torch.Tensor:
+    """nvfp4_norm_fwd: layer norm (NORM_LAYER) or RMS norm (NORM_RMS) of every row of X.  For training pass stats (alloc_stats) and, to keep
+    the input in 8 bits, ckpt (alloc_ckpt8); both are filled."""
+    kind, ldx = _rows(X, "X")
+    N, D = X.shape
+    Y, ldy = _out_rows(Y, (N, D), out_dtype, X.device, "Y")
+    cs = None
+    if ckpt is not None:
+        _check_ckpt(ckpt, N, D)
+        cs = C.byref(ckpt.c_struct())
+    if stats is not None:
+        _check_stats(stats, N)
+    _check(lib().nvfp4_norm_fwd(_ptr(X), kind, ldx, N, D, _param(gamma, D, "gamma"), _param(beta, D, "beta"), eps, norm, _ptr(Y), out_dtype,
+                                ldy, _ptr(stats), cs, _stream()), "nvfp4_norm_fwd")
+    return Y
+
+
+def norm_bwd(dY: torch.Tensor, X, stats: torch.Tensor, gamma: Optional[torch.Tensor] = None, *, norm: int = NORM_LAYER,
+             out_dtype: int = OUT_BF16, dX: Optional[torch.Tensor] = None, dgamma: Optional[torch.Tensor] = None,
+             dbeta: Optional[torch.Tensor] = None, params: bool = True, ws: Optional[torch.Tensor] = None):
+    """nvfp4_norm_bwd: (dX, dgamma, dbeta); X is the forward call's input or its Ckpt8.  params=False: dX alone; RMS norm has no dbeta
+    unless one is passed."""
+    dkind, lddy = _rows(dY, "dY")
+    N, D = dY.shape
+    dev = dY.device
+    if isinstance(X, Ckpt8):
+        _check_ckpt(X, N, D)
+        kind, ldx, src = SRC_CKPT8, 0, C.byref(X.c_struct())
+    else:
+        kind, ldx = _rows(X, "X")
+        assert X.shape == dY.shape, "X: the shape of dY"
+        src = _ptr(X)
+    _check_stats(stats, N)
+    dX, lddx = _out_rows(dX, (N, D), out_dtype, dev, "dX")
+    if params:
+        dgamma = torch.empty(D, dtype=torch.float32, device=dev) if dgamma is None else dgamma
+        if dbeta is None and norm == NORM_LAYER:
+            dbeta = torch.empty(D, dtype=torch.float32, device=dev)
+        if ws is None:
+            ws = alloc_workspace(lib().nvfp4_norm_workspace_bytes(N, D), dev)
+    else:
+        dgamma = dbeta = None
+    _check(lib().nvfp4_norm_bwd(_ptr(dY), dkind, lddy, src, kind, ldx, _ptr(stats), _param(gamma, D, "gamma"), N, D, norm, _ptr(dX), out_dtype,
+                                lddx, _param(dgamma, D, "dgamma"), _param(dbeta, D, "dbeta"), _ptr(ws), 0 if ws is None else ws.numel(),
+                                _stream()), "nvfp4_norm_bwd")
+    return dX, dgamma, dbeta
+
+
+def act_fwd(H: torch.Tensor, act: int = ACT_SWIGLU, out_dtype: int = OUT_BF16, *, A: Optional[torch.Tensor] = None,
+            ckpt: Optional[Ckpt8] = None) -> torch.Tensor:
+    """nvfp4_act_fwd: SwiGLU of H [N, 2F] (gates, then up values) or GELU (tanh form) of H [N, F]; ckpt (alloc_act_ckpt8) receives H in 8 bits."""
+    kind, ldh = _rows(H, "H")
+    N, F = H.shape
+    if act == ACT_SWIGLU:
+        assert F % 2 == 0, "H: gates and up values"
+        F //= 2
+    A, lda = _out_rows(A, (N, F), out_dtype, H.device, "A")
+    cs = None
+    if ckpt is not None:
+        _check_ckpt(ckpt, 2 * N if act == ACT_SWIGLU else N, F)
+        cs = C.byref(ckpt.c_struct())
+    _check(lib().nvfp4_act_fwd(_ptr(H), kind, ldh, N, F, act, _ptr(A), out_dtype, lda, cs, _stream()), "nvfp4_act_fwd")
+    return A
+
+
+def act_bwd(dA: torch.Tensor, H, act: int = ACT_SWIGLU, out_dtype: int = OUT_BF16, *, dH: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """nvfp4_act_bwd: dH from dA and the forward call's input or its Ckpt8."""
+    dkind, ldda = _rows(dA, "dA")
+    N, F = dA.shape
+    parts = 2 if act == ACT_SWIGLU else 1
+    if isinstance(H, Ckpt8):
+        _check_ckpt(H, parts * N, F)
+        kind, ldh, src = SRC_CKPT8, 0, C.byref(H.c_struct())
+    else:
+        kind, ldh = _rows(H, "H")
+        assert tuple(H.shape) == (N, parts * F), "H"
+        src = _ptr(H)
+    dH, lddh = _out_rows(dH, (N, parts * F), out_dtype, dA.device, "dH")
+    _check(lib().nvfp4_act_bwd(_ptr(dA), dkind, ldda, src, kind, ldh, N, F, act, _ptr(dH), out_dtype, lddh, _stream()), "nvfp4_act_bwd")
+    return dH
+
+
+def ckpt8_save(X: torch.Tensor, out: Optional[Ckpt8] = None) -> Ckpt8:
+    """nvfp4_ckpt8_save: an activation [N, D] in 8 bits."""
+    kind, ldx = _rows(X, "X")
+    N, D = X.shape
+    out = alloc_ckpt8(N, D, X.device) if out is None else out
+    _check_ckpt(out, N, D)
+    _check(lib().nvfp4_ckpt8_save(_ptr(X), kind, ldx, N, D, C.byref(out.c_struct()), _stream()), "nvfp4_ckpt8_save")
+    return out
+
+
+def ckpt8_load(src: Ckpt8, out_dtype: int = OUT_BF16, *, Y: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """nvfp4_ckpt8_load: the activation that a checkpoint holds."""
+    _check_ckpt(src, src.rows, src.K)
+    Y, ldy = _out_rows(Y, (src.rows, src.K), out_dtype, src.codes.device, "Y")
+    _check(lib().nvfp4_ckpt8_load(C.byref(src.c_struct()), _ptr(Y), out_dtype, ldy, _stream()), "nvfp4_ckpt8_load")
+    return Y
+
+
+def gemv(X: torch.Tensor, W: NVFP4Tensor, out_dtype: int = OUT_BF16, *, Y: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """nvfp4_gemv: Y = X W^T for the bf16 activations of a few tokens on packed weights (linear_fwd's Wq)."""
+    kind, ldx = _rows(X, "X")
+    M, K = X.shape
+    assert kind == SRC_BF16 and K == W.K, "X: bf16 [M, W.K]"
+    Y, ldy = _out_rows(Y, (M, W.rows), out_dtype, X.device, "Y")
+    _check(lib().nvfp4_gemv(_ptr(X), ldx, M, C.byref(W.c_struct()), _ptr(Y), out_dtype, ldy, _stream()), "nvfp4_gemv")
+    return Y
