@@ -5,6 +5,8 @@
 //   with s(z) = 1 / (1 + exp(-z)); s(-z) comes from the same exponential, without the cancellation of 1 - s(z).
 //
 // Element by element but for the maxima of a checkpoint's groups, which the 16 lanes of a group exchange in registers.  Bound: HBM.
+#include <type_traits>
+
 #include "rowwise.h"
 
 namespace tj {
@@ -13,13 +15,15 @@ namespace {
 
 constexpr int kSwiglu = 0, kGelu = 1;
 constexpr int kThreads = 256;
-constexpr int kMaxBlocks = 1 << 16;     // workgroups of a launch; beyond that each walks over several runs of chunks
+// rows of a thread whose loads are on their way together: two, us of one / two: SwiGLU forward 16384 x 4096 99 / 95, GELU 4099 x 2752 14.4 / 13.8,
+// checkpoint 8192 x 8192 saved 42 / 39.7 and loaded 35.8 / 31.2; one for SwiGLU's backward pass, where five streams are enough (101 / 122)
+constexpr int kRows = 2, kRowsSwigluBwd = 1;
+constexpr int kMaxRowBlocks = 65535;    // of a launch's grid; beyond that a workgroup walks over several
 
-// the chunks of all rows in one sequence, each row padded to whole groups
+// rows x cols in chunks of eight; a workgroup takes 2^shift chunks of 256 / 2^shift rows, whole groups of 16 chunks
 struct Chunks {
     int64_t rows;
-    int64_t per_row;                     // a multiple of 16
-    int64_t cols;
+    int cols, shift;
 };
 
 struct ActArgs {
@@ -40,7 +44,7 @@ struct Sigmoid { float pos, neg; };      // s(z) and s(-z)
 __device__ __forceinline__ Sigmoid sigmoid(float z)
 {
     const float e = __expf(-fabsf(z));   // never overflows
-    const float r = 1.0f / (1.0f + e), q = e * r;
+    const float r = __builtin_amdgcn_rcpf(1.0f + e), q = e * r;      // within one unit in the last place
     return z >= 0.0f ? Sigmoid{r, q} : Sigmoid{q, r};
 }
 
@@ -49,35 +53,56 @@ constexpr float kGeluC = 1.5957691216057308f, kGeluA = 0.044715f;
 __device__ __forceinline__ float gelu_in(float x) { return x > 16.0f ? 16.0f : x < -16.0f ? -16.0f : x; }
 __device__ __forceinline__ float gelu_z(float c) { return kGeluC * fmaf(kGeluA * c * c, c, c); }
 
-// f(row, column) for every chunk of the launch; the lanes of a group come together, those past the end of a row with col >= cols
-template <typename F>
-__device__ __forceinline__ void for_chunks(const Chunks &n, const F &f)
+// For every chunk of the launch use(row, column, load(row, column)), R rows of a thread loaded before the first is used.  The lanes of a
+// group come together, those past the end of a row with col >= cols.
+template <int R, typename Load, typename Use>
+__device__ __forceinline__ void for_chunks(const Chunks &n, const Load &load, const Use &use)
 {
-    const int64_t total = n.rows * n.per_row;
-    for (int64_t base = (int64_t)blockIdx.x * kThreads; base < total; base += (int64_t)gridDim.x * kThreads) {
-        const int64_t row0 = base / n.per_row;
-        const int64_t c = base - row0 * n.per_row + threadIdx.x;          // under per_row + 256
-        const int64_t over = (uint64_t)c < (uint64_t)n.per_row ? 0 : (int64_t)((uint32_t)c / (uint32_t)n.per_row);
-        if (row0 + over < n.rows) f(row0 + over, (c - over * n.per_row) * kChunk);   // whole groups: total and the runs are multiples of 16
+    const int col = (int)((blockIdx.x << n.shift) | (threadIdx.x & ((1u << n.shift) - 1))) * kChunk;
+    const int step = kThreads >> n.shift;                          // rows that the workgroup takes at once, R times in succession
+    for (int64_t row = (int64_t)blockIdx.y * (R * step) + (threadIdx.x >> n.shift); row < n.rows; row += (int64_t)gridDim.y * (R * step)) {
+        decltype(load(row, col)) in[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (row + r * step < n.rows) in[r] = load(row + r * step, col);
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (row + r * step < n.rows) use(row + r * step, col, in[r]);
     }
 }
 
-template <int KIND>
-__device__ __forceinline__ Raw<KIND> load8_or_0(const RowSrc &s, int64_t row, int64_t col, int64_t n, int64_t at)
+// chunk of a row's part that starts at `at` and has n elements
+template <int KIND, bool STREAM>
+__device__ __forceinline__ Raw<KIND> load8_at(const RowSrc &s, int64_t row, int col, int n, int at)
 {
-    return col < n ? load8<KIND>(s, row, at + col, at + n) : zero8<KIND>();
+    const int size = KIND == kF32 ? 4 : 2;
+    return load8<KIND, true, STREAM>(RowSrc{static_cast<const char *>(s.p) + (int64_t)at * size, nullptr, s.ld, 0, s.kind}, row, col, n);
+}
+template <int KIND, bool STREAM>
+__device__ __forceinline__ Raw<KIND> load8_or_0(const RowSrc &s, int64_t row, int col, int n, int at)
+{
+    return col < n ? load8_at<KIND, STREAM>(s, row, col, n, at) : zero8<KIND>();
 }
 
-template <int KIND, bool OF32, int ACT>
+template <int KIND> struct Pair { Raw<KIND> a, b; };
+template <int KIND, int GKIND> struct Triple { Raw<KIND> a, b; Raw<GKIND> da; };
+
+template <int KIND, bool OF32, bool STREAM, int ACT>
 __global__ __launch_bounds__(kThreads) void act_fwd_kernel(const ActArgs a)
 {
-    for_chunks(a.n, [&](int64_t row, int64_t col) {
-        const int64_t F = a.n.cols;
+    const int F = a.n.cols;
+    const auto load = [&](int64_t row, int col) {
+        Pair<KIND> in;
+        in.a = load8_or_0<KIND, STREAM>(a.h, row, col, F, 0);
+        if constexpr (ACT == kSwiglu) in.b = load8_or_0<KIND, STREAM>(a.h, row, col, F, F);
+        return in;
+    };
+    for_chunks<kRows>(a.n, load, [&](int64_t row, int col, const Pair<KIND> &in) {
         float x[8], o[8];
-        widen8(load8_or_0<KIND>(a.h, row, col, F, 0), x);
+        widen8(in.a, x);
         if constexpr (ACT == kSwiglu) {
             float u[8];
-            widen8(load8_or_0<KIND>(a.h, row, col, F, F), u);
+            widen8(in.b, u);
             if (a.ckpt.codes) {
                 ckpt_store8(a.ckpt, 2 * row, col, F, x);
                 ckpt_store8(a.ckpt, 2 * row + 1, col, F, u);
@@ -93,24 +118,35 @@ __global__ __launch_bounds__(kThreads) void act_fwd_kernel(const ActArgs a)
     });
 }
 
-template <int KIND, bool GF32, bool OF32, int ACT>
+template <int KIND, bool GF32, bool OF32, bool STREAM, int ACT>
 __global__ __launch_bounds__(kThreads) void act_bwd_kernel(const ActArgs a)
 {
     constexpr int GKIND = GF32 ? kF32 : kBf16;
-    for_chunks(a.n, [&](int64_t row, int64_t col) {
-        const int64_t F = a.n.cols;
+    using In = Triple<KIND, GKIND>;
+    const int F = a.n.cols;
+    const auto load = [&](int64_t row, int col) {
+        In in;
+        if (col >= F) return in;
+        in.da = load8<GKIND, true, STREAM>(a.da, row, col, F);
+        if constexpr (ACT == kGelu) {
+            in.a = load8<KIND, true, STREAM>(a.h, row, col, F);
+        } else if constexpr (KIND == kCkpt8) {
+            in.a = load8<KIND, true, STREAM>(a.h, 2 * row, col, F);
+            in.b = load8<KIND, true, STREAM>(a.h, 2 * row + 1, col, F);
+        } else {
+            in.a = load8<KIND, true, STREAM>(a.h, row, col, F);
+            in.b = load8_at<KIND, STREAM>(a.h, row, col, F, F);
+        }
+        return in;
+    };
+    for_chunks<ACT == kSwiglu ? kRowsSwigluBwd : kRows>(a.n, load, [&](int64_t row, int col, const In &in) {
         if (col >= F) return;
         float x[8], da[8];
-        widen8(load8<GKIND>(a.da, row, col, F), da);
+        widen8(in.da, da);
+        widen8(in.a, x);
         if constexpr (ACT == kSwiglu) {
             float u[8];
-            if constexpr (KIND == kCkpt8) {
-                widen8(load8<KIND>(a.h, 2 * row, col, F), x);
-                widen8(load8<KIND>(a.h, 2 * row + 1, col, F), u);
-            } else {
-                widen8(load8<KIND>(a.h, row, col, F), x);
-                widen8(load8<KIND>(a.h, row, F + col, 2 * F), u);
-            }
+            widen8(in.b, u);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const Sigmoid s = sigmoid(x[i]);
@@ -119,9 +155,8 @@ __global__ __launch_bounds__(kThreads) void act_bwd_kernel(const ActArgs a)
                 u[i] = du;
             }
             store8<OF32>(a.out.p, a.out.ld, row, col, F, x);
-            store8<OF32>(static_cast<char *>(a.out.p) + F * (OF32 ? 4 : 2), a.out.ld, row, col, F, u);
+            store8<OF32>(static_cast<char *>(a.out.p) + (int64_t)F * (OF32 ? 4 : 2), a.out.ld, row, col, F, u);
         } else {
-            widen8(load8<KIND>(a.h, row, col, F), x);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float c = gelu_in(x[i]);
@@ -134,49 +169,71 @@ __global__ __launch_bounds__(kThreads) void act_bwd_kernel(const ActArgs a)
     });
 }
 
-template <int KIND>
+template <int KIND, bool STREAM>
 __global__ __launch_bounds__(kThreads) void ckpt8_save_kernel(const CopyArgs a)
 {
-    for_chunks(a.n, [&](int64_t row, int64_t col) {
+    for_chunks<kRows>(a.n, [&](int64_t row, int col) { return load8_or_0<KIND, STREAM>(a.src, row, col, a.n.cols, 0); },
+                      [&](int64_t row, int col, const Raw<KIND> &in) {
         float x[8];
-        widen8(load8_or_0<KIND>(a.src, row, col, a.n.cols, 0), x);
+        widen8(in, x);
         ckpt_store8(a.ckpt, row, col, a.n.cols, x);
     });
 }
 
-template <bool OF32>
+template <bool OF32, bool STREAM>
 __global__ __launch_bounds__(kThreads) void ckpt8_load_kernel(const CopyArgs a)
 {
-    for_chunks(a.n, [&](int64_t row, int64_t col) {
+    for_chunks<kRows>(a.n, [&](int64_t row, int col) { return col < a.n.cols ? load8<kCkpt8, true, STREAM>(a.src, row, col, a.n.cols) : zero8<kCkpt8>(); },
+                      [&](int64_t row, int col, const Raw<kCkpt8> &in) {
         if (col >= a.n.cols) return;
         float x[8];
-        widen8(load8<kCkpt8>(a.src, row, col, a.n.cols), x);
+        widen8(in, x);
         store8<OF32>(a.out.p, a.out.ld, row, col, a.n.cols, x);
     });
 }
 
+// As many chunks of a row as leave at most an eighth of the workgroups' threads without work (sixteen leave none but in the last group)
 Chunks chunks_of(int64_t rows, int64_t cols)
 {
-    const int64_t groups = (cols + kCkptGroup - 1) / kCkptGroup;
-    return Chunks{rows, groups * kGroupLanes, cols};
+    const int64_t per_row = (cols + kCkptGroup - 1) / kCkptGroup * kGroupLanes;
+    int shift = 8;
+    const auto padded = [&](int sh) { return (((per_row - 1) >> sh) + 1) << sh; };
+    while (shift > 4 && padded(shift) * 8 > per_row * 9) --shift;
+    return Chunks{rows, (int)cols, shift};
 }
 
-unsigned blocks_of(const Chunks &n)
+dim3 grid_of(const Chunks &n, int rows = kRows)      // of a thread
 {
-    const int64_t want = (n.rows * n.per_row + kThreads - 1) / kThreads;
-    return (unsigned)(want < kMaxBlocks ? want : kMaxBlocks);
+    const int64_t wide = (int64_t)kChunk << n.shift, tall = kThreads >> n.shift, blocks = (n.rows + rows * tall - 1) / (rows * tall);
+    return dim3((unsigned)((n.cols + wide - 1) / wide), (unsigned)(blocks < kMaxRowBlocks ? blocks : kMaxRowBlocks));
 }
+
+// f(std::true_type) for a call of so many bytes per element that streams, f(std::false_type) for another
+template <typename F> void by_size(const Chunks &n, double bytes, const F &f)
+{
+    if (streams((double)n.rows * n.cols * bytes)) f(std::true_type{});
+    else f(std::false_type{});
+}
+constexpr double bytes_of(int kind) { return kind == kF32 ? 4.0 : kind == kBf16 ? 2.0 : 1.0; }
 
 template <int KIND, bool OF32> void run_act_fwd(const ActArgs &a, int act, hipStream_t st)
 {
-    if (act == kSwiglu) act_fwd_kernel<KIND, OF32, kSwiglu><<<blocks_of(a.n), kThreads, 0, st>>>(a);
-    else act_fwd_kernel<KIND, OF32, kGelu><<<blocks_of(a.n), kThreads, 0, st>>>(a);
+    const double parts = act == kSwiglu ? 2.0 : 1.0;
+    by_size(a.n, parts * (bytes_of(KIND) + (a.ckpt.codes ? 1.0 : 0.0)) + (OF32 ? 4.0 : 2.0), [&](auto stream) {
+        constexpr bool S = decltype(stream)::value;
+        if (act == kSwiglu) act_fwd_kernel<KIND, OF32, S, kSwiglu><<<grid_of(a.n), kThreads, 0, st>>>(a);
+        else act_fwd_kernel<KIND, OF32, S, kGelu><<<grid_of(a.n), kThreads, 0, st>>>(a);
+    });
 }
 
 template <int KIND, bool GF32, bool OF32> void run_act_bwd(const ActArgs &a, int act, hipStream_t st)
 {
-    if (act == kSwiglu) act_bwd_kernel<KIND, GF32, OF32, kSwiglu><<<blocks_of(a.n), kThreads, 0, st>>>(a);
-    else act_bwd_kernel<KIND, GF32, OF32, kGelu><<<blocks_of(a.n), kThreads, 0, st>>>(a);
+    const double parts = act == kSwiglu ? 2.0 : 1.0;
+    by_size(a.n, parts * (bytes_of(KIND) + (OF32 ? 4.0 : 2.0)) + (GF32 ? 4.0 : 2.0), [&](auto stream) {
+        constexpr bool S = decltype(stream)::value;
+        if (act == kSwiglu) act_bwd_kernel<KIND, GF32, OF32, S, kSwiglu><<<grid_of(a.n, kRowsSwigluBwd), kThreads, 0, st>>>(a);
+        else act_bwd_kernel<KIND, GF32, OF32, S, kGelu><<<grid_of(a.n), kThreads, 0, st>>>(a);
+    });
 }
 
 template <int KIND> void run_act_bwd(const ActArgs &a, int act, hipStream_t st)
@@ -207,16 +264,22 @@ hipError_t launch_act_bwd(const RowSrc &da, const RowSrc &h, int64_t N, int64_t 
 hipError_t launch_ckpt8_save(const RowSrc &src, int64_t N, int64_t D, const CkptOut &ckpt, hipStream_t st)
 {
     const CopyArgs a{src, chunks_of(N, D), RowDst{}, ckpt};
-    if (src.kind == kF32) ckpt8_save_kernel<kF32><<<blocks_of(a.n), kThreads, 0, st>>>(a);
-    else ckpt8_save_kernel<kBf16><<<blocks_of(a.n), kThreads, 0, st>>>(a);
+    by_size(a.n, bytes_of(src.kind) + 1.0, [&](auto stream) {
+        constexpr bool S = decltype(stream)::value;
+        if (src.kind == kF32) ckpt8_save_kernel<kF32, S><<<grid_of(a.n), kThreads, 0, st>>>(a);
+        else ckpt8_save_kernel<kBf16, S><<<grid_of(a.n), kThreads, 0, st>>>(a);
+    });
     return hipGetLastError();
 }
 
 hipError_t launch_ckpt8_load(const RowSrc &src, int64_t N, int64_t D, const RowDst &out, hipStream_t st)
 {
     const CopyArgs a{src, chunks_of(N, D), out, CkptOut{}};
-    if (out.f32) ckpt8_load_kernel<true><<<blocks_of(a.n), kThreads, 0, st>>>(a);
-    else ckpt8_load_kernel<false><<<blocks_of(a.n), kThreads, 0, st>>>(a);
+    by_size(a.n, 1.0 + (out.f32 ? 4.0 : 2.0), [&](auto stream) {
+        constexpr bool S = decltype(stream)::value;
+        if (out.f32) ckpt8_load_kernel<true, S><<<grid_of(a.n), kThreads, 0, st>>>(a);
+        else ckpt8_load_kernel<false, S><<<grid_of(a.n), kThreads, 0, st>>>(a);
+    });
     return hipGetLastError();
 }
 

@@ -10,12 +10,13 @@ namespace {
 constexpr int64_t kMaxElems = (int64_t)1 << 33;      // of an array
 constexpr int64_t kMaxSpan = (int64_t)1 << 46;       // elements from its first to its last, with the strides
 constexpr int64_t kMaxRow = (int64_t)1 << 22;        // of a norm, and of a reduction
+constexpr int64_t kMaxCols = (int64_t)1 << 30;       // of any other row
 
 bool aligned(const void *p, unsigned to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
 int check_sizes(int64_t rows, int64_t cols)
 {
-    if (rows < 0 || cols < 0 || rows > kMaxElems || cols > kMaxElems) return NVFP4_ERR_SHAPE;
+    if (rows < 0 || cols < 0 || rows > kMaxElems || cols > kMaxCols) return NVFP4_ERR_SHAPE;
     return rows > 0 && cols > kMaxElems / rows ? NVFP4_ERR_SHAPE : NVFP4_OK;
 }
 
@@ -150,7 +151,7 @@ int nvfp4_act_fwd(const void *H, int src_kind, int64_t ldh, int64_t N, int64_t F
 {
     if (act != NVFP4_ACT_SWIGLU && act != NVFP4_ACT_GELU) return NVFP4_ERR_ENUM;
     const int64_t parts = act == NVFP4_ACT_SWIGLU ? 2 : 1;
-    int rc = F > kMaxElems / 2 ? NVFP4_ERR_SHAPE : check_sizes(N, parts * F);
+    int rc = F > kMaxCols ? NVFP4_ERR_SHAPE : check_sizes(N, parts * F);
     if (rc) return rc;
     RowSrc h;
     RowDst a;
@@ -171,7 +172,7 @@ int nvfp4_act_bwd(const void *dA, int da_kind, int64_t ldda, const void *H, int 
 {
     if (act != NVFP4_ACT_SWIGLU && act != NVFP4_ACT_GELU) return NVFP4_ERR_ENUM;
     const int64_t parts = act == NVFP4_ACT_SWIGLU ? 2 : 1;
-    int rc = F > kMaxElems / 2 ? NVFP4_ERR_SHAPE : check_sizes(N, parts * F);
+    int rc = F > kMaxCols ? NVFP4_ERR_SHAPE : check_sizes(N, parts * F);
     if (rc) return rc;
     RowSrc da, h;
     RowDst dh;

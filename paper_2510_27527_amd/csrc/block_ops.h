@@ -25,6 +25,13 @@ struct CkptOut {
     int64_t groups;
 };
 
+// Calls that move more than half of the 256 MB last-level cache read their arrays past it: what the reads would leave there displaces what the call
+// writes, which is read next.  A kernel of its own: asked at each access, the question costs more than it gives.  us, through the caches /
+// past them: SwiGLU backward 16384 x 4096 (537 MB) 99.5 / 91, norm backward 4096 x 16384 (336 MB) 78 / 68.5, checkpoint 8192 x 8192
+// saved (201 MB) 39.7 / 34.7; and under it the other way: GELU 4099 x 2752 (56 MB) forward 13.8 / 15.0, backward 14.4 / 16.6.  (The norm's
+// forward pass gains nothing: 4096 x 16384 67.9 / 68.7; writes past the caches make the next reader pay: the same checkpoint loaded 31 / 40.)
+inline bool streams(double bytes) { return bytes > (double)(128 << 20); }
+
 // norm of N rows of D (layer: with the mean taken off); gamma, beta, stats ([N] pairs of mean and 1 / deviation) and the checkpoint are optional
 hipError_t launch_norm_fwd(const RowSrc &x, int64_t N, int64_t D, const float *gamma, const float *beta, float eps, int layer, const RowDst &y,
                            float *stats, const CkptOut &ckpt, hipStream_t st);

@@ -51,31 +51,40 @@ __device__ __forceinline__ void param8(const float *p, int col, int D, float fil
     }
 }
 
-constexpr int rows_at_once(int TPR) { return TPR == 64 ? 4 : 1; }
-
+// A row lies in the registers of TPR threads, V chunks of eight each; the parameters of a thread's columns stay there for all of its rows,
+// and the next row is on its way while a row is summed and written.
 template <int KIND, bool OF32, int TPR, int V>
-__global__ __launch_bounds__(TPR *rows_at_once(TPR)) void norm_fwd_kernel(const NormFwdArgs a)
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_fwd_kernel(const NormFwdArgs a)
 {
-    constexpr int ROWS = rows_at_once(TPR);
-    __shared__ float red[2][2 * (TPR / 64)];
+    constexpr int ROWS = TPR < 256 ? 256 / TPR : 1;
+    __shared__ float2_t red[2][ROWS * TPR / 64];
     const int t = threadIdx.x % TPR;
     const int64_t step = (int64_t)gridDim.x * ROWS;
     const float inv_d = 1.0f / (float)a.D;
-    for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR; row < a.N; row += step) {
-        float x[V][8];
-        float sum = 0.0f, none = 0.0f;
+    float g[V][8], b[V][8];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        param8(a.gamma, (t + v * TPR) * kChunk, a.D, 1.0f, g[v]);
+        param8(a.beta, (t + v * TPR) * kChunk, a.D, 0.0f, b[v]);
+    }
+    Raw<KIND> next[V];
+    const auto load = [&](int64_t row) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int col = (t + v * TPR) * kChunk;
-            const Raw<KIND> raw = col < a.D ? load8<KIND>(a.x, row, col, a.D) : zero8<KIND>();
-            widen8(raw, x[v]);
+            next[v] = col < a.D ? load8<KIND, false, false>(a.x, row, col, a.D) : zero8<KIND>();
         }
-        if (a.ckpt.codes) {
+    };
+    int64_t row = (int64_t)blockIdx.x * ROWS + __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);     // the same in all lanes of a wave
+    if (row < a.N) load(row);
+    for (; row < a.N; row += step) {       // one row a workgroup where TPR > 64: all of its threads are here
+        float x[V][8];
 #pragma unroll
-            for (int v = 0; v < V; ++v) ckpt_store8(a.ckpt, row, (t + v * TPR) * kChunk, a.D, x[v]);
-        }
-        float mean = 0.0f;
+        for (int v = 0; v < V; ++v) widen8(next[v], x[v]);
+        if (row + step < a.N) load(row + step);
+        float mean = 0.0f, none = 0.0f;
         if (a.layer) {
+            float sum = 0.0f;
 #pragma unroll
             for (int v = 0; v < V; ++v)
 #pragma unroll
@@ -83,13 +92,17 @@ __global__ __launch_bounds__(TPR *rows_at_once(TPR)) void norm_fwd_kernel(const 
             row_sum2<TPR>(sum, none, red[0]);
             mean = sum * inv_d;
         }
+        if (a.ckpt.codes) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) ckpt_store8(a.ckpt, row, (t + v * TPR) * kChunk, a.D, x[v]);
+        }
         float sq = 0.0f;
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float d = x[v][i] - mean;
-                if ((t + v * TPR) * kChunk + i < a.D) sq = fmaf(d, d, sq);
+                x[v][i] -= mean;
+                if ((t + v * TPR) * kChunk + i < a.D) sq = fmaf(x[v][i], x[v][i], sq);
             }
         row_sum2<TPR>(sq, none, red[1]);
         const float rstd = 1.0f / sqrtf(sq * inv_d + a.eps);
@@ -98,22 +111,19 @@ __global__ __launch_bounds__(TPR *rows_at_once(TPR)) void norm_fwd_kernel(const 
         for (int v = 0; v < V; ++v) {
             const int col = (t + v * TPR) * kChunk;
             if (col >= a.D) continue;
-            float g[8], b[8];
-            param8(a.gamma, col, a.D, 1.0f, g);
-            param8(a.beta, col, a.D, 0.0f, b);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[v][i] = fmaf((x[v][i] - mean) * rstd, g[i], b[i]);
+            for (int i = 0; i < 8; ++i) x[v][i] = fmaf(x[v][i] * rstd, g[v][i], b[v][i]);
             store8<OF32>(a.y.p, a.y.ld, row, col, a.D, x[v]);
         }
     }
 }
 
-// rows that no workgroup's registers hold: three sweeps over the row, the later ones from the caches
+// rows that no workgroup's registers hold, and rows shorter than a chunk: three sweeps over the row, the later ones from the caches
 template <int KIND, bool OF32>
 __global__ __launch_bounds__(1024) void norm_fwd_long_kernel(const NormFwdArgs a)
 {
     constexpr int TPR = 1024;
-    __shared__ float red[2][2 * (TPR / 64)];
+    __shared__ float2_t red[2][TPR / 64];
     const int t = threadIdx.x;
     const float inv_d = 1.0f / (float)a.D;
     for (int64_t row = blockIdx.x; row < a.N; row += gridDim.x) {
@@ -122,7 +132,7 @@ __global__ __launch_bounds__(1024) void norm_fwd_long_kernel(const NormFwdArgs a
         if (a.layer) {
             float sum = 0.0f;
             for (int col = t * kChunk; col < a.D; col += TPR * kChunk) {
-                widen8(load8<KIND>(a.x, row, col, a.D), x);
+                widen8(load8<KIND, true, false>(a.x, row, col, a.D), x);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum += x[i];
             }
@@ -130,7 +140,7 @@ __global__ __launch_bounds__(1024) void norm_fwd_long_kernel(const NormFwdArgs a
             mean = sum * inv_d;
         }
         for (int col = t * kChunk; col < a.D; col += TPR * kChunk) {
-            widen8(load8<KIND>(a.x, row, col, a.D), x);
+            widen8(load8<KIND, true, false>(a.x, row, col, a.D), x);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float d = x[i] - mean;
@@ -142,7 +152,7 @@ __global__ __launch_bounds__(1024) void norm_fwd_long_kernel(const NormFwdArgs a
         if (a.stats && t == 0) a.stats[row] = float2_t{mean, rstd};
         for (int base = 0; base < a.D; base += TPR * kChunk) {     // all lanes of a group stay for the checkpoint
             const int col = base + t * kChunk;
-            const Raw<KIND> raw = col < a.D ? load8<KIND>(a.x, row, col, a.D) : zero8<KIND>();
+            const Raw<KIND> raw = col < a.D ? load8<KIND, true, false>(a.x, row, col, a.D) : zero8<KIND>();
             widen8(raw, x);
             if (a.ckpt.codes) ckpt_store8(a.ckpt, row, col, a.D, x);
             if (col >= a.D) continue;
@@ -156,41 +166,69 @@ __global__ __launch_bounds__(1024) void norm_fwd_long_kernel(const NormFwdArgs a
     }
 }
 
-template <int KIND, bool GF32, bool OF32, int TPR, int V>
-__global__ __launch_bounds__(TPR *rows_at_once(TPR)) void norm_bwd_kernel(const NormBwdArgs a)
+// As the forward kernel, with blockDim.x / TPR rows at once; a thread also keeps the sums of its columns over all of its rows.  In the
+// end those of the workgroup's rows are added through LDS, in their order.
+template <int KIND, bool GF32, bool OF32, bool STREAM, int TPR, int V>
+__global__ __launch_bounds__(1024) void norm_bwd_kernel(const NormBwdArgs a)
 {
-    constexpr int ROWS = rows_at_once(TPR);
     constexpr int GKIND = GF32 ? kF32 : kBf16;
-    __shared__ float red[2][2 * (TPR / 64)];
-    const int t = threadIdx.x % TPR;
-    const int64_t step = (int64_t)gridDim.x * ROWS;
+    constexpr int CHUNKS = V * TPR;
+    __shared__ float2_t red[2][16];
+    extern __shared__ float all[];                  // first the weights, then [rows at once][D] sums
+    float4_t *const weight = reinterpret_cast<float4_t *>(all);      // [halves of a chunk][chunks]: not in registers, which the sums need
+    const int rows = blockDim.x / TPR, slot = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR), t = threadIdx.x % TPR;
+    const int64_t step = (int64_t)gridDim.x * rows;
     const float inv_d = 1.0f / (float)a.D;
     float sum_g[V][8], sum_b[V][8];
 #pragma unroll
-    for (int v = 0; v < V; ++v)
+    for (int v = 0; v < V; ++v) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum_g[v][i] = sum_b[v][i] = 0.0f;
+    }
+    for (int c = threadIdx.x; c < CHUNKS; c += blockDim.x) {
+        float w[8];
+        param8(a.gamma, c * kChunk, a.D, 1.0f, w);
+        weight[c] = float4_t{w[0], w[1], w[2], w[3]};
+        weight[CHUNKS + c] = float4_t{w[4], w[5], w[6], w[7]};
+    }
+    __syncthreads();
+    Raw<KIND> next_x[V];
+    Raw<GKIND> next_g[V];
+    float2_t next_st = {0.0f, 0.0f};
+    const auto load = [&](int64_t row) {             // a row past the end, and columns past the row's: zeros, which add nothing
+        const int D = row < a.N ? a.D : 0;
+        if (D) next_st = a.stats[row];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int col = (t + v * TPR) * kChunk;
+            next_x[v] = col < D ? load8<KIND, false, STREAM>(a.x, row, col, a.D) : zero8<KIND>();
+            next_g[v] = col < D ? load8<GKIND, false, STREAM>(a.dy, row, col, a.D) : zero8<GKIND>();
+        }
+    };
     int turn = 0;
-    for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR; row < a.N; row += step) {
-        const float2_t st = a.stats[row];
+    int64_t base = (int64_t)blockIdx.x * rows;      // of the workgroup: all of its threads stay together for the sums
+    load(base + slot);
+    for (; base < a.N; base += step) {
+        const int64_t row = base + slot;
+        if (TPR == 64 && row >= a.N) break;
+        const float2_t st = next_st;
         float h[V][8], g[V][8];
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int col = (t + v * TPR) * kChunk;
-            const Raw<KIND> rx = col < a.D ? load8<KIND>(a.x, row, col, a.D) : zero8<KIND>();
-            const Raw<GKIND> rg = col < a.D ? load8<GKIND>(a.dy, row, col, a.D) : zero8<GKIND>();
-            widen8(rx, h[v]);
-            widen8(rg, g[v]);
-            float w[8];
-            param8(a.gamma, col, a.D, 1.0f, w);
+            widen8(next_x[v], h[v]);
+            widen8(next_g[v], g[v]);
+        }
+        load(row + step);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const float4_t w[2] = {weight[t + v * TPR], weight[CHUNKS + t + v * TPR]};
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 h[v][i] = (h[v][i] - st.x) * st.y;
-                if (col + i >= a.D) h[v][i] = 0.0f;
                 sum_g[v][i] = fmaf(g[v][i], h[v][i], sum_g[v][i]);
                 sum_b[v][i] += g[v][i];
-                g[v][i] *= w[i];
+                g[v][i] *= w[i / 4][i & 3];
                 s1 += g[v][i];
                 s2 = fmaf(g[v][i], h[v][i], s2);
             }
@@ -201,50 +239,48 @@ __global__ __launch_bounds__(TPR *rows_at_once(TPR)) void norm_bwd_kernel(const 
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int col = (t + v * TPR) * kChunk;
-            if (col >= a.D) continue;
+            if (col >= a.D || row >= a.N) continue;
             float o[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) o[i] = st.y * (fmaf(-h[v][i], m2, g[v][i]) - m1);
             store8<OF32>(a.dx.p, a.dx.ld, row, col, a.D, o);
         }
     }
-    if (!a.part_g && !a.part_b) return;
-    if constexpr (ROWS > 1) {      // the waves' sums, in the order of the waves
-        __shared__ float all[ROWS][V * TPR * kChunk];
 #pragma unroll
-        for (int which = 0; which < 2; ++which) {
-            float *const part = which ? a.part_b : a.part_g;
-            if (which) __syncthreads();
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) all[threadIdx.x / TPR][(t + v * TPR) * kChunk + i] = which ? sum_b[v][i] : sum_g[v][i];
+    for (int which = 0; which < 2; ++which) {
+        float *const part = which ? a.part_b : a.part_g;
+        if (!part) continue;
+        if (rows > 1) {
             __syncthreads();
-            if (part)
-                for (int c = threadIdx.x; c < a.D; c += TPR * ROWS) {
-                    float s = all[0][c];
 #pragma unroll
-                    for (int r = 1; r < ROWS; ++r) s += all[r][c];
-                    part[blockIdx.x * a.part_ld + c] = s;
-                }
-        }
-    } else {
+            for (int v = 0; v < V; ++v) {
+                const int col = (t + v * TPR) * kChunk;
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int col = (t + v * TPR) * kChunk;
-            if (col >= a.D) continue;
-            if (a.part_g) store8<true>(a.part_g, a.part_ld, blockIdx.x, col, a.D, sum_g[v]);
-            if (a.part_b) store8<true>(a.part_b, a.part_ld, blockIdx.x, col, a.D, sum_b[v]);
+                for (int i = 0; i < 8; ++i)
+                    if (col + i < a.D) all[slot * a.D + col + i] = which ? sum_b[v][i] : sum_g[v][i];
+            }
+            __syncthreads();
+            for (int c = threadIdx.x; c < a.D; c += blockDim.x) {
+                float s = all[c];
+                for (int r = 1; r < rows; ++r) s += all[r * a.D + c];
+                part[blockIdx.x * a.part_ld + c] = s;
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int col = (t + v * TPR) * kChunk;
+                if (col < a.D) store8<true>(part, a.part_ld, blockIdx.x, col, a.D, which ? sum_b[v] : sum_g[v]);
+            }
         }
     }
 }
 
-// longer rows: the gradient of the input by two sweeps over a row ...
+// rows longer than that or shorter than a chunk: the gradient of the input by two sweeps over a row ...
 template <int KIND, bool GF32, bool OF32>
 __global__ __launch_bounds__(1024) void norm_bwd_long_kernel(const NormBwdArgs a)
 {
     constexpr int TPR = 1024, GKIND = GF32 ? kF32 : kBf16;
-    __shared__ float red[2][2 * (TPR / 64)];
+    __shared__ float2_t red[2][TPR / 64];
     const int t = threadIdx.x;
     const float inv_d = 1.0f / (float)a.D;
     int turn = 0;
@@ -253,8 +289,8 @@ __global__ __launch_bounds__(1024) void norm_bwd_long_kernel(const NormBwdArgs a
         float h[8], g[8], w[8];
         float s1 = 0.0f, s2 = 0.0f;
         for (int col = t * kChunk; col < a.D; col += TPR * kChunk) {
-            widen8(load8<KIND>(a.x, row, col, a.D), h);
-            widen8(load8<GKIND>(a.dy, row, col, a.D), g);
+            widen8(load8<KIND, true, false>(a.x, row, col, a.D), h);
+            widen8(load8<GKIND, true, false>(a.dy, row, col, a.D), g);
             param8(a.gamma, col, a.D, 1.0f, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -267,8 +303,8 @@ __global__ __launch_bounds__(1024) void norm_bwd_long_kernel(const NormBwdArgs a
         turn ^= 1;
         const float m1 = a.layer ? s1 * inv_d : 0.0f, m2 = s2 * inv_d;
         for (int col = t * kChunk; col < a.D; col += TPR * kChunk) {
-            widen8(load8<KIND>(a.x, row, col, a.D), h);
-            widen8(load8<GKIND>(a.dy, row, col, a.D), g);
+            widen8(load8<KIND, true, false>(a.x, row, col, a.D), h);
+            widen8(load8<GKIND, true, false>(a.dy, row, col, a.D), g);
             param8(a.gamma, col, a.D, 1.0f, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) g[i] = st.y * (fmaf(-((h[i] - st.x) * st.y), m2, g[i] * w[i]) - m1);
@@ -282,14 +318,14 @@ template <int KIND, bool GF32>
 __global__ __launch_bounds__(256) void norm_params_long_kernel(const NormBwdArgs a)
 {
     constexpr int GKIND = GF32 ? kF32 : kBf16;
-    const int64_t col = ((int64_t)blockIdx.x * 256 + threadIdx.x) * kChunk;
+    const int col = (blockIdx.x * 256 + threadIdx.x) * kChunk;
     if (col >= a.D) return;
     float sum_g[8] = {}, sum_b[8] = {};
     for (int64_t row = blockIdx.y; row < a.N; row += gridDim.y) {
         const float2_t st = a.stats[row];
         float h[8], g[8];
-        widen8(load8<KIND>(a.x, row, col, a.D), h);
-        widen8(load8<GKIND>(a.dy, row, col, a.D), g);
+        widen8(load8<KIND, true, false>(a.x, row, col, a.D), h);
+        widen8(load8<GKIND, true, false>(a.dy, row, col, a.D), g);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             sum_g[i] = fmaf(g[i], (h[i] - st.x) * st.y, sum_g[i]);
@@ -300,7 +336,9 @@ __global__ __launch_bounds__(256) void norm_params_long_kernel(const NormBwdArgs
     if (a.part_b) store8<true>(a.part_b, a.part_ld, blockIdx.y, col, a.D, sum_b);
 }
 
-// The partial sums of G workgroups, in their order: a workgroup takes 64 columns, each of its 16 waves every sixteenth partial sum.
+// The partial sums of G <= 256 workgroups, in an order of their own: a workgroup takes 64 columns, each of its 16 waves every sixteenth partial
+// sum (all of a thread's loads are on their way at once), then the waves' sums in their order.
+constexpr int kMostPartials = 256;
 __global__ __launch_bounds__(1024) void norm_params_reduce_kernel(const float *part_g, const float *part_b, int64_t part_ld, int G, int D, float *dgamma, float *dbeta)
 {
     __shared__ float red[16][64];
@@ -309,8 +347,13 @@ __global__ __launch_bounds__(1024) void norm_params_reduce_kernel(const float *p
     const float *const part = blockIdx.y ? part_b : part_g;
     float *const out = blockIdx.y ? dbeta : dgamma;
     float s = 0.0f;
-    if (out && c < D)
-        for (int g = w; g < G; g += 16) s += part[g * part_ld + c];
+    if (out && c < D) {
+        float v[kMostPartials / 16];
+#pragma unroll
+        for (int i = 0; i < kMostPartials / 16; ++i) v[i] = w + 16 * i < G ? part[(w + 16 * i) * part_ld + c] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < kMostPartials / 16; ++i) s += v[i];
+    }
     red[w][lane] = s;
     __syncthreads();
     if (w == 0 && out && c < D) {
@@ -321,43 +364,67 @@ __global__ __launch_bounds__(1024) void norm_params_reduce_kernel(const float *p
 }
 
 constexpr int kMaxHeldRow = 16384;      // longest row that a workgroup's registers hold
-constexpr int kFwdBlocks = 8192;        // most workgroups of a forward launch
-constexpr int kBwdBlocks = 512;         // most workgroups, and partial sums, of a backward launch
+constexpr int kLongBlocks = 8192;       // most workgroups where a row is longer
 
+// threads that hold a row
+bool held(int64_t D) { return D >= kChunk && D <= kMaxHeldRow; }
+int threads_of_row(int64_t D) { return D <= 1024 ? 64 : D <= 4096 ? 256 : D <= 8192 ? 512 : 1024; }
+
+// rows that a workgroup of the backward kernel takes at once, as many as give every CU a workgroup and at most 1024 threads, and its workgroups: each leaves
+// a partial sum of D columns, so there is one a CU
+int64_t bwd_rows(int64_t N, int64_t D)
+{
+    const int64_t most = !held(D) ? 1 : 1024 / threads_of_row(D), want = (N + kMostPartials - 1) / kMostPartials;
+    return want < 1 ? 1 : want < most ? want : most;
+}
 int64_t bwd_blocks(int64_t N, int64_t D)
 {
-    const int64_t rows = D <= 1024 ? 4 : 1;
-    const int64_t want = (N + rows - 1) / rows;
-    const int64_t most = D <= 8192 ? kBwdBlocks : kBwdBlocks / 2;
-    return want < most ? want : most;
+    const int64_t rows = bwd_rows(N, D), want = (N + rows - 1) / rows;
+    return want < kMostPartials ? want : kMostPartials;
+}
+
+template <int KIND, bool OF32, int TPR, int V> void run_norm_fwd(const NormFwdArgs &a, hipStream_t st)
+{
+    constexpr int THREADS = TPR < 256 ? 256 : TPR, ROWS = THREADS / TPR;
+    constexpr int MOST = 256 * (1024 / THREADS);       // 16 waves a CU, which then walk over their rows
+    const int64_t want = (a.N + ROWS - 1) / ROWS;
+    norm_fwd_kernel<KIND, OF32, TPR, V><<<(unsigned)(want < MOST ? want : MOST), THREADS, 0, st>>>(a);
 }
 
 template <int KIND, bool OF32> void run_norm_fwd(const NormFwdArgs &a, hipStream_t st)
 {
-    const int64_t want4 = (a.N + 3) / 4;
-    const unsigned waves = (unsigned)(want4 < kFwdBlocks ? want4 : kFwdBlocks), rows = (unsigned)(a.N < kFwdBlocks ? a.N : kFwdBlocks);
-    if (a.D <= 512) norm_fwd_kernel<KIND, OF32, 64, 1><<<waves, 256, 0, st>>>(a);
-    else if (a.D <= 1024) norm_fwd_kernel<KIND, OF32, 64, 2><<<waves, 256, 0, st>>>(a);
-    else if (a.D <= 2048) norm_fwd_kernel<KIND, OF32, 64, 4><<<waves, 256, 0, st>>>(a);
-    else if (a.D <= 4096) norm_fwd_kernel<KIND, OF32, 256, 2><<<rows, 256, 0, st>>>(a);
-    else if (a.D <= 8192) norm_fwd_kernel<KIND, OF32, 256, 4><<<rows, 256, 0, st>>>(a);
-    else if (a.D <= kMaxHeldRow) norm_fwd_kernel<KIND, OF32, 1024, 2><<<rows, 1024, 0, st>>>(a);
-    else norm_fwd_long_kernel<KIND, OF32><<<rows, 1024, 0, st>>>(a);
+    if (!held(a.D)) norm_fwd_long_kernel<KIND, OF32><<<(unsigned)(a.N < kLongBlocks ? a.N : kLongBlocks), 1024, 0, st>>>(a);
+    else if (a.D <= 512) run_norm_fwd<KIND, OF32, 64, 1>(a, st);
+    else if (a.D <= 1024) run_norm_fwd<KIND, OF32, 64, 2>(a, st);
+    else if (a.D <= 2048) run_norm_fwd<KIND, OF32, 256, 1>(a, st);
+    else if (a.D <= 4096) run_norm_fwd<KIND, OF32, 256, 2>(a, st);
+    else if (a.D <= 8192) run_norm_fwd<KIND, OF32, 512, 2>(a, st);
+    else run_norm_fwd<KIND, OF32, 1024, 2>(a, st);
+}
+
+template <int KIND, bool GF32, bool OF32, int TPR, int V> void run_norm_bwd(const NormBwdArgs &a, unsigned blocks, hipStream_t st)
+{
+    const unsigned rows = (unsigned)bwd_rows(a.N, a.D);
+    const size_t weights = (size_t)V * TPR * kChunk, sums = rows > 1 ? rows * (size_t)a.D : 0;
+    const size_t lds = (weights > sums ? weights : sums) * sizeof(float);
+    const double each = (GF32 ? 4 : 2) + (KIND == kF32 ? 4 : KIND == kBf16 ? 2 : 1) + (OF32 ? 4 : 2);
+    if (streams((double)a.N * a.D * each)) norm_bwd_kernel<KIND, GF32, OF32, true, TPR, V><<<blocks, rows * TPR, lds, st>>>(a);
+    else norm_bwd_kernel<KIND, GF32, OF32, false, TPR, V><<<blocks, rows * TPR, lds, st>>>(a);
 }
 
 template <int KIND, bool GF32, bool OF32> void run_norm_bwd(const NormBwdArgs &a, unsigned blocks, hipStream_t st)
 {
-    if (a.D <= 512) norm_bwd_kernel<KIND, GF32, OF32, 64, 1><<<blocks, 256, 0, st>>>(a);
-    else if (a.D <= 1024) norm_bwd_kernel<KIND, GF32, OF32, 64, 2><<<blocks, 256, 0, st>>>(a);
-    else if (a.D <= 2048) norm_bwd_kernel<KIND, GF32, OF32, 256, 1><<<blocks, 256, 0, st>>>(a);
-    else if (a.D <= 4096) norm_bwd_kernel<KIND, GF32, OF32, 256, 2><<<blocks, 256, 0, st>>>(a);
-    else if (a.D <= 8192) norm_bwd_kernel<KIND, GF32, OF32, 256, 4><<<blocks, 256, 0, st>>>(a);
-    else if (a.D <= kMaxHeldRow) norm_bwd_kernel<KIND, GF32, OF32, 1024, 2><<<blocks, 1024, 0, st>>>(a);
-    else {
-        norm_bwd_long_kernel<KIND, GF32, OF32><<<(unsigned)(a.N < kFwdBlocks ? a.N : kFwdBlocks), 1024, 0, st>>>(a);
+    if (!held(a.D)) {
+        norm_bwd_long_kernel<KIND, GF32, OF32><<<(unsigned)(a.N < kLongBlocks ? a.N : kLongBlocks), 1024, 0, st>>>(a);
         if (a.part_g || a.part_b)
             norm_params_long_kernel<KIND, GF32><<<dim3((unsigned)((a.D + 2047) / 2048), blocks), 256, 0, st>>>(a);
     }
+    else if (a.D <= 512) run_norm_bwd<KIND, GF32, OF32, 64, 1>(a, blocks, st);
+    else if (a.D <= 1024) run_norm_bwd<KIND, GF32, OF32, 64, 2>(a, blocks, st);
+    else if (a.D <= 2048) run_norm_bwd<KIND, GF32, OF32, 256, 1>(a, blocks, st);
+    else if (a.D <= 4096) run_norm_bwd<KIND, GF32, OF32, 256, 2>(a, blocks, st);
+    else if (a.D <= 8192) run_norm_bwd<KIND, GF32, OF32, 512, 2>(a, blocks, st);
+    else run_norm_bwd<KIND, GF32, OF32, 1024, 2>(a, blocks, st);
 }
 
 }  // namespace

@@ -34,41 +34,77 @@ template <> struct Raw<kBf16> { u32x4 q; };
 template <> struct Raw<kF32> { float4_t lo, hi; };
 template <> struct Raw<kCkpt8> { u32x2 q; uint32_t e; };
 
-// elements [col, col + 8) of a row; those at or past n are zeros (n > col: at least one is there)
-template <int KIND>
-__device__ __forceinline__ Raw<KIND> load8(const RowSrc &s, int64_t row, int64_t col, int64_t n)
+// STREAM: past the caches (see streams())
+template <typename T, bool STREAM> __device__ __forceinline__ T load_as(const void *p)
+{
+    if constexpr (STREAM) return __builtin_nontemporal_load(static_cast<const T *>(p));
+    else return *static_cast<const T *>(p);
+}
+
+// v moved down by `by` elements (0 to 7), zeros above
+__device__ __forceinline__ u32x4 move_down(u32x4 v, uint32_t by)      // bf16
+{
+    const uint32_t half = (by & 1) * 16;
+    v = u32x4{__builtin_amdgcn_alignbit(v[1], v[0], half), __builtin_amdgcn_alignbit(v[2], v[1], half), __builtin_amdgcn_alignbit(v[3], v[2], half), v[3] >> half};
+    if (by & 2) v = u32x4{v[1], v[2], v[3], 0};
+    if (by & 4) v = u32x4{v[2], v[3], 0, 0};
+    return v;
+}
+__device__ __forceinline__ u32x2 move_down(u32x2 v, uint32_t by)      // bytes
+{
+    const uint64_t u = (((uint64_t)v[1] << 32) | v[0]) >> (8 * by);
+    return u32x2{(uint32_t)u, (uint32_t)(u >> 32)};
+}
+__device__ __forceinline__ void move_down(float4_t &lo, float4_t &hi, uint32_t by)
+{
+    if (by & 1) lo = float4_t{lo[1], lo[2], lo[3], hi[0]}, hi = float4_t{hi[1], hi[2], hi[3], 0.0f};
+    if (by & 2) lo = float4_t{lo[2], lo[3], hi[0], hi[1]}, hi = float4_t{hi[2], hi[3], 0.0f, 0.0f};
+    if (by & 4) lo = hi, hi = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+}
+
+// Elements [col, col + 8) of a row; those at or past n are zeros (n > col: at least one is there).  A chunk that the row's end cuts
+// is read as the row's last eight elements and moved down, where there are eight (one load, few registers); else
+// element by element.  SHORT: rows may have fewer than eight.  Whether rows have such a chunk is asked of the row length, the same for all lanes: a
+// question to each lane would be passed with the lanes masked and wait for the load on the way (SwiGLU backward 129 us instead of 107).
+template <int KIND, bool SHORT, bool STREAM, typename I>
+__device__ __forceinline__ Raw<KIND> load8(const RowSrc &s, int64_t row, I col, I n)
 {
     Raw<KIND> r;
+    const I at = col + kChunk > n ? n - kChunk : col;     // below zero in a row of fewer than eight
+    const uint32_t by = (uint32_t)(col - at);
     if constexpr (KIND == kBf16) {
-        const uint16_t *p = static_cast<const uint16_t *>(s.p) + row * s.ld + col;
-        if (col + kChunk <= n) {
-            r.q = *reinterpret_cast<const bf16x8_at2 *>(p);
+        const uint16_t *const p = static_cast<const uint16_t *>(s.p) + row * s.ld;
+        if (!SHORT || n >= kChunk) {
+            r.q = load_as<bf16x8_at2, STREAM>(p + at);
+            if (n % kChunk != 0) r.q = move_down(r.q, by);
         } else {
             r.q = u32x4{0, 0, 0, 0};
 #pragma unroll
             for (int i = 0; i < kChunk - 1; ++i)
-                if (col + i < n) r.q[i / 2] |= (uint32_t)p[i] << (16 * (i & 1));
+                if (i < n) r.q[i / 2] |= (uint32_t)p[i] << (16 * (i & 1));
         }
     } else if constexpr (KIND == kF32) {
-        const float *p = static_cast<const float *>(s.p) + row * s.ld + col;
-        if (col + kChunk <= n) {
-            r.lo = *reinterpret_cast<const f32x4_at4 *>(p);
-            r.hi = *reinterpret_cast<const f32x4_at4 *>(p + 4);
+        const float *const p = static_cast<const float *>(s.p) + row * s.ld;
+        if (!SHORT || n >= kChunk) {
+            r.lo = load_as<f32x4_at4, STREAM>(p + at);
+            r.hi = load_as<f32x4_at4, STREAM>(p + at + 4);
+            if (n % kChunk != 0) move_down(r.lo, r.hi, by);
         } else {
             r.lo = r.hi = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int i = 0; i < kChunk - 1; ++i)
-                if (col + i < n) (i < 4 ? r.lo : r.hi)[i & 3] = p[i];
+                if (i < n) (i < 4 ? r.lo : r.hi)[i & 3] = p[i];
         }
     } else {
-        const uint8_t *p = static_cast<const uint8_t *>(s.p) + row * s.ld + col;
-        if (col + kChunk <= n) {
-            r.q = *reinterpret_cast<const code8_at1 *>(p);
+        const uint8_t *const p = static_cast<const uint8_t *>(s.p) + row * s.ld;
+        if (!SHORT || n >= kChunk) {
+            r.q = load_as<code8_at1, STREAM>(p + at);
+            if (n % kChunk != 0) r.q = move_down(r.q, by);
         } else {
             r.q = u32x2{0, 0};
 #pragma unroll
             for (int i = 0; i < kChunk - 1; ++i)
-                if (col + i < n) r.q[i / 4] |= (uint32_t)p[i] << (8 * (i & 3));
+                if (i < n) r.q[i / 4] |= (uint32_t)p[i] << (8 * (i & 3));
         }
         r.e = s.exps[row * s.groups + col / kCkptGroup];
     }
@@ -117,11 +153,11 @@ __device__ __forceinline__ void widen8(const Raw<kCkpt8> &r, float (&v)[8])
 
 // ---- stores -----------------------------------------------------------------------------------
 
-template <bool F32>
-__device__ __forceinline__ void store8(void *out, int64_t ld, int64_t row, int64_t col, int64_t n, const float (&v)[8])
+template <bool F32, typename I>
+__device__ __forceinline__ void store8(void *out, int64_t ld, int64_t row, I col, I n, const float (&v)[8])
 {
     if constexpr (F32) {
-        float *p = static_cast<float *>(out) + row * ld + col;
+        float *const p = static_cast<float *>(out) + row * ld + col;
         if (col + kChunk <= n) {
             *reinterpret_cast<f32x4_at4 *>(p) = f32x4_at4{v[0], v[1], v[2], v[3]};
             *reinterpret_cast<f32x4_at4 *>(p + 4) = f32x4_at4{v[4], v[5], v[6], v[7]};
@@ -131,7 +167,7 @@ __device__ __forceinline__ void store8(void *out, int64_t ld, int64_t row, int64
                 if (col + i < n) p[i] = v[i];
         }
     } else {
-        uint16_t *p = static_cast<uint16_t *>(out) + row * ld + col;
+        uint16_t *const p = static_cast<uint16_t *>(out) + row * ld + col;
         const u32x4 q = {bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
         if (col + kChunk <= n) {
             *reinterpret_cast<bf16x8_at2 *>(p) = q;
@@ -149,7 +185,8 @@ __device__ __forceinline__ void store8(void *out, int64_t ld, int64_t row, int64
 // row's end with zeros).  a = max |v| over the finite values, e the least integer with a <= 1.75 * 2^(8 + e) = 448 * 2^e within
 // [-126, 120]: both 2^e and 2^-e are then ordinary binary32 numbers, the product v * 2^-e is exact (rounded below 2^-126, far
 // under half of the smallest code) and the conversion's rounding is the only one.  Values that are not finite become the NaN 0x7F.
-__device__ __forceinline__ void ckpt_store8(const CkptOut &o, int64_t row, int64_t col, int64_t n, const float (&v)[8])
+template <typename I>
+__device__ __forceinline__ void ckpt_store8(const CkptOut &o, int64_t row, I col, I n, const float (&v)[8])
 {
     uint32_t a = 0;
 #pragma unroll
@@ -195,35 +232,44 @@ __device__ __forceinline__ void ckpt_store8(const CkptOut &o, int64_t row, int64
 
 // ---- sums over the threads of a row -----------------------------------------------------------
 
+// over the 64 lanes of a wave, the same bits in each: four exchanges inside rows of 16 lanes, then between the rows
 __device__ __forceinline__ float wave_sum(float v)
 {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-    return v;
+    v += u2f(dpp<DPP_QUAD_XOR1>(f2u(v)));
+    v += u2f(dpp<DPP_QUAD_XOR2>(f2u(v)));
+    v += u2f(dpp<DPP_ROW_HALF_MIRROR>(f2u(v)));
+    v += u2f(dpp<DPP_ROW_MIRROR>(f2u(v)));
+    const auto a = __builtin_amdgcn_permlane16_swap(f2u(v), f2u(v), false, false);
+    v = u2f(a[0]) + u2f(a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(f2u(v), f2u(v), false, false);
+    return u2f(b[0]) + u2f(b[1]);
 }
 
-// Sums of two numbers over the TPR threads that hold a row; every one of them gets both.  red: 2 floats per wave of the workgroup;
-// a workgroup that sums again passes the other half of a doubled array, so that no barrier is needed before the next sum.
+// Sums of two numbers over the TPR threads that hold a row; every one of them gets both.  red: two floats per wave of the workgroup, all of whose
+// threads call this together where TPR > 64; a workgroup that sums again passes the other half of a doubled array, so that no barrier is
+// needed before the next sum.
 template <int TPR>
-__device__ __forceinline__ void row_sum2(float &a, float &b, float *red)
+__device__ __forceinline__ void row_sum2(float &a, float &b, float2_t *red)
 {
     a = wave_sum(a);
     b = wave_sum(b);
     if constexpr (TPR > 64) {
         constexpr int W = TPR / 64;
         const int w = threadIdx.x >> 6;
-        if ((threadIdx.x & 63) == 0) {
-            red[2 * w] = a;
-            red[2 * w + 1] = b;
-        }
+        if ((threadIdx.x & 63) == 0) red[w] = float2_t{a, b};
         __syncthreads();
-        a = red[0];
-        b = red[1];
-#pragma unroll
-        for (int i = 1; i < W; ++i) {
-            a += red[2 * i];
-            b += red[2 * i + 1];
-        }
+        const float2_t m = red[w / W * W + (threadIdx.x & (W - 1))];     // W lanes add what the row's W waves left
+        a = m.x;
+        b = m.y;
+        const auto both = [&](auto step) {
+            a += u2f(step(f2u(a)));
+            b += u2f(step(f2u(b)));
+        };
+        static_assert(W == 4 || W == 8 || W == 16);
+        both([](uint32_t v) { return dpp<DPP_QUAD_XOR1>(v); });
+        both([](uint32_t v) { return dpp<DPP_QUAD_XOR2>(v); });
+        if constexpr (W >= 8) both([](uint32_t v) { return dpp<DPP_ROW_HALF_MIRROR>(v); });
+        if constexpr (W >= 16) both([](uint32_t v) { return dpp<DPP_ROW_MIRROR>(v); });
     }
 }
 
