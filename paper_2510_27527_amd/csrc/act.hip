@@ -76,7 +76,7 @@ template <int KIND, bool STREAM>
 __device__ __forceinline__ Raw<KIND> load8_at(const RowSrc &s, int64_t row, int col, int n, int at)
 {
     const int size = KIND == kF32 ? 4 : 2;
-    return load8<KIND, true, STREAM>(RowSrc{static_cast<const char *>(s.p) + (int64_t)at * size, nullptr, s.ld, 0, s.kind}, row, col, n);
+    return load8<KIND, false, STREAM>(RowSrc{static_cast<const char *>(s.p) + (int64_t)at * size, nullptr, s.ld, 0, s.kind}, row, col, n);
 }
 template <int KIND, bool STREAM>
 __device__ __forceinline__ Raw<KIND> load8_or_0(const RowSrc &s, int64_t row, int col, int n, int at)
@@ -104,17 +104,17 @@ __global__ __launch_bounds__(kThreads) void act_fwd_kernel(const ActArgs a)
             float u[8];
             widen8(in.b, u);
             if (a.ckpt.codes) {
-                ckpt_store8(a.ckpt, 2 * row, col, F, x);
-                ckpt_store8(a.ckpt, 2 * row + 1, col, F, u);
+                ckpt_store8<false>(a.ckpt, 2 * row, col, F, x);
+                ckpt_store8<false>(a.ckpt, 2 * row + 1, col, F, u);
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) o[i] = x[i] * sigmoid(x[i]).pos * u[i];
         } else {
-            if (a.ckpt.codes) ckpt_store8(a.ckpt, row, col, F, x);
+            if (a.ckpt.codes) ckpt_store8<false>(a.ckpt, row, col, F, x);
 #pragma unroll
             for (int i = 0; i < 8; ++i) o[i] = x[i] * sigmoid(gelu_z(gelu_in(x[i]))).pos;
         }
-        if (col < F) store8<OF32>(a.out.p, a.out.ld, row, col, F, o);
+        if (col < F) store8<OF32, false>(a.out.p, a.out.ld, row, col, F, o);
     });
 }
 
@@ -127,14 +127,14 @@ __global__ __launch_bounds__(kThreads) void act_bwd_kernel(const ActArgs a)
     const auto load = [&](int64_t row, int col) {
         In in;
         if (col >= F) return in;
-        in.da = load8<GKIND, true, STREAM>(a.da, row, col, F);
+        in.da = load8<GKIND, false, STREAM>(a.da, row, col, F);
         if constexpr (ACT == kGelu) {
-            in.a = load8<KIND, true, STREAM>(a.h, row, col, F);
+            in.a = load8<KIND, false, STREAM>(a.h, row, col, F);
         } else if constexpr (KIND == kCkpt8) {
-            in.a = load8<KIND, true, STREAM>(a.h, 2 * row, col, F);
-            in.b = load8<KIND, true, STREAM>(a.h, 2 * row + 1, col, F);
+            in.a = load8<KIND, false, STREAM>(a.h, 2 * row, col, F);
+            in.b = load8<KIND, false, STREAM>(a.h, 2 * row + 1, col, F);
         } else {
-            in.a = load8<KIND, true, STREAM>(a.h, row, col, F);
+            in.a = load8<KIND, false, STREAM>(a.h, row, col, F);
             in.b = load8_at<KIND, STREAM>(a.h, row, col, F, F);
         }
         return in;
@@ -154,8 +154,8 @@ __global__ __launch_bounds__(kThreads) void act_bwd_kernel(const ActArgs a)
                 x[i] = da[i] * u[i] * s.pos * fmaf(x[i], s.neg, 1.0f);
                 u[i] = du;
             }
-            store8<OF32>(a.out.p, a.out.ld, row, col, F, x);
-            store8<OF32>(static_cast<char *>(a.out.p) + (int64_t)F * (OF32 ? 4 : 2), a.out.ld, row, col, F, u);
+            store8<OF32, false>(a.out.p, a.out.ld, row, col, F, x);
+            store8<OF32, false>(static_cast<char *>(a.out.p) + (int64_t)F * (OF32 ? 4 : 2), a.out.ld, row, col, F, u);
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -164,7 +164,7 @@ __global__ __launch_bounds__(kThreads) void act_bwd_kernel(const ActArgs a)
                 const float slope = kGeluC * fmaf(3.0f * kGeluA * c, c, 1.0f);
                 x[i] = da[i] * fmaf(c * s.pos * s.neg, slope, s.pos);
             }
-            store8<OF32>(a.out.p, a.out.ld, row, col, F, x);
+            store8<OF32, false>(a.out.p, a.out.ld, row, col, F, x);
         }
     });
 }
@@ -176,19 +176,19 @@ __global__ __launch_bounds__(kThreads) void ckpt8_save_kernel(const CopyArgs a)
                       [&](int64_t row, int col, const Raw<KIND> &in) {
         float x[8];
         widen8(in, x);
-        ckpt_store8(a.ckpt, row, col, a.n.cols, x);
+        ckpt_store8<false>(a.ckpt, row, col, a.n.cols, x);
     });
 }
 
 template <bool OF32, bool STREAM>
 __global__ __launch_bounds__(kThreads) void ckpt8_load_kernel(const CopyArgs a)
 {
-    for_chunks<kRows>(a.n, [&](int64_t row, int col) { return col < a.n.cols ? load8<kCkpt8, true, STREAM>(a.src, row, col, a.n.cols) : zero8<kCkpt8>(); },
+    for_chunks<kRows>(a.n, [&](int64_t row, int col) { return col < a.n.cols ? load8<kCkpt8, false, STREAM>(a.src, row, col, a.n.cols) : zero8<kCkpt8>(); },
                       [&](int64_t row, int col, const Raw<kCkpt8> &in) {
         if (col >= a.n.cols) return;
         float x[8];
         widen8(in, x);
-        store8<OF32>(a.out.p, a.out.ld, row, col, a.n.cols, x);
+        store8<OF32, false>(a.out.p, a.out.ld, row, col, a.n.cols, x);
     });
 }
 

@@ -72,7 +72,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_fwd_kernel(const N
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int col = (t + v * TPR) * kChunk;
-            next[v] = col < a.D ? load8<KIND, false, false>(a.x, row, col, a.D) : zero8<KIND>();
+            next[v] = col < a.D ? load8<KIND, true, false>(a.x, row, col, a.D) : zero8<KIND>();
         }
     };
     int64_t row = (int64_t)blockIdx.x * ROWS + __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);     // the same in all lanes of a wave
@@ -94,7 +94,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_fwd_kernel(const N
         }
         if (a.ckpt.codes) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) ckpt_store8(a.ckpt, row, (t + v * TPR) * kChunk, a.D, x[v]);
+            for (int v = 0; v < V; ++v) ckpt_store8<true>(a.ckpt, row, (t + v * TPR) * kChunk, a.D, x[v]);
         }
         float sq = 0.0f;
 #pragma unroll
@@ -113,7 +113,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_fwd_kernel(const N
             if (col >= a.D) continue;
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[v][i] = fmaf(x[v][i] * rstd, g[v][i], b[v][i]);
-            store8<OF32>(a.y.p, a.y.ld, row, col, a.D, x[v]);
+            store8<OF32, true>(a.y.p, a.y.ld, row, col, a.D, x[v]);
         }
     }
 }
@@ -132,7 +132,7 @@ __global__ __launch_bounds__(1024) void norm_fwd_long_kernel(const NormFwdArgs a
         if (a.layer) {
             float sum = 0.0f;
             for (int col = t * kChunk; col < a.D; col += TPR * kChunk) {
-                widen8(load8<KIND, true, false>(a.x, row, col, a.D), x);
+                widen8(load8<KIND, false, false>(a.x, row, col, a.D), x);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum += x[i];
             }
@@ -140,7 +140,7 @@ __global__ __launch_bounds__(1024) void norm_fwd_long_kernel(const NormFwdArgs a
             mean = sum * inv_d;
         }
         for (int col = t * kChunk; col < a.D; col += TPR * kChunk) {
-            widen8(load8<KIND, true, false>(a.x, row, col, a.D), x);
+            widen8(load8<KIND, false, false>(a.x, row, col, a.D), x);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float d = x[i] - mean;
@@ -152,16 +152,16 @@ __global__ __launch_bounds__(1024) void norm_fwd_long_kernel(const NormFwdArgs a
         if (a.stats && t == 0) a.stats[row] = float2_t{mean, rstd};
         for (int base = 0; base < a.D; base += TPR * kChunk) {     // all lanes of a group stay for the checkpoint
             const int col = base + t * kChunk;
-            const Raw<KIND> raw = col < a.D ? load8<KIND, true, false>(a.x, row, col, a.D) : zero8<KIND>();
+            const Raw<KIND> raw = col < a.D ? load8<KIND, false, false>(a.x, row, col, a.D) : zero8<KIND>();
             widen8(raw, x);
-            if (a.ckpt.codes) ckpt_store8(a.ckpt, row, col, a.D, x);
+            if (a.ckpt.codes) ckpt_store8<false>(a.ckpt, row, col, a.D, x);
             if (col >= a.D) continue;
             float g[8], b[8];
             param8(a.gamma, col, a.D, 1.0f, g);
             param8(a.beta, col, a.D, 0.0f, b);
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[i] = fmaf((x[i] - mean) * rstd, g[i], b[i]);
-            store8<OF32>(a.y.p, a.y.ld, row, col, a.D, x);
+            store8<OF32, false>(a.y.p, a.y.ld, row, col, a.D, x);
         }
     }
 }
@@ -174,7 +174,7 @@ __global__ __launch_bounds__(1024) void norm_bwd_kernel(const NormBwdArgs a)
     constexpr int GKIND = GF32 ? kF32 : kBf16;
     constexpr int CHUNKS = V * TPR;
     __shared__ float2_t red[2][16];
-    extern __shared__ float all[];                  // first the weights, then [rows at once][D] sums
+    extern __shared__ float all[];                  // first the weights, then the sums
     float4_t *const weight = reinterpret_cast<float4_t *>(all);      // [halves of a chunk][chunks]: not in registers, which the sums need
     const int rows = blockDim.x / TPR, slot = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR), t = threadIdx.x % TPR;
     const int64_t step = (int64_t)gridDim.x * rows;
@@ -185,13 +185,6 @@ __global__ __launch_bounds__(1024) void norm_bwd_kernel(const NormBwdArgs a)
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum_g[v][i] = sum_b[v][i] = 0.0f;
     }
-    for (int c = threadIdx.x; c < CHUNKS; c += blockDim.x) {
-        float w[8];
-        param8(a.gamma, c * kChunk, a.D, 1.0f, w);
-        weight[c] = float4_t{w[0], w[1], w[2], w[3]};
-        weight[CHUNKS + c] = float4_t{w[4], w[5], w[6], w[7]};
-    }
-    __syncthreads();
     Raw<KIND> next_x[V];
     Raw<GKIND> next_g[V];
     float2_t next_st = {0.0f, 0.0f};
@@ -201,36 +194,46 @@ __global__ __launch_bounds__(1024) void norm_bwd_kernel(const NormBwdArgs a)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int col = (t + v * TPR) * kChunk;
-            next_x[v] = col < D ? load8<KIND, false, STREAM>(a.x, row, col, a.D) : zero8<KIND>();
-            next_g[v] = col < D ? load8<GKIND, false, STREAM>(a.dy, row, col, a.D) : zero8<GKIND>();
+            next_x[v] = col < D ? load8<KIND, true, STREAM>(a.x, row, col, a.D) : zero8<KIND>();
+            next_g[v] = col < D ? load8<GKIND, true, STREAM>(a.dy, row, col, a.D) : zero8<GKIND>();
         }
     };
     int turn = 0;
     int64_t base = (int64_t)blockIdx.x * rows;      // of the workgroup: all of its threads stay together for the sums
     load(base + slot);
+    for (int c = threadIdx.x; c < CHUNKS; c += blockDim.x) {
+        float w[8];
+        param8(a.gamma, c * kChunk, a.D, 1.0f, w);
+        weight[c] = float4_t{w[0], w[1], w[2], w[3]};
+        weight[CHUNKS + c] = float4_t{w[4], w[5], w[6], w[7]};
+    }
+    __syncthreads();
     for (; base < a.N; base += step) {
         const int64_t row = base + slot;
         if (TPR == 64 && row >= a.N) break;
         const float2_t st = next_st;
-        float h[V][8], g[V][8];
+        float h[V][8];
+        Raw<GKIND> dy[V];                            // widened twice: registers
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             widen8(next_x[v], h[v]);
-            widen8(next_g[v], g[v]);
+            dy[v] = next_g[v];
         }
         load(row + step);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const float4_t w[2] = {weight[t + v * TPR], weight[CHUNKS + t + v * TPR]};
+            float g[8];
+            widen8(dy[v], g);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 h[v][i] = (h[v][i] - st.x) * st.y;
-                sum_g[v][i] = fmaf(g[v][i], h[v][i], sum_g[v][i]);
-                sum_b[v][i] += g[v][i];
-                g[v][i] *= w[i / 4][i & 3];
-                s1 += g[v][i];
-                s2 = fmaf(g[v][i], h[v][i], s2);
+                sum_g[v][i] = fmaf(g[i], h[v][i], sum_g[v][i]);
+                sum_b[v][i] += g[i];
+                g[i] *= w[i / 4][i & 3];
+                s1 += g[i];
+                s2 = fmaf(g[i], h[v][i], s2);
             }
         }
         row_sum2<TPR>(s1, s2, red[turn]);
@@ -240,37 +243,50 @@ __global__ __launch_bounds__(1024) void norm_bwd_kernel(const NormBwdArgs a)
         for (int v = 0; v < V; ++v) {
             const int col = (t + v * TPR) * kChunk;
             if (col >= a.D || row >= a.N) continue;
+            const float4_t w[2] = {weight[t + v * TPR], weight[CHUNKS + t + v * TPR]};
             float o[8];
+            widen8(dy[v], o);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) o[i] = st.y * (fmaf(-h[v][i], m2, g[v][i]) - m1);
-            store8<OF32>(a.dx.p, a.dx.ld, row, col, a.D, o);
+            for (int i = 0; i < 8; ++i) o[i] = st.y * (fmaf(-h[v][i], m2, o[i] * w[i / 4][i & 3]) - m1);
+            store8<OF32, true>(a.dx.p, a.dx.ld, row, col, a.D, o);
         }
     }
+    if (!a.part_g && !a.part_b) return;
+    if (rows > 1) {
+        float4_t *const both = reinterpret_cast<float4_t *>(all);      // [sums][rows at once][halves of a chunk][chunks]
+        __syncthreads();
 #pragma unroll
-    for (int which = 0; which < 2; ++which) {
-        float *const part = which ? a.part_b : a.part_g;
-        if (!part) continue;
-        if (rows > 1) {
-            __syncthreads();
+        for (int v = 0; v < V; ++v) {
+            float4_t *const mine = both + slot * 2 * CHUNKS + t + v * TPR;
+            mine[0] = float4_t{sum_g[v][0], sum_g[v][1], sum_g[v][2], sum_g[v][3]};
+            mine[CHUNKS] = float4_t{sum_g[v][4], sum_g[v][5], sum_g[v][6], sum_g[v][7]};
+            mine[rows * 2 * CHUNKS] = float4_t{sum_b[v][0], sum_b[v][1], sum_b[v][2], sum_b[v][3]};
+            mine[(rows * 2 + 1) * CHUNKS] = float4_t{sum_b[v][4], sum_b[v][5], sum_b[v][6], sum_b[v][7]};
+        }
+        __syncthreads();
+        for (int u = threadIdx.x; u < 4 * CHUNKS; u += blockDim.x) {
+            const int which = u / (2 * CHUNKS), at = u % (2 * CHUNKS), col = at % CHUNKS * kChunk + at / CHUNKS * 4;
+            float *const part = which ? a.part_b : a.part_g;
+            if (!part || col >= a.D) continue;
+            const float4_t *const from = both + which * rows * 2 * CHUNKS + at;
+            float4_t s = from[0];
+            for (int r = 1; r < rows; ++r) s += from[r * 2 * CHUNKS];
+            float *const to = part + blockIdx.x * a.part_ld + col;
+            if (col + 4 <= a.D) {
+                *reinterpret_cast<f32x4_at4 *>(to) = s;
+            } else {
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const int col = (t + v * TPR) * kChunk;
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (col + i < a.D) all[slot * a.D + col + i] = which ? sum_b[v][i] : sum_g[v][i];
+                for (int i = 0; i < 3; ++i)
+                    if (col + i < a.D) to[i] = s[i];
             }
-            __syncthreads();
-            for (int c = threadIdx.x; c < a.D; c += blockDim.x) {
-                float s = all[c];
-                for (int r = 1; r < rows; ++r) s += all[r * a.D + c];
-                part[blockIdx.x * a.part_ld + c] = s;
-            }
-        } else {
+        }
+    } else {
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const int col = (t + v * TPR) * kChunk;
-                if (col < a.D) store8<true>(part, a.part_ld, blockIdx.x, col, a.D, which ? sum_b[v] : sum_g[v]);
-            }
+        for (int v = 0; v < V; ++v) {
+            const int col = (t + v * TPR) * kChunk;
+            if (col >= a.D) continue;
+            if (a.part_g) store8<true, true>(a.part_g, a.part_ld, blockIdx.x, col, a.D, sum_g[v]);
+            if (a.part_b) store8<true, true>(a.part_b, a.part_ld, blockIdx.x, col, a.D, sum_b[v]);
         }
     }
 }
@@ -289,8 +305,8 @@ __global__ __launch_bounds__(1024) void norm_bwd_long_kernel(const NormBwdArgs a
         float h[8], g[8], w[8];
         float s1 = 0.0f, s2 = 0.0f;
         for (int col = t * kChunk; col < a.D; col += TPR * kChunk) {
-            widen8(load8<KIND, true, false>(a.x, row, col, a.D), h);
-            widen8(load8<GKIND, true, false>(a.dy, row, col, a.D), g);
+            widen8(load8<KIND, false, false>(a.x, row, col, a.D), h);
+            widen8(load8<GKIND, false, false>(a.dy, row, col, a.D), g);
             param8(a.gamma, col, a.D, 1.0f, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -303,12 +319,12 @@ __global__ __launch_bounds__(1024) void norm_bwd_long_kernel(const NormBwdArgs a
         turn ^= 1;
         const float m1 = a.layer ? s1 * inv_d : 0.0f, m2 = s2 * inv_d;
         for (int col = t * kChunk; col < a.D; col += TPR * kChunk) {
-            widen8(load8<KIND, true, false>(a.x, row, col, a.D), h);
-            widen8(load8<GKIND, true, false>(a.dy, row, col, a.D), g);
+            widen8(load8<KIND, false, false>(a.x, row, col, a.D), h);
+            widen8(load8<GKIND, false, false>(a.dy, row, col, a.D), g);
             param8(a.gamma, col, a.D, 1.0f, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) g[i] = st.y * (fmaf(-((h[i] - st.x) * st.y), m2, g[i] * w[i]) - m1);
-            store8<OF32>(a.dx.p, a.dx.ld, row, col, a.D, g);
+            store8<OF32, false>(a.dx.p, a.dx.ld, row, col, a.D, g);
         }
     }
 }
@@ -324,50 +340,62 @@ __global__ __launch_bounds__(256) void norm_params_long_kernel(const NormBwdArgs
     for (int64_t row = blockIdx.y; row < a.N; row += gridDim.y) {
         const float2_t st = a.stats[row];
         float h[8], g[8];
-        widen8(load8<KIND, true, false>(a.x, row, col, a.D), h);
-        widen8(load8<GKIND, true, false>(a.dy, row, col, a.D), g);
+        widen8(load8<KIND, false, false>(a.x, row, col, a.D), h);
+        widen8(load8<GKIND, false, false>(a.dy, row, col, a.D), g);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             sum_g[i] = fmaf(g[i], (h[i] - st.x) * st.y, sum_g[i]);
             sum_b[i] += g[i];
         }
     }
-    if (a.part_g) store8<true>(a.part_g, a.part_ld, blockIdx.y, col, a.D, sum_g);
-    if (a.part_b) store8<true>(a.part_b, a.part_ld, blockIdx.y, col, a.D, sum_b);
+    if (a.part_g) store8<true, false>(a.part_g, a.part_ld, blockIdx.y, col, a.D, sum_g);
+    if (a.part_b) store8<true, false>(a.part_b, a.part_ld, blockIdx.y, col, a.D, sum_b);
 }
 
-// The partial sums of G <= 256 workgroups, in an order of their own: a workgroup takes 64 columns, each of its 16 waves every sixteenth partial
-// sum (all of a thread's loads are on their way at once), then the waves' sums in their order.
+// The partial sums of G <= 256 workgroups, in an order of their own: a workgroup takes 32 columns (a cache line), four neighbouring ones a thread; of
+// the 32 threads of a column each adds every 32nd partial sum (all of its loads are on their way at once), then eight lanes the threads' sums.
 constexpr int kMostPartials = 256;
-__global__ __launch_bounds__(1024) void norm_params_reduce_kernel(const float *part_g, const float *part_b, int64_t part_ld, int G, int D, float *dgamma, float *dbeta)
+__global__ __launch_bounds__(256) void norm_params_reduce_kernel(const float *part_g, const float *part_b, int64_t part_ld, int G, int D, float *dgamma, float *dbeta)
 {
-    __shared__ float red[16][64];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int c = blockIdx.x * 64 + lane;
+    __shared__ float4_t red[32][8];
+    const int quad = threadIdx.x & 7, first = threadIdx.x >> 3;
+    const int c = blockIdx.x * 32 + quad * 4;
     const float *const part = blockIdx.y ? part_b : part_g;
     float *const out = blockIdx.y ? dbeta : dgamma;
-    float s = 0.0f;
-    if (out && c < D) {
-        float v[kMostPartials / 16];
+    if (!out) return;
+    float4_t v[kMostPartials / 32];
 #pragma unroll
-        for (int i = 0; i < kMostPartials / 16; ++i) v[i] = w + 16 * i < G ? part[(w + 16 * i) * part_ld + c] : 0.0f;
+    for (int i = 0; i < kMostPartials / 32; ++i) {
+        v[i] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        const int g = first + 32 * i;
+        const float *const p = part + g * part_ld + c;
+        if (g < G && c + 4 <= D) {
+            v[i] = *reinterpret_cast<const f32x4_at4 *>(p);
+        } else if (g < G) {
 #pragma unroll
-        for (int i = 0; i < kMostPartials / 16; ++i) s += v[i];
+            for (int j = 0; j < 3; ++j)
+                if (c + j < D) v[i][j] = p[j];
+        }
     }
-    red[w][lane] = s;
+#pragma unroll
+    for (int i = 1; i < kMostPartials / 32; ++i) v[0] += v[i];
+    red[first][quad] = v[0];
     __syncthreads();
-    if (w == 0 && out && c < D) {
+    const int lane = threadIdx.x & 7, column = threadIdx.x >> 3;
+    float s = 0.0f;
 #pragma unroll
-        for (int i = 1; i < 16; ++i) s += red[i][lane];
-        out[c] = s;
-    }
+    for (int i = 0; i < 4; ++i) s += red[lane + 8 * i][column >> 2][column & 3];
+    s += u2f(dpp<DPP_QUAD_XOR1>(f2u(s)));
+    s += u2f(dpp<DPP_QUAD_XOR2>(f2u(s)));
+    s += u2f(dpp<DPP_ROW_HALF_MIRROR>(f2u(s)));
+    if (lane == 0 && blockIdx.x * 32 + column < D) out[blockIdx.x * 32 + column] = s;
 }
 
 constexpr int kMaxHeldRow = 16384;      // longest row that a workgroup's registers hold
 constexpr int kLongBlocks = 8192;       // most workgroups where a row is longer
 
-// threads that hold a row
 bool held(int64_t D) { return D >= kChunk && D <= kMaxHeldRow; }
+// threads that hold a row
 int threads_of_row(int64_t D) { return D <= 1024 ? 64 : D <= 4096 ? 256 : D <= 8192 ? 512 : 1024; }
 
 // rows that a workgroup of the backward kernel takes at once, as many as give every CU a workgroup and at most 1024 threads, and its workgroups: each leaves
@@ -405,7 +433,7 @@ template <int KIND, bool OF32> void run_norm_fwd(const NormFwdArgs &a, hipStream
 template <int KIND, bool GF32, bool OF32, int TPR, int V> void run_norm_bwd(const NormBwdArgs &a, unsigned blocks, hipStream_t st)
 {
     const unsigned rows = (unsigned)bwd_rows(a.N, a.D);
-    const size_t weights = (size_t)V * TPR * kChunk, sums = rows > 1 ? rows * (size_t)a.D : 0;
+    const size_t weights = (size_t)V * TPR * kChunk, sums = rows > 1 && (a.part_g || a.part_b) ? 2 * rows * weights : 0;
     const size_t lds = (weights > sums ? weights : sums) * sizeof(float);
     const double each = (GF32 ? 4 : 2) + (KIND == kF32 ? 4 : KIND == kBf16 ? 2 : 1) + (OF32 ? 4 : 2);
     if (streams((double)a.N * a.D * each)) norm_bwd_kernel<KIND, GF32, OF32, true, TPR, V><<<blocks, rows * TPR, lds, st>>>(a);
@@ -448,9 +476,9 @@ hipError_t launch_norm_bwd(const RowSrc &dy, const RowSrc &x, const float *stats
                            const RowDst &dx, float *dgamma, float *dbeta, void *ws, hipStream_t st)
 {
     const int64_t G = bwd_blocks(N, D);
-    const dim3 params((unsigned)((D + 63) / 64), dbeta ? 2 : 1);
+    const dim3 params((unsigned)((D + 31) / 32), dbeta ? 2 : 1);
     if (N == 0) {                        // sums over no rows
-        if (dgamma || dbeta) norm_params_reduce_kernel<<<params, 1024, 0, st>>>(nullptr, nullptr, 0, 0, (int)D, dgamma, dbeta);
+        if (dgamma || dbeta) norm_params_reduce_kernel<<<params, 256, 0, st>>>(nullptr, nullptr, 0, 0, (int)D, dgamma, dbeta);
         return hipGetLastError();
     }
     NormBwdArgs a{dy, x, reinterpret_cast<const float2_t *>(stats), gamma, N, (int)D, layer, dx, dgamma, dbeta, 0};
@@ -473,7 +501,7 @@ hipError_t launch_norm_bwd(const RowSrc &dy, const RowSrc &x, const float *stats
     else if (x.kind == kF32) by_dy(std::integral_constant<int, kF32>{});
     else by_dy(std::integral_constant<int, kBf16>{});
     if (G > 1 && (dgamma || dbeta))
-        norm_params_reduce_kernel<<<params, 1024, 0, st>>>(a.part_g, a.part_b, a.part_ld, (int)G, (int)D, dgamma, dbeta);
+        norm_params_reduce_kernel<<<params, 256, 0, st>>>(a.part_g, a.part_b, a.part_ld, (int)G, (int)D, dgamma, dbeta);
     return hipGetLastError();
 }
 

@@ -34,6 +34,21 @@ template <> struct Raw<kBf16> { u32x4 q; };
 template <> struct Raw<kF32> { float4_t lo, hi; };
 template <> struct Raw<kCkpt8> { u32x2 q; uint32_t e; };
 
+// Start of a row that all lanes of a wave share, in scalar registers: a lane's addresses are then this and a 32-bit offset, not a pair of registers
+// each (which the loops over rows would hold for every array).
+template <typename T> __device__ __forceinline__ T *shared_row(T *p)
+{
+    const uint64_t a = reinterpret_cast<uint64_t>(p);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)a), hi = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
+    return reinterpret_cast<T *>((uint64_t)hi << 32 | lo);
+}
+// SHARED: the lanes of a wave share the row, whose elements 32-bit numbers count
+template <bool SHARED, typename T, typename I> __device__ __forceinline__ T *row_at(T *p, int64_t row, int64_t ld, I at)
+{
+    if constexpr (SHARED) return shared_row(p + row * ld) + (uint32_t)at;
+    else return p + row * ld + at;
+}
+
 // STREAM: past the caches (see streams())
 template <typename T, bool STREAM> __device__ __forceinline__ T load_as(const void *p)
 {
@@ -64,49 +79,49 @@ __device__ __forceinline__ void move_down(float4_t &lo, float4_t &hi, uint32_t b
 
 // Elements [col, col + 8) of a row; those at or past n are zeros (n > col: at least one is there).  A chunk that the row's end cuts
 // is read as the row's last eight elements and moved down, where there are eight (one load, few registers); else
-// element by element.  SHORT: rows may have fewer than eight.  Whether rows have such a chunk is asked of the row length, the same for all lanes: a
+// element by element.  HELD: rows have at least eight elements, and the lanes of a wave share them.  Whether rows have such a chunk is asked of the row length, the same for all lanes: a
 // question to each lane would be passed with the lanes masked and wait for the load on the way (SwiGLU backward 129 us instead of 107).
-template <int KIND, bool SHORT, bool STREAM, typename I>
+template <int KIND, bool HELD, bool STREAM, typename I>
 __device__ __forceinline__ Raw<KIND> load8(const RowSrc &s, int64_t row, I col, I n)
 {
     Raw<KIND> r;
     const I at = col + kChunk > n ? n - kChunk : col;     // below zero in a row of fewer than eight
     const uint32_t by = (uint32_t)(col - at);
     if constexpr (KIND == kBf16) {
-        const uint16_t *const p = static_cast<const uint16_t *>(s.p) + row * s.ld;
-        if (!SHORT || n >= kChunk) {
-            r.q = load_as<bf16x8_at2, STREAM>(p + at);
+        const uint16_t *const p = static_cast<const uint16_t *>(s.p);
+        if (HELD || n >= kChunk) {
+            r.q = load_as<bf16x8_at2, STREAM>(row_at<HELD>(p, row, s.ld, at));
             if (n % kChunk != 0) r.q = move_down(r.q, by);
         } else {
             r.q = u32x4{0, 0, 0, 0};
 #pragma unroll
             for (int i = 0; i < kChunk - 1; ++i)
-                if (i < n) r.q[i / 2] |= (uint32_t)p[i] << (16 * (i & 1));
+                if (i < n) r.q[i / 2] |= (uint32_t)p[row * s.ld + i] << (16 * (i & 1));
         }
     } else if constexpr (KIND == kF32) {
-        const float *const p = static_cast<const float *>(s.p) + row * s.ld;
-        if (!SHORT || n >= kChunk) {
-            r.lo = load_as<f32x4_at4, STREAM>(p + at);
-            r.hi = load_as<f32x4_at4, STREAM>(p + at + 4);
+        const float *const p = static_cast<const float *>(s.p);
+        if (HELD || n >= kChunk) {
+            r.lo = load_as<f32x4_at4, STREAM>(row_at<HELD>(p, row, s.ld, at));
+            r.hi = load_as<f32x4_at4, STREAM>(row_at<HELD>(p, row, s.ld, at) + 4);
             if (n % kChunk != 0) move_down(r.lo, r.hi, by);
         } else {
             r.lo = r.hi = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int i = 0; i < kChunk - 1; ++i)
-                if (i < n) (i < 4 ? r.lo : r.hi)[i & 3] = p[i];
+                if (i < n) (i < 4 ? r.lo : r.hi)[i & 3] = p[row * s.ld + i];
         }
     } else {
-        const uint8_t *const p = static_cast<const uint8_t *>(s.p) + row * s.ld;
-        if (!SHORT || n >= kChunk) {
-            r.q = load_as<code8_at1, STREAM>(p + at);
+        const uint8_t *const p = static_cast<const uint8_t *>(s.p);
+        if (HELD || n >= kChunk) {
+            r.q = load_as<code8_at1, STREAM>(row_at<HELD>(p, row, s.ld, at));
             if (n % kChunk != 0) r.q = move_down(r.q, by);
         } else {
             r.q = u32x2{0, 0};
 #pragma unroll
             for (int i = 0; i < kChunk - 1; ++i)
-                if (i < n) r.q[i / 4] |= (uint32_t)p[i] << (8 * (i & 3));
+                if (i < n) r.q[i / 4] |= (uint32_t)p[row * s.ld + i] << (8 * (i & 3));
         }
-        r.e = s.exps[row * s.groups + col / kCkptGroup];
+        r.e = *row_at<HELD>(s.exps, row, s.groups, col / kCkptGroup);
     }
     return r;
 }
@@ -153,11 +168,11 @@ __device__ __forceinline__ void widen8(const Raw<kCkpt8> &r, float (&v)[8])
 
 // ---- stores -----------------------------------------------------------------------------------
 
-template <bool F32, typename I>
+template <bool F32, bool SHARED, typename I>
 __device__ __forceinline__ void store8(void *out, int64_t ld, int64_t row, I col, I n, const float (&v)[8])
 {
     if constexpr (F32) {
-        float *const p = static_cast<float *>(out) + row * ld + col;
+        float *const p = row_at<SHARED>(static_cast<float *>(out), row, ld, col);
         if (col + kChunk <= n) {
             *reinterpret_cast<f32x4_at4 *>(p) = f32x4_at4{v[0], v[1], v[2], v[3]};
             *reinterpret_cast<f32x4_at4 *>(p + 4) = f32x4_at4{v[4], v[5], v[6], v[7]};
@@ -167,7 +182,7 @@ __device__ __forceinline__ void store8(void *out, int64_t ld, int64_t row, I col
                 if (col + i < n) p[i] = v[i];
         }
     } else {
-        uint16_t *const p = static_cast<uint16_t *>(out) + row * ld + col;
+        uint16_t *const p = row_at<SHARED>(static_cast<uint16_t *>(out), row, ld, col);
         const u32x4 q = {bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
         if (col + kChunk <= n) {
             *reinterpret_cast<bf16x8_at2 *>(p) = q;
@@ -185,7 +200,7 @@ __device__ __forceinline__ void store8(void *out, int64_t ld, int64_t row, I col
 // row's end with zeros).  a = max |v| over the finite values, e the least integer with a <= 1.75 * 2^(8 + e) = 448 * 2^e within
 // [-126, 120]: both 2^e and 2^-e are then ordinary binary32 numbers, the product v * 2^-e is exact (rounded below 2^-126, far
 // under half of the smallest code) and the conversion's rounding is the only one.  Values that are not finite become the NaN 0x7F.
-template <typename I>
+template <bool SHARED, typename I>
 __device__ __forceinline__ void ckpt_store8(const CkptOut &o, int64_t row, I col, I n, const float (&v)[8])
 {
     uint32_t a = 0;
@@ -219,7 +234,7 @@ __device__ __forceinline__ void ckpt_store8(const CkptOut &o, int64_t row, I col
             if ((f2u(v[i]) & 0x7FFFFFFFu) >= 0x7F800000u) q[i / 4] = (q[i / 4] & ~(0xFFu << (8 * (i & 3)))) | (0x7Fu << (8 * (i & 3)));
     }
     if (col >= n) return;
-    uint8_t *p = o.codes + row * n + col;
+    uint8_t *const p = row_at<SHARED>(o.codes, row, n, col);
     if (col + kChunk <= n) {
         *reinterpret_cast<code8_at1 *>(p) = q;
     } else {
@@ -227,7 +242,7 @@ __device__ __forceinline__ void ckpt_store8(const CkptOut &o, int64_t row, I col
         for (int i = 0; i < kChunk - 1; ++i)
             if (col + i < n) p[i] = (uint8_t)(q[i / 4] >> (8 * (i & 3)));
     }
-    if (col % kCkptGroup == 0) o.exps[row * o.groups + col / kCkptGroup] = (uint8_t)(e + 127);
+    if (col % kCkptGroup == 0) *row_at<SHARED>(o.exps, row, o.groups, col / kCkptGroup) = (uint8_t)(e + 127);
 }
 
 // ---- sums over the threads of a row -----------------------------------------------------------
