@@ -40,18 +40,32 @@ struct CopyArgs {
     CkptOut ckpt;
 };
 
-struct Sigmoid { float pos, neg; };      // s(z) and s(-z)
-__device__ __forceinline__ Sigmoid sigmoid(float z)
+// s(z) and s(-z) with w = -z log2(e); the exponential never overflows, and the two are exact to a few units in the last place however far z is out
+struct Sigmoid { float pos, neg; };
+__device__ __forceinline__ Sigmoid sigmoid(float w)
 {
-    const float e = __expf(-fabsf(z));   // never overflows
-    const float r = __builtin_amdgcn_rcpf(1.0f + e), q = e * r;      // within one unit in the last place
-    return z >= 0.0f ? Sigmoid{r, q} : Sigmoid{q, r};
+    const float e = __builtin_amdgcn_exp2f(-fabsf(w));
+    const float r = __builtin_amdgcn_rcpf(1.0f + e), q = e * r;      // reciprocal: within one unit in the last place
+    return w <= 0.0f ? Sigmoid{r, q} : Sigmoid{q, r};
 }
+// s(z) alone: an exponential that overflows gives 0
+__device__ __forceinline__ float sigmoid_pos(float w) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(w)); }
 
-constexpr float kGeluC = 1.5957691216057308f, kGeluA = 0.044715f;
-// beyond |x| = 16 both s(z) and x s(z) s(-z) z'(x) have reached their limits in binary32, and x^3 overflows far out; a NaN stays
-__device__ __forceinline__ float gelu_in(float x) { return x > 16.0f ? 16.0f : x < -16.0f ? -16.0f : x; }
-__device__ __forceinline__ float gelu_z(float c) { return kGeluC * fmaf(kGeluA * c * c, c, c); }
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr double kGeluC = 1.5957691216057308, kGeluA = 0.044715;     // z(x) = C (x + A x^3)
+// -z log2(e) = x (k0 + k1 x^2)
+__device__ __forceinline__ float gelu_w(float x)
+{
+    return x * fmaf(x * x, (float)(-kGeluC * kGeluA * 1.4426950408889634), (float)(-kGeluC * 1.4426950408889634));
+}
+__device__ __forceinline__ float gelu(float x) { return x * sigmoid_pos(gelu_w(x)); }
+// z and its slope are taken at most at |x| = 16, beyond which s(z) s(-z) is zero in binary32 (x^2 times it would overflow far out)
+__device__ __forceinline__ float gelu_slope(float x)
+{
+    const float c = __builtin_amdgcn_fmed3f(x, -16.0f, 16.0f);
+    const Sigmoid s = sigmoid(gelu_w(c));
+    return fmaf(x * (s.pos * s.neg), fmaf(c * c, (float)(3.0 * kGeluC * kGeluA), (float)kGeluC), s.pos);
+}
 
 // For every chunk of the launch use(row, column, load(row, column)), R rows of a thread loaded before the first is used.  The lanes of a
 // group come together, those past the end of a row with col >= cols.
@@ -108,11 +122,11 @@ __global__ __launch_bounds__(kThreads) void act_fwd_kernel(const ActArgs a)
                 ckpt_store8<false>(a.ckpt, 2 * row + 1, col, F, u);
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) o[i] = x[i] * sigmoid(x[i]).pos * u[i];
+            for (int i = 0; i < 8; ++i) o[i] = x[i] * sigmoid_pos(-kLog2e * x[i]) * u[i];
         } else {
             if (a.ckpt.codes) ckpt_store8<false>(a.ckpt, row, col, F, x);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) o[i] = x[i] * sigmoid(gelu_z(gelu_in(x[i]))).pos;
+            for (int i = 0; i < 8; ++i) o[i] = gelu(x[i]);
         }
         if (col < F) store8<OF32, false>(a.out.p, a.out.ld, row, col, F, o);
     });
@@ -149,7 +163,7 @@ __global__ __launch_bounds__(kThreads) void act_bwd_kernel(const ActArgs a)
             widen8(in.b, u);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const Sigmoid s = sigmoid(x[i]);
+                const Sigmoid s = sigmoid(-kLog2e * x[i]);
                 const float du = da[i] * x[i] * s.pos;
                 x[i] = da[i] * u[i] * s.pos * fmaf(x[i], s.neg, 1.0f);
                 u[i] = du;
@@ -158,12 +172,7 @@ __global__ __launch_bounds__(kThreads) void act_bwd_kernel(const ActArgs a)
             store8<OF32, false>(static_cast<char *>(a.out.p) + (int64_t)F * (OF32 ? 4 : 2), a.out.ld, row, col, F, u);
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float c = gelu_in(x[i]);
-                const Sigmoid s = sigmoid(gelu_z(c));
-                const float slope = kGeluC * fmaf(3.0f * kGeluA * c, c, 1.0f);
-                x[i] = da[i] * fmaf(c * s.pos * s.neg, slope, s.pos);
-            }
+            for (int i = 0; i < 8; ++i) x[i] = da[i] * gelu_slope(x[i]);
             store8<OF32, false>(a.out.p, a.out.ld, row, col, F, x);
         }
     });
