@@ -568,22 +568,26 @@ def alloc_stats(N: int, device="cuda") -> torch.Tensor:
     return torch.empty((N, 2), dtype=torch.float32, device=device)
 
 
+_KINDS = {torch.bfloat16: SRC_BF16, torch.float32: SRC_F32}
+
+
 def _rows(t: torch.Tensor, what: str):
-    """(kind, row stride) of a bf16 or float32 matrix whose rows are contiguous; the rows may be any distance apart."""
-    assert t.dim() == 2 and t.is_cuda, what + ": 2-D, on the GPU"
-    assert t.dtype == torch.bfloat16 or t.dtype == torch.float32, what + ": bf16 or float32"
-    n = t.shape[1]
+    """(kind, row stride, rows, elements of a row) of a bf16 or float32 matrix whose rows are contiguous; the rows may be any distance apart."""
+    kind = _KINDS.get(t.dtype)
+    shape = t.shape
+    assert kind is not None and len(shape) == 2 and t.is_cuda, what + ": bf16 or float32, 2-D, on the GPU"
+    rows, n = shape
     s0, s1 = t.stride()
     assert s1 == 1 or n <= 1, what + ": rows of contiguous elements"
-    return (SRC_BF16 if t.dtype == torch.bfloat16 else SRC_F32), (s0 if t.shape[0] > 1 else n)
+    return kind, s0 if rows > 1 else n, rows, n
 
 
-def _out_rows(t: Optional[torch.Tensor], shape, out_dtype: int, device, what: str):
+def _out_rows(t: Optional[torch.Tensor], rows: int, n: int, out_dtype: int, device, what: str):
     """The output matrix, allocated where none is given, and its row stride."""
     if t is None:
-        return _out_tensor(*shape, out_dtype, device), shape[1]
-    kind, ld = _rows(t, what)
-    assert tuple(t.shape) == tuple(shape) and kind == (SRC_BF16 if out_dtype == OUT_BF16 else SRC_F32), what
+        return torch.empty((rows, n), dtype=torch.bfloat16 if out_dtype == OUT_BF16 else torch.float32, device=device), n
+    kind, ld, r, c = _rows(t, what)
+    assert r == rows and c == n and kind == (SRC_BF16 if out_dtype == OUT_BF16 else SRC_F32), what
     return t, ld
 
 
@@ -607,9 +611,8 @@ def norm_fwd(X: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Option
              ckpt: Optional[Ckpt8] = None) -> torch.Tensor:
     """nvfp4_norm_fwd: layer norm (NORM_LAYER) or RMS norm (NORM_RMS) of every row of X.  For training pass stats (alloc_stats) and, to keep
     the input in 8 bits, ckpt (alloc_ckpt8); both are filled."""
-    kind, ldx = _rows(X, "X")
-    N, D = X.shape
-    Y, ldy = _out_rows(Y, (N, D), out_dtype, X.device, "Y")
+    kind, ldx, N, D = _rows(X, "X")
+    Y, ldy = _out_rows(Y, N, D, out_dtype, X.device, "Y")
     cs = None
     if ckpt is not None:
         _check_ckpt(ckpt, N, D)
@@ -626,18 +629,17 @@ def norm_bwd(dY: torch.Tensor, X, stats: torch.Tensor, gamma: Optional[torch.Ten
              dbeta: Optional[torch.Tensor] = None, params: bool = True, ws: Optional[torch.Tensor] = None):
     """nvfp4_norm_bwd: (dX, dgamma, dbeta); X is the forward call's input or its Ckpt8.  params=False: dX alone; RMS norm has no dbeta
     unless one is passed."""
-    dkind, lddy = _rows(dY, "dY")
-    N, D = dY.shape
+    dkind, lddy, N, D = _rows(dY, "dY")
     dev = dY.device
     if isinstance(X, Ckpt8):
         _check_ckpt(X, N, D)
         kind, ldx, src = SRC_CKPT8, 0, C.byref(X.c_struct())
     else:
-        kind, ldx = _rows(X, "X")
-        assert X.shape == dY.shape, "X: the shape of dY"
+        kind, ldx, *shape = _rows(X, "X")
+        assert shape == [N, D], "X: the shape of dY"
         src = _ptr(X)
     _check_stats(stats, N)
-    dX, lddx = _out_rows(dX, (N, D), out_dtype, dev, "dX")
+    dX, lddx = _out_rows(dX, N, D, out_dtype, dev, "dX")
     if params:
         dgamma = torch.empty(D, dtype=torch.float32, device=dev) if dgamma is None else dgamma
         if dbeta is None and norm == NORM_LAYER:
@@ -655,12 +657,11 @@ def norm_bwd(dY: torch.Tensor, X, stats: torch.Tensor, gamma: Optional[torch.Ten
 def act_fwd(H: torch.Tensor, act: int = ACT_SWIGLU, out_dtype: int = OUT_BF16, *, A: Optional[torch.Tensor] = None,
             ckpt: Optional[Ckpt8] = None) -> torch.Tensor:
     """nvfp4_act_fwd: SwiGLU of H [N, 2F] (gates, then up values) or GELU (tanh form) of H [N, F]; ckpt (alloc_act_ckpt8) receives H in 8 bits."""
-    kind, ldh = _rows(H, "H")
-    N, F = H.shape
+    kind, ldh, N, F = _rows(H, "H")
     if act == ACT_SWIGLU:
         assert F % 2 == 0, "H: gates and up values"
         F //= 2
-    A, lda = _out_rows(A, (N, F), out_dtype, H.device, "A")
+    A, lda = _out_rows(A, N, F, out_dtype, H.device, "A")
     cs = None
     if ckpt is not None:
         _check_ckpt(ckpt, 2 * N if act == ACT_SWIGLU else N, F)
@@ -671,25 +672,23 @@ def act_fwd(H: torch.Tensor, act: int = ACT_SWIGLU, out_dtype: int = OUT_BF16, *
 
 def act_bwd(dA: torch.Tensor, H, act: int = ACT_SWIGLU, out_dtype: int = OUT_BF16, *, dH: Optional[torch.Tensor] = None) -> torch.Tensor:
     """nvfp4_act_bwd: dH from dA and the forward call's input or its Ckpt8."""
-    dkind, ldda = _rows(dA, "dA")
-    N, F = dA.shape
+    dkind, ldda, N, F = _rows(dA, "dA")
     parts = 2 if act == ACT_SWIGLU else 1
     if isinstance(H, Ckpt8):
         _check_ckpt(H, parts * N, F)
         kind, ldh, src = SRC_CKPT8, 0, C.byref(H.c_struct())
     else:
-        kind, ldh = _rows(H, "H")
-        assert tuple(H.shape) == (N, parts * F), "H"
+        kind, ldh, *shape = _rows(H, "H")
+        assert shape == [N, parts * F], "H"
         src = _ptr(H)
-    dH, lddh = _out_rows(dH, (N, parts * F), out_dtype, dA.device, "dH")
+    dH, lddh = _out_rows(dH, N, parts * F, out_dtype, dA.device, "dH")
     _check(lib().nvfp4_act_bwd(_ptr(dA), dkind, ldda, src, kind, ldh, N, F, act, _ptr(dH), out_dtype, lddh, _stream()), "nvfp4_act_bwd")
     return dH
 
 
 def ckpt8_save(X: torch.Tensor, out: Optional[Ckpt8] = None) -> Ckpt8:
     """nvfp4_ckpt8_save: an activation [N, D] in 8 bits."""
-    kind, ldx = _rows(X, "X")
-    N, D = X.shape
+    kind, ldx, N, D = _rows(X, "X")
     out = alloc_ckpt8(N, D, X.device) if out is None else out
     _check_ckpt(out, N, D)
     _check(lib().nvfp4_ckpt8_save(_ptr(X), kind, ldx, N, D, C.byref(out.c_struct()), _stream()), "nvfp4_ckpt8_save")
@@ -699,16 +698,15 @@ def ckpt8_save(X: torch.Tensor, out: Optional[Ckpt8] = None) -> Ckpt8:
 def ckpt8_load(src: Ckpt8, out_dtype: int = OUT_BF16, *, Y: Optional[torch.Tensor] = None) -> torch.Tensor:
     """nvfp4_ckpt8_load: the activation that a checkpoint holds."""
     _check_ckpt(src, src.rows, src.K)
-    Y, ldy = _out_rows(Y, (src.rows, src.K), out_dtype, src.codes.device, "Y")
+    Y, ldy = _out_rows(Y, src.rows, src.K, out_dtype, src.codes.device, "Y")
     _check(lib().nvfp4_ckpt8_load(C.byref(src.c_struct()), _ptr(Y), out_dtype, ldy, _stream()), "nvfp4_ckpt8_load")
     return Y
 
 
 def gemv(X: torch.Tensor, W: NVFP4Tensor, out_dtype: int = OUT_BF16, *, Y: Optional[torch.Tensor] = None) -> torch.Tensor:
     """nvfp4_gemv: Y = X W^T for the bf16 activations of a few tokens on packed weights (linear_fwd's Wq)."""
-    kind, ldx = _rows(X, "X")
-    M, K = X.shape
+    kind, ldx, M, K = _rows(X, "X")
     assert kind == SRC_BF16 and K == W.K, "X: bf16 [M, W.K]"
-    Y, ldy = _out_rows(Y, (M, W.rows), out_dtype, X.device, "Y")
+    Y, ldy = _out_rows(Y, M, W.rows, out_dtype, X.device, "Y")
     _check(lib().nvfp4_gemv(_ptr(X), ldx, M, C.byref(W.c_struct()), _ptr(Y), out_dtype, ldy, _stream()), "nvfp4_gemv")
     return Y
