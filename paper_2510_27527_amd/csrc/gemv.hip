@@ -352,18 +352,20 @@ template <int NT, int RT> void run_gemv(const GemvArgs &a, int outer, int most_w
     else gemv_kernel<NT, RT, false><<<grid, waves * 64, lds, st>>>(a);
 }
 
-// Tiles of 16 rows: where they leave a CU one workgroup (85 KB of LDS with eight waves), the reduction is split eight ways; with more, four ways
-// (three workgroups share a CU); from four tiles a CU on two of them share the activations.  us, M x C x K:
-//                                8 waves   4 waves   4 waves, 32 rows
-//   16 x 1024 x 8192               8.9      11.0         14.6
-//   16 x 4096 x 4096, outer        7.5       7.9         10.1
-//   16 x 8192 x 8192              20.0      17.4         19.0
-//   16 x 16384 x 16384            62.9      56.2         42.7
+// Tiles of 16 rows.  Up to one a CU: a workgroup each, whose eight waves split the reduction (85 KB of LDS).  From two a CU on a workgroup takes two,
+// which share the activations; where that is more than one workgroup a CU, and between one and two tiles a CU, four waves leave room for
+// several (more than one round of large workgroups is what costs most).  us by rows x waves of a workgroup, M x C x K:
+//                                16 x 8   16 x 4   32 x 8   32 x 4
+//   16 x 4096 x 4096, outer        7.3      7.8      8.9     10.1
+//   5 x 5003 x 2064                9.9      7.1      7.5      8.6
+//   16 x 8192 x 8192              19.6     17.4     16.1     18.8
+//   32 x 8192 x 8192              28.0     27.0     22.5     25.2      (32 rows: six waves, 127 KB of LDS, for eight)
+//   16 x 16384 x 16384            62.7     56.5     47.6     42.9
 template <int NT> void run_gemv(const GemvArgs &a, int outer, hipStream_t st)
 {
     const int64_t tiles = (a.C + 15) / 16;
-    if (tiles >= 1024) run_gemv<NT, 2>(a, outer, 4, st);
-    else run_gemv<NT, 1>(a, outer, tiles <= 256 ? 8 : 4, st);
+    if (tiles < 512) run_gemv<NT, 1>(a, outer, tiles <= 256 ? 8 : 4, st);
+    else run_gemv<NT, 2>(a, outer, tiles > 512 ? 4 : NT == 1 ? 8 : 6, st);
 }
 
 template <int M, int LR, int R> void run_few(const GemvArgs &a, int outer, hipStream_t st)
