@@ -298,8 +298,9 @@ int nvfp4_osci_suppress_sparse(float *W, int64_t C, int64_t D, const uint32_t *i
  * for bf16, 4 for binary32).  Sources are NVFP4_SRC_BF16, NVFP4_SRC_F32 or, where a checkpoint is taken, NVFP4_SRC_CKPT8: then
  * the pointer is a HOST pointer to an nvfp4_ckpt8 and its ld is not read.  Outputs are NVFP4_OUT_BF16 or NVFP4_OUT_F32, independently of the
  * sources.  An output must not overlap an input.  Sums and statistics are binary32, each output is rounded once.
- * Arrays have at most 2^33 elements, 2^30 in a row, and span at most 2^46 (SHAPE).  A NaN or infinity stays in the row (norms), the element or the token that it is in;
- * in the norm's backward pass it reaches dgamma and dbeta in its columns.
+ * Arrays have at most 2^33 elements, 2^30 in a row, and span at most 2^46 (SHAPE).  A NaN or infinity stays in the row (norms), the
+ * element or the token that it is in; in the norm's backward pass dgamma and dbeta take it up: from dY in its column, from a row of X (whose statistics
+ * it reaches) in every column.
  */
 enum { NVFP4_SRC_F32 = 2, NVFP4_SRC_CKPT8 = 3 };
 enum { NVFP4_NORM_LAYER = 0, NVFP4_NORM_RMS = 1 };
