@@ -113,10 +113,10 @@ __global__ __launch_bounds__(kThreads) void act_fwd_kernel(const ActArgs a)
     };
     for_chunks<kRows>(a.n, load, [&](int64_t row, int col, const Pair<KIND> &in) {
         float x[8], o[8];
-        widen8(in.a, x);
+        widen8(in.a, col, F, x);
         if constexpr (ACT == kSwiglu) {
             float u[8];
-            widen8(in.b, u);
+            widen8(in.b, col, F, u);
             if (a.ckpt.codes) {
                 ckpt_store8<false>(a.ckpt, 2 * row, col, F, x);
                 ckpt_store8<false>(a.ckpt, 2 * row + 1, col, F, u);
@@ -156,11 +156,11 @@ __global__ __launch_bounds__(kThreads) void act_bwd_kernel(const ActArgs a)
     for_chunks<ACT == kSwiglu ? kRowsSwigluBwd : kRows>(a.n, load, [&](int64_t row, int col, const In &in) {
         if (col >= F) return;
         float x[8], da[8];
-        widen8(in.da, da);
-        widen8(in.a, x);
+        widen8(in.da, col, F, da);
+        widen8(in.a, col, F, x);
         if constexpr (ACT == kSwiglu) {
             float u[8];
-            widen8(in.b, u);
+            widen8(in.b, col, F, u);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const Sigmoid s = sigmoid(-kLog2e * x[i]);
@@ -184,7 +184,7 @@ __global__ __launch_bounds__(kThreads) void ckpt8_save_kernel(const CopyArgs a)
     for_chunks<kRows>(a.n, [&](int64_t row, int col) { return load8_or_0<KIND, STREAM>(a.src, row, col, a.n.cols, 0); },
                       [&](int64_t row, int col, const Raw<KIND> &in) {
         float x[8];
-        widen8(in, x);
+        widen8(in, col, a.n.cols, x);
         ckpt_store8<false>(a.ckpt, row, col, a.n.cols, x);
     });
 }
@@ -196,7 +196,7 @@ __global__ __launch_bounds__(kThreads) void ckpt8_load_kernel(const CopyArgs a)
                       [&](int64_t row, int col, const Raw<kCkpt8> &in) {
         if (col >= a.n.cols) return;
         float x[8];
-        widen8(in, x);
+        widen8(in, col, a.n.cols, x);
         store8<OF32, false>(a.out.p, a.out.ld, row, col, a.n.cols, x);
     });
 }

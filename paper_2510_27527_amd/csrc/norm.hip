@@ -80,7 +80,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_fwd_kernel(const N
     for (; row < a.N; row += step) {       // one row a workgroup where TPR > 64: all of its threads are here
         float x[V][8];
 #pragma unroll
-        for (int v = 0; v < V; ++v) widen8(next[v], x[v]);
+        for (int v = 0; v < V; ++v) widen8(next[v], (t + v * TPR) * kChunk, a.D, x[v]);
         if (row + step < a.N) load(row + step);
         float mean = 0.0f, none = 0.0f;
         if (a.layer) {
@@ -132,7 +132,7 @@ __global__ __launch_bounds__(1024) void norm_fwd_long_kernel(const NormFwdArgs a
         if (a.layer) {
             float sum = 0.0f;
             for (int col = t * kChunk; col < a.D; col += TPR * kChunk) {
-                widen8(load8<KIND, false, false>(a.x, row, col, a.D), x);
+                widen8(load8<KIND, false, false>(a.x, row, col, a.D), col, a.D, x);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum += x[i];
             }
@@ -140,7 +140,7 @@ __global__ __launch_bounds__(1024) void norm_fwd_long_kernel(const NormFwdArgs a
             mean = sum * inv_d;
         }
         for (int col = t * kChunk; col < a.D; col += TPR * kChunk) {
-            widen8(load8<KIND, false, false>(a.x, row, col, a.D), x);
+            widen8(load8<KIND, false, false>(a.x, row, col, a.D), col, a.D, x);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float d = x[i] - mean;
@@ -153,7 +153,7 @@ __global__ __launch_bounds__(1024) void norm_fwd_long_kernel(const NormFwdArgs a
         for (int base = 0; base < a.D; base += TPR * kChunk) {     // all lanes of a group stay for the checkpoint
             const int col = base + t * kChunk;
             const Raw<KIND> raw = col < a.D ? load8<KIND, false, false>(a.x, row, col, a.D) : zero8<KIND>();
-            widen8(raw, x);
+            widen8(raw, col, a.D, x);
             if (a.ckpt.codes) ckpt_store8<false>(a.ckpt, row, col, a.D, x);
             if (col >= a.D) continue;
             float g[8], b[8];
@@ -217,15 +217,15 @@ __global__ __launch_bounds__(1024) void norm_bwd_kernel(const NormBwdArgs a)
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            widen8(next_x[v], h[v]);
-            dy[v] = next_g[v];
+            widen8(next_x[v], (t + v * TPR) * kChunk, a.D, h[v]);
+            dy[v] = settle8(next_g[v], (t + v * TPR) * kChunk, a.D);
         }
         load(row + step);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const float4_t w[2] = {weight[t + v * TPR], weight[CHUNKS + t + v * TPR]};
             float g[8];
-            widen8(dy[v], g);
+            widen(dy[v], g);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 h[v][i] = (h[v][i] - st.x) * st.y;
@@ -245,7 +245,7 @@ __global__ __launch_bounds__(1024) void norm_bwd_kernel(const NormBwdArgs a)
             if (col >= a.D || row >= a.N) continue;
             const float4_t w[2] = {weight[t + v * TPR], weight[CHUNKS + t + v * TPR]};
             float o[8];
-            widen8(dy[v], o);
+            widen(dy[v], o);
 #pragma unroll
             for (int i = 0; i < 8; ++i) o[i] = st.y * (fmaf(-h[v][i], m2, o[i] * w[i / 4][i & 3]) - m1);
             store8<OF32, true>(a.dx.p, a.dx.ld, row, col, a.D, o);
@@ -305,8 +305,8 @@ __global__ __launch_bounds__(1024) void norm_bwd_long_kernel(const NormBwdArgs a
         float h[8], g[8], w[8];
         float s1 = 0.0f, s2 = 0.0f;
         for (int col = t * kChunk; col < a.D; col += TPR * kChunk) {
-            widen8(load8<KIND, false, false>(a.x, row, col, a.D), h);
-            widen8(load8<GKIND, false, false>(a.dy, row, col, a.D), g);
+            widen8(load8<KIND, false, false>(a.x, row, col, a.D), col, a.D, h);
+            widen8(load8<GKIND, false, false>(a.dy, row, col, a.D), col, a.D, g);
             param8(a.gamma, col, a.D, 1.0f, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -319,8 +319,8 @@ __global__ __launch_bounds__(1024) void norm_bwd_long_kernel(const NormBwdArgs a
         turn ^= 1;
         const float m1 = a.layer ? s1 * inv_d : 0.0f, m2 = s2 * inv_d;
         for (int col = t * kChunk; col < a.D; col += TPR * kChunk) {
-            widen8(load8<KIND, false, false>(a.x, row, col, a.D), h);
-            widen8(load8<GKIND, false, false>(a.dy, row, col, a.D), g);
+            widen8(load8<KIND, false, false>(a.x, row, col, a.D), col, a.D, h);
+            widen8(load8<GKIND, false, false>(a.dy, row, col, a.D), col, a.D, g);
             param8(a.gamma, col, a.D, 1.0f, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) g[i] = st.y * (fmaf(-((h[i] - st.x) * st.y), m2, g[i] * w[i]) - m1);
@@ -340,8 +340,8 @@ __global__ __launch_bounds__(256) void norm_params_long_kernel(const NormBwdArgs
     for (int64_t row = blockIdx.y; row < a.N; row += gridDim.y) {
         const float2_t st = a.stats[row];
         float h[8], g[8];
-        widen8(load8<KIND, false, false>(a.x, row, col, a.D), h);
-        widen8(load8<GKIND, false, false>(a.dy, row, col, a.D), g);
+        widen8(load8<KIND, false, false>(a.x, row, col, a.D), col, a.D, h);
+        widen8(load8<GKIND, false, false>(a.dy, row, col, a.D), col, a.D, g);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             sum_g[i] = fmaf(g[i], (h[i] - st.x) * st.y, sum_g[i]);

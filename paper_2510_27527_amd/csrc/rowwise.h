@@ -56,6 +56,59 @@ template <typename T, bool STREAM> __device__ __forceinline__ T load_as(const vo
     else return *static_cast<const T *>(p);
 }
 
+// Elements [col, col + 8) of a row (n > col: at least one is there), for widen8 of the same place.  A chunk that the row's end cuts is read as
+// the row's last eight elements, where there are eight (one load, few registers), else element by element.
+// HELD: rows have at least eight elements, and the lanes of a wave share them.
+template <int KIND, bool HELD, bool STREAM, typename I>
+__device__ __forceinline__ Raw<KIND> load8(const RowSrc &s, int64_t row, I col, I n)
+{
+    Raw<KIND> r;
+    const I at = col + kChunk > n ? n - kChunk : col;     // below zero in a row of fewer than eight
+    if constexpr (KIND == kBf16) {
+        const uint16_t *const p = static_cast<const uint16_t *>(s.p);
+        if (HELD || n >= kChunk) {
+            r.q = load_as<bf16x8_at2, STREAM>(row_at<HELD>(p, row, s.ld, at));
+        } else {
+            r.q = u32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < kChunk - 1; ++i)
+                if (i < n) r.q[i / 2] |= (uint32_t)p[row * s.ld + i] << (16 * (i & 1));
+        }
+    } else if constexpr (KIND == kF32) {
+        const float *const p = static_cast<const float *>(s.p);
+        if (HELD || n >= kChunk) {
+            r.lo = load_as<f32x4_at4, STREAM>(row_at<HELD>(p, row, s.ld, at));
+            r.hi = load_as<f32x4_at4, STREAM>(row_at<HELD>(p, row, s.ld, at) + 4);
+        } else {
+            r.lo = r.hi = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int i = 0; i < kChunk - 1; ++i)
+                if (i < n) (i < 4 ? r.lo : r.hi)[i & 3] = p[row * s.ld + i];
+        }
+    } else {
+        const uint8_t *const p = static_cast<const uint8_t *>(s.p);
+        if (HELD || n >= kChunk) {
+            r.q = load_as<code8_at1, STREAM>(row_at<HELD>(p, row, s.ld, at));
+        } else {
+            r.q = u32x2{0, 0};
+#pragma unroll
+            for (int i = 0; i < kChunk - 1; ++i)
+                if (i < n) r.q[i / 4] |= (uint32_t)p[row * s.ld + i] << (8 * (i & 3));
+        }
+        r.e = *row_at<HELD>(s.exps, row, s.groups, col / kCkptGroup);
+    }
+    return r;
+}
+
+template <int KIND> __device__ __forceinline__ Raw<KIND> zero8()
+{
+    Raw<KIND> r;
+    if constexpr (KIND == kBf16) r.q = u32x4{0, 0, 0, 0};
+    else if constexpr (KIND == kF32) r.lo = r.hi = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    else { r.q = u32x2{0, 0}; r.e = 127; }
+    return r;
+}
+
 // v moved down by `by` elements (0 to 7), zeros above
 __device__ __forceinline__ u32x4 move_down(u32x4 v, uint32_t by)      // bf16
 {
@@ -77,65 +130,7 @@ __device__ __forceinline__ void move_down(float4_t &lo, float4_t &hi, uint32_t b
     if (by & 4) lo = hi, hi = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
 }
 
-// Elements [col, col + 8) of a row; those at or past n are zeros (n > col: at least one is there).  A chunk that the row's end cuts
-// is read as the row's last eight elements and moved down, where there are eight (one load, few registers); else
-// element by element.  HELD: rows have at least eight elements, and the lanes of a wave share them.  Whether rows have such a chunk is asked of the row length, the same for all lanes: a
-// question to each lane would be passed with the lanes masked and wait for the load on the way (SwiGLU backward 129 us instead of 107).
-template <int KIND, bool HELD, bool STREAM, typename I>
-__device__ __forceinline__ Raw<KIND> load8(const RowSrc &s, int64_t row, I col, I n)
-{
-    Raw<KIND> r;
-    const I at = col + kChunk > n ? n - kChunk : col;     // below zero in a row of fewer than eight
-    const uint32_t by = (uint32_t)(col - at);
-    if constexpr (KIND == kBf16) {
-        const uint16_t *const p = static_cast<const uint16_t *>(s.p);
-        if (HELD || n >= kChunk) {
-            r.q = load_as<bf16x8_at2, STREAM>(row_at<HELD>(p, row, s.ld, at));
-            if (n % kChunk != 0) r.q = move_down(r.q, by);
-        } else {
-            r.q = u32x4{0, 0, 0, 0};
-#pragma unroll
-            for (int i = 0; i < kChunk - 1; ++i)
-                if (i < n) r.q[i / 2] |= (uint32_t)p[row * s.ld + i] << (16 * (i & 1));
-        }
-    } else if constexpr (KIND == kF32) {
-        const float *const p = static_cast<const float *>(s.p);
-        if (HELD || n >= kChunk) {
-            r.lo = load_as<f32x4_at4, STREAM>(row_at<HELD>(p, row, s.ld, at));
-            r.hi = load_as<f32x4_at4, STREAM>(row_at<HELD>(p, row, s.ld, at) + 4);
-            if (n % kChunk != 0) move_down(r.lo, r.hi, by);
-        } else {
-            r.lo = r.hi = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int i = 0; i < kChunk - 1; ++i)
-                if (i < n) (i < 4 ? r.lo : r.hi)[i & 3] = p[row * s.ld + i];
-        }
-    } else {
-        const uint8_t *const p = static_cast<const uint8_t *>(s.p);
-        if (HELD || n >= kChunk) {
-            r.q = load_as<code8_at1, STREAM>(row_at<HELD>(p, row, s.ld, at));
-            if (n % kChunk != 0) r.q = move_down(r.q, by);
-        } else {
-            r.q = u32x2{0, 0};
-#pragma unroll
-            for (int i = 0; i < kChunk - 1; ++i)
-                if (i < n) r.q[i / 4] |= (uint32_t)p[row * s.ld + i] << (8 * (i & 3));
-        }
-        r.e = *row_at<HELD>(s.exps, row, s.groups, col / kCkptGroup);
-    }
-    return r;
-}
-
-template <int KIND> __device__ __forceinline__ Raw<KIND> zero8()
-{
-    Raw<KIND> r;
-    if constexpr (KIND == kBf16) r.q = u32x4{0, 0, 0, 0};
-    else if constexpr (KIND == kF32) r.lo = r.hi = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    else { r.q = u32x2{0, 0}; r.e = 127; }
-    return r;
-}
-
-__device__ __forceinline__ void widen8(const Raw<kBf16> &r, float (&v)[8])
+__device__ __forceinline__ void widen(const Raw<kBf16> &r, float (&v)[8])
 {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -143,7 +138,7 @@ __device__ __forceinline__ void widen8(const Raw<kBf16> &r, float (&v)[8])
         v[2 * i + 1] = bf16_hi(r.q[i]);
     }
 }
-__device__ __forceinline__ void widen8(const Raw<kF32> &r, float (&v)[8])
+__device__ __forceinline__ void widen(const Raw<kF32> &r, float (&v)[8])
 {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -152,7 +147,7 @@ __device__ __forceinline__ void widen8(const Raw<kF32> &r, float (&v)[8])
     }
 }
 // code * 2^e: exact but for results below 2^-126
-__device__ __forceinline__ void widen8(const Raw<kCkpt8> &r, float (&v)[8])
+__device__ __forceinline__ void widen(const Raw<kCkpt8> &r, float (&v)[8])
 {
     const float scale = u2f(r.e << 23);
 #pragma unroll
@@ -164,6 +159,25 @@ __device__ __forceinline__ void widen8(const Raw<kCkpt8> &r, float (&v)[8])
         v[4 * i + 2] = b.x * scale;
         v[4 * i + 3] = b.y * scale;
     }
+}
+
+// A chunk that load8 or zero8 gave for this place, in its place: one that the row's end cuts was read further up and is moved down here, where the
+// loads after it are on their way.  Whether rows have such a chunk is asked of the row length, the same for all lanes: a question to each
+// lane would be passed with the lanes masked, the wait for the load included.
+template <int KIND, typename I> __device__ __forceinline__ Raw<KIND> settle8(Raw<KIND> r, I col, I n)
+{
+    if (n % kChunk != 0 && n > kChunk) {
+        const I over = col + kChunk - n;
+        const uint32_t by = over > 0 && over < kChunk ? (uint32_t)over : 0;      // past the end altogether: zeros already
+        if constexpr (KIND == kF32) move_down(r.lo, r.hi, by);
+        else r.q = move_down(r.q, by);
+    }
+    return r;
+}
+// its values; those at or past n are zeros
+template <int KIND, typename I> __device__ __forceinline__ void widen8(const Raw<KIND> &r, I col, I n, float (&v)[8])
+{
+    widen(settle8(r, col, n), v);
 }
 
 // ---- stores -----------------------------------------------------------------------------------
