@@ -15,9 +15,21 @@ namespace {
 
 constexpr int kSwiglu = 0, kGelu = 1;
 constexpr int kThreads = 256;
-// rows of a thread whose loads are on their way together: two, us of one / two: SwiGLU forward 16384 x 4096 99 / 95, GELU 4099 x 2752 14.4 / 13.8,
-// checkpoint 8192 x 8192 saved 42 / 39.7 and loaded 35.8 / 31.2; one for SwiGLU's backward pass, where five streams are enough (101 / 122)
-constexpr int kRows = 2, kRowsSwigluBwd = 1;
+// Calls by the bytes that they move: large ones read past the caches (see streams()).
+enum { kSmall = 0, kMiddle = 1, kLarge = 2 };
+constexpr double kMiddleBytes = 8 << 20;
+// Rows of a thread whose loads are on their way together: two keep more bytes in flight, one starts and ends sooner and leaves registers for more waves.
+// us of one / two, bf16 source where nothing else stands:
+//   SwiGLU forward with checkpoint   16384 x 4096  92 / 96      2000 x 2752  10.6 / 11.4    64 x 8192  3.9 / 4.8      always one
+//   SwiGLU backward from one         16384 x 4096  81 / 90                                                            always one
+//   GELU backward                    8192 x 8192   62 / 63      4099 x 2752  12.3 / 13.8    64 x 8192  3.0 / 3.6      always one
+//   GELU backward, checkpoint        8192 x 8192   58 / 55      4099 x 2752  11.7 / 12.1    64 x 8192  3.1 / 3.7      two if large
+//   GELU forward with checkpoint     8192 x 8192   57 / 52      4099 x 2752  11.7 / 11.5    64 x 8192  3.1 / 3.8      two from the middle on
+//   checkpoint saved                 8192 x 8192   41 / 36      4099 x 2752   8.2 /  7.8    64 x 8192  2.9 / 3.3      two from the middle on
+//   checkpoint loaded                8192 x 8192   42 / 38      4099 x 2752   7.9 /  7.3    64 x 8192  2.6 / 2.9      two from the middle on
+constexpr int rows_fwd(int act, int size) { return act == kSwiglu || size == kSmall ? 1 : 2; }
+constexpr int rows_bwd(int act, int kind, int size) { return act == kGelu && kind == kCkpt8 && size == kLarge ? 2 : 1; }
+constexpr int rows_copy(int size) { return size == kSmall ? 1 : 2; }
 constexpr int kMaxRowBlocks = 65535;    // of a launch's grid; beyond that a workgroup walks over several
 
 // rows x cols in chunks of eight; a workgroup takes 2^shift chunks of 256 / 2^shift rows, whole groups of 16 chunks
@@ -101,9 +113,10 @@ __device__ __forceinline__ Raw<KIND> load8_or_0(const RowSrc &s, int64_t row, in
 template <int KIND> struct Pair { Raw<KIND> a, b; };
 template <int KIND, int GKIND> struct Triple { Raw<KIND> a, b; Raw<GKIND> da; };
 
-template <int KIND, bool OF32, bool STREAM, int ACT>
+template <int KIND, bool OF32, int SIZE, int ACT>
 __global__ __launch_bounds__(kThreads) void act_fwd_kernel(const ActArgs a)
 {
+    constexpr bool STREAM = SIZE == kLarge;
     const int F = a.n.cols;
     const auto load = [&](int64_t row, int col) {
         Pair<KIND> in;
@@ -111,7 +124,7 @@ __global__ __launch_bounds__(kThreads) void act_fwd_kernel(const ActArgs a)
         if constexpr (ACT == kSwiglu) in.b = load8_or_0<KIND, STREAM>(a.h, row, col, F, F);
         return in;
     };
-    for_chunks<kRows>(a.n, load, [&](int64_t row, int col, const Pair<KIND> &in) {
+    for_chunks<rows_fwd(ACT, SIZE)>(a.n, load, [&](int64_t row, int col, const Pair<KIND> &in) {
         float x[8], o[8];
         widen8(in.a, col, F, x);
         if constexpr (ACT == kSwiglu) {
@@ -132,9 +145,10 @@ __global__ __launch_bounds__(kThreads) void act_fwd_kernel(const ActArgs a)
     });
 }
 
-template <int KIND, bool GF32, bool OF32, bool STREAM, int ACT>
+template <int KIND, bool GF32, bool OF32, int SIZE, int ACT>
 __global__ __launch_bounds__(kThreads) void act_bwd_kernel(const ActArgs a)
 {
+    constexpr bool STREAM = SIZE == kLarge;
     constexpr int GKIND = GF32 ? kF32 : kBf16;
     using In = Triple<KIND, GKIND>;
     const int F = a.n.cols;
@@ -153,7 +167,7 @@ __global__ __launch_bounds__(kThreads) void act_bwd_kernel(const ActArgs a)
         }
         return in;
     };
-    for_chunks<ACT == kSwiglu ? kRowsSwigluBwd : kRows>(a.n, load, [&](int64_t row, int col, const In &in) {
+    for_chunks<rows_bwd(ACT, KIND, SIZE)>(a.n, load, [&](int64_t row, int col, const In &in) {
         if (col >= F) return;
         float x[8], da[8];
         widen8(in.da, col, F, da);
@@ -178,10 +192,11 @@ __global__ __launch_bounds__(kThreads) void act_bwd_kernel(const ActArgs a)
     });
 }
 
-template <int KIND, bool STREAM>
+template <int KIND, int SIZE>
 __global__ __launch_bounds__(kThreads) void ckpt8_save_kernel(const CopyArgs a)
 {
-    for_chunks<kRows>(a.n, [&](int64_t row, int col) { return load8_or_0<KIND, STREAM>(a.src, row, col, a.n.cols, 0); },
+    constexpr bool STREAM = SIZE == kLarge;
+    for_chunks<rows_copy(SIZE)>(a.n, [&](int64_t row, int col) { return load8_or_0<KIND, STREAM>(a.src, row, col, a.n.cols, 0); },
                       [&](int64_t row, int col, const Raw<KIND> &in) {
         float x[8];
         widen8(in, col, a.n.cols, x);
@@ -189,10 +204,11 @@ __global__ __launch_bounds__(kThreads) void ckpt8_save_kernel(const CopyArgs a)
     });
 }
 
-template <bool OF32, bool STREAM>
+template <bool OF32, int SIZE>
 __global__ __launch_bounds__(kThreads) void ckpt8_load_kernel(const CopyArgs a)
 {
-    for_chunks<kRows>(a.n, [&](int64_t row, int col) { return col < a.n.cols ? load8<kCkpt8, false, STREAM>(a.src, row, col, a.n.cols) : zero8<kCkpt8>(); },
+    constexpr bool STREAM = SIZE == kLarge;
+    for_chunks<rows_copy(SIZE)>(a.n, [&](int64_t row, int col) { return col < a.n.cols ? load8<kCkpt8, false, STREAM>(a.src, row, col, a.n.cols) : zero8<kCkpt8>(); },
                       [&](int64_t row, int col, const Raw<kCkpt8> &in) {
         if (col >= a.n.cols) return;
         float x[8];
@@ -211,37 +227,47 @@ Chunks chunks_of(int64_t rows, int64_t cols)
     return Chunks{rows, (int)cols, shift};
 }
 
-dim3 grid_of(const Chunks &n, int rows = kRows)      // of a thread
+dim3 grid_of(const Chunks &n, int rows)      // of a thread
 {
     const int64_t wide = (int64_t)kChunk << n.shift, tall = kThreads >> n.shift, blocks = (n.rows + rows * tall - 1) / (rows * tall);
     return dim3((unsigned)((n.cols + wide - 1) / wide), (unsigned)(blocks < kMaxRowBlocks ? blocks : kMaxRowBlocks));
 }
 
-// f(std::true_type) for a call of so many bytes per element that streams, f(std::false_type) for another
+// f(size) for a call of so many bytes per element, the size as a constant
 template <typename F> void by_size(const Chunks &n, double bytes, const F &f)
 {
-    if (streams((double)n.rows * n.cols * bytes)) f(std::true_type{});
-    else f(std::false_type{});
+    const double all = (double)n.rows * n.cols * bytes;
+    if (streams(all)) f(std::integral_constant<int, kLarge>{});
+    else if (all > kMiddleBytes) f(std::integral_constant<int, kMiddle>{});
+    else f(std::integral_constant<int, kSmall>{});
 }
 constexpr double bytes_of(int kind) { return kind == kF32 ? 4.0 : kind == kBf16 ? 2.0 : 1.0; }
 
+template <int KIND, bool OF32, int SIZE, int ACT> void run_act_fwd(const ActArgs &a, hipStream_t st)
+{
+    constexpr int R = rows_fwd(ACT, SIZE), S = R == 1 && SIZE == kMiddle ? kSmall : SIZE;     // what differs in nothing is one kernel
+    act_fwd_kernel<KIND, OF32, S, ACT><<<grid_of(a.n, R), kThreads, 0, st>>>(a);
+}
 template <int KIND, bool OF32> void run_act_fwd(const ActArgs &a, int act, hipStream_t st)
 {
     const double parts = act == kSwiglu ? 2.0 : 1.0;
-    by_size(a.n, parts * (bytes_of(KIND) + (a.ckpt.codes ? 1.0 : 0.0)) + (OF32 ? 4.0 : 2.0), [&](auto stream) {
-        constexpr bool S = decltype(stream)::value;
-        if (act == kSwiglu) act_fwd_kernel<KIND, OF32, S, kSwiglu><<<grid_of(a.n), kThreads, 0, st>>>(a);
-        else act_fwd_kernel<KIND, OF32, S, kGelu><<<grid_of(a.n), kThreads, 0, st>>>(a);
+    by_size(a.n, parts * (bytes_of(KIND) + (a.ckpt.codes ? 1.0 : 0.0)) + (OF32 ? 4.0 : 2.0), [&](auto size) {
+        constexpr int S = decltype(size)::value;
+        act == kSwiglu ? run_act_fwd<KIND, OF32, S, kSwiglu>(a, st) : run_act_fwd<KIND, OF32, S, kGelu>(a, st);
     });
 }
 
+template <int KIND, bool GF32, bool OF32, int SIZE, int ACT> void run_act_bwd(const ActArgs &a, hipStream_t st)
+{
+    constexpr int S = SIZE == kMiddle ? kSmall : SIZE;
+    act_bwd_kernel<KIND, GF32, OF32, S, ACT><<<grid_of(a.n, rows_bwd(ACT, KIND, S)), kThreads, 0, st>>>(a);
+}
 template <int KIND, bool GF32, bool OF32> void run_act_bwd(const ActArgs &a, int act, hipStream_t st)
 {
     const double parts = act == kSwiglu ? 2.0 : 1.0;
-    by_size(a.n, parts * (bytes_of(KIND) + (OF32 ? 4.0 : 2.0)) + (GF32 ? 4.0 : 2.0), [&](auto stream) {
-        constexpr bool S = decltype(stream)::value;
-        if (act == kSwiglu) act_bwd_kernel<KIND, GF32, OF32, S, kSwiglu><<<grid_of(a.n, kRowsSwigluBwd), kThreads, 0, st>>>(a);
-        else act_bwd_kernel<KIND, GF32, OF32, S, kGelu><<<grid_of(a.n), kThreads, 0, st>>>(a);
+    by_size(a.n, parts * (bytes_of(KIND) + (OF32 ? 4.0 : 2.0)) + (GF32 ? 4.0 : 2.0), [&](auto size) {
+        constexpr int S = decltype(size)::value;
+        act == kSwiglu ? run_act_bwd<KIND, GF32, OF32, S, kSwiglu>(a, st) : run_act_bwd<KIND, GF32, OF32, S, kGelu>(a, st);
     });
 }
 
@@ -273,10 +299,10 @@ hipError_t launch_act_bwd(const RowSrc &da, const RowSrc &h, int64_t N, int64_t 
 hipError_t launch_ckpt8_save(const RowSrc &src, int64_t N, int64_t D, const CkptOut &ckpt, hipStream_t st)
 {
     const CopyArgs a{src, chunks_of(N, D), RowDst{}, ckpt};
-    by_size(a.n, bytes_of(src.kind) + 1.0, [&](auto stream) {
-        constexpr bool S = decltype(stream)::value;
-        if (src.kind == kF32) ckpt8_save_kernel<kF32, S><<<grid_of(a.n), kThreads, 0, st>>>(a);
-        else ckpt8_save_kernel<kBf16, S><<<grid_of(a.n), kThreads, 0, st>>>(a);
+    by_size(a.n, bytes_of(src.kind) + 1.0, [&](auto size) {
+        constexpr int S = decltype(size)::value;
+        if (src.kind == kF32) ckpt8_save_kernel<kF32, S><<<grid_of(a.n, rows_copy(S)), kThreads, 0, st>>>(a);
+        else ckpt8_save_kernel<kBf16, S><<<grid_of(a.n, rows_copy(S)), kThreads, 0, st>>>(a);
     });
     return hipGetLastError();
 }
@@ -284,10 +310,10 @@ hipError_t launch_ckpt8_save(const RowSrc &src, int64_t N, int64_t D, const Ckpt
 hipError_t launch_ckpt8_load(const RowSrc &src, int64_t N, int64_t D, const RowDst &out, hipStream_t st)
 {
     const CopyArgs a{src, chunks_of(N, D), out, CkptOut{}};
-    by_size(a.n, 1.0 + (out.f32 ? 4.0 : 2.0), [&](auto stream) {
-        constexpr bool S = decltype(stream)::value;
-        if (out.f32) ckpt8_load_kernel<true, S><<<grid_of(a.n), kThreads, 0, st>>>(a);
-        else ckpt8_load_kernel<false, S><<<grid_of(a.n), kThreads, 0, st>>>(a);
+    by_size(a.n, 1.0 + (out.f32 ? 4.0 : 2.0), [&](auto size) {
+        constexpr int S = decltype(size)::value;
+        if (out.f32) ckpt8_load_kernel<true, S><<<grid_of(a.n, rows_copy(S)), kThreads, 0, st>>>(a);
+        else ckpt8_load_kernel<false, S><<<grid_of(a.n, rows_copy(S)), kThreads, 0, st>>>(a);
     });
     return hipGetLastError();
 }
