@@ -4,7 +4,10 @@
 //   GELU    a = x s(z(x))        dx = da (s(z) + x s(z) s(-z) z'(x)),  z = 2 sqrt(2 / pi) (x + 0.044715 x^3)   (the tanh form)
 //   with s(z) = 1 / (1 + exp(-z)); s(-z) comes from the same exponential, without the cancellation of 1 - s(z).
 //
-// Element by element but for the maxima of a checkpoint's groups, which the 16 lanes of a group exchange in registers.  Bound: HBM.
+// Element by element but for the maxima of a checkpoint's groups, which the 16 lanes of a group exchange in registers.  Bound: HBM (a copy of
+// 1 GB reaches 5.1 TB/s here, one of 64 MB, which the last-level cache holds, 6.9); small calls: the launch.
+//
+// Figures: bf16 arrays, us and TB/s over the bytes that a call has to read and write.
 #include <type_traits>
 
 #include "rowwise.h"
@@ -113,6 +116,8 @@ __device__ __forceinline__ Raw<KIND> load8_or_0(const RowSrc &s, int64_t row, in
 template <int KIND> struct Pair { Raw<KIND> a, b; };
 template <int KIND, int GKIND> struct Triple { Raw<KIND> a, b; Raw<GKIND> da; };
 
+// SwiGLU with a checkpoint 16384 x 4096 91 us, 5.9 TB/s (alone in its arrays 80.5, 6.7), without 62, 6.5; GELU with a checkpoint 4099 x 2752 11.5, 4.9,
+// 8192 x 8192 52, 6.4; 64 x 8192 3.1
 template <int KIND, bool OF32, int SIZE, int ACT>
 __global__ __launch_bounds__(kThreads) void act_fwd_kernel(const ActArgs a)
 {
@@ -145,6 +150,7 @@ __global__ __launch_bounds__(kThreads) void act_fwd_kernel(const ActArgs a)
     });
 }
 
+// SwiGLU 16384 x 4096 from a checkpoint 81 us, 6.6 TB/s, from H 107, 6.3; GELU from a checkpoint 4099 x 2752 11.8, 4.8, 8192 x 8192 56, 6.0
 template <int KIND, bool GF32, bool OF32, int SIZE, int ACT>
 __global__ __launch_bounds__(kThreads) void act_bwd_kernel(const ActArgs a)
 {
@@ -192,6 +198,7 @@ __global__ __launch_bounds__(kThreads) void act_bwd_kernel(const ActArgs a)
     });
 }
 
+// 8192 x 8192 35 us, 5.8 TB/s
 template <int KIND, int SIZE>
 __global__ __launch_bounds__(kThreads) void ckpt8_save_kernel(const CopyArgs a)
 {
@@ -204,6 +211,7 @@ __global__ __launch_bounds__(kThreads) void ckpt8_save_kernel(const CopyArgs a)
     });
 }
 
+// 8192 x 8192 31 us, 6.5 TB/s right after it was saved
 template <bool OF32, int SIZE>
 __global__ __launch_bounds__(kThreads) void ckpt8_load_kernel(const CopyArgs a)
 {

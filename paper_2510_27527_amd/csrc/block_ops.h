@@ -27,8 +27,8 @@ struct CkptOut {
 
 // Calls that move more than half of the 256 MB last-level cache read their arrays past it: what the reads would leave there displaces what the call
 // writes, which is read next.  A kernel of its own: asked at each access, the question costs more than it gives.  us, through the caches /
-// past them: SwiGLU backward 16384 x 4096 (537 MB) 99.5 / 91, norm backward 4096 x 16384 (336 MB) 78 / 68.5, checkpoint 8192 x 8192
-// saved (201 MB) 39.7 / 34.7; and under it the other way: GELU 4099 x 2752 (56 MB) forward 13.8 / 15.0, backward 14.4 / 16.6.  (The norm's
+// past them: SwiGLU 16384 x 4096 (537 MB) forward 95.5 / 91.5, backward 91 / 82, norm backward 4096 x 16384 (336 MB) 78 / 66, checkpoint 8192 x 8192
+// saved (201 MB) 39.5 / 34.7; and under it the other way: GELU 4099 x 2752 (56 MB) forward 11.8 / 13.2, backward 12.2 / 13.5.  (The norm's
 // forward pass gains nothing: 4096 x 16384 67.9 / 68.7; writes past the caches make the next reader pay: the same checkpoint loaded 31 / 40.)
 inline bool streams(double bytes) { return bytes > (double)(128 << 20); }
 
