@@ -367,6 +367,51 @@ def test_strided_and_unaligned(tj, at, gap):
             assert torch.equal(ys, y) and untouched(buf, ys)
 
 
+# calls of under 8 MB, of more, of more than half the last-level cache: what a row gives does not depend on the rows around it
+@pytest.mark.parametrize("N,F", [(1601, 1999), (30011, 1543)])
+@pytest.mark.parametrize("swiglu", [True, False])
+def test_rows_do_not_depend_on_the_size_of_a_call(tj, N, F, swiglu):
+    B = tj.binding
+    act, parts = (B.ACT_SWIGLU, 2) if swiglu else (B.ACT_GELU, 1)
+    g = torch.Generator(device="cuda").manual_seed(N)
+    H = torch.randn(N, parts * F, generator=g, device="cuda").to(BF)
+    dA = torch.randn(N, F, generator=g, device="cuda").to(BF)
+    kept = tj.alloc_act_ckpt8(N, F, act)
+    A = tj.act_fwd(H, act, ckpt=kept)
+    dH, dH8 = tj.act_bwd(dA, H, act), tj.act_bwd(dA, kept, act)
+    saved = tj.ckpt8_save(H)
+    loaded = tj.ckpt8_load(saved)
+    for at in (0, N // 2, N - 200):
+        rows = slice(at, at + 200)
+        h, da = H[rows].contiguous(), dA[rows].contiguous()
+        k = tj.alloc_act_ckpt8(200, F, act)
+        assert torch.equal(tj.act_fwd(h, act, ckpt=k), A[rows])
+        both = slice(at * parts, (at + 200) * parts)
+        assert torch.equal(k.codes, kept.codes[both]) and torch.equal(k.exps, kept.exps[both])
+        assert torch.equal(tj.act_bwd(da, h, act), dH[rows]) and torch.equal(tj.act_bwd(da, k, act), dH8[rows])
+        s = tj.ckpt8_save(h)
+        assert torch.equal(s.codes, saved.codes[rows]) and torch.equal(s.exps, saved.exps[rows])
+        assert torch.equal(tj.ckpt8_load(s), loaded[rows])
+
+
+@pytest.mark.parametrize("D", [500, 1023, 2047, 4096, 8191, 16384])
+def test_norm_rows_do_not_depend_on_the_size_of_a_call(tj, D):
+    N = (144 << 20) // (5 * D)
+    g = torch.Generator(device="cuda").manual_seed(D)
+    x, dy = torch.randn(N, D, generator=g, device="cuda").to(BF), torch.randn(N, D, generator=g, device="cuda").to(BF)
+    gamma, beta = torch.randn(D, generator=g, device="cuda"), torch.randn(D, generator=g, device="cuda")
+    stats, kept = tj.alloc_stats(N), tj.alloc_ckpt8(N, D)
+    y = tj.norm_fwd(x, gamma, beta, stats=stats, ckpt=kept)
+    dx, dx8 = tj.norm_bwd(dy, x, stats, gamma)[0], tj.norm_bwd(dy, kept, stats, gamma)[0]
+    for at in (0, N // 2, N - 100):
+        rows = slice(at, at + 100)
+        s, k = tj.alloc_stats(100), tj.alloc_ckpt8(100, D)
+        h, d = x[rows].contiguous(), dy[rows].contiguous()
+        assert torch.equal(tj.norm_fwd(h, gamma, beta, stats=s, ckpt=k), y[rows])
+        assert torch.equal(s, stats[rows]) and torch.equal(k.codes, kept.codes[rows]) and torch.equal(k.exps, kept.exps[rows])
+        assert torch.equal(tj.norm_bwd(d, h, s, gamma)[0], dx[rows]) and torch.equal(tj.norm_bwd(d, k, s, gamma)[0], dx8[rows])
+
+
 def test_checkpoints_write_nothing_past_their_ends(tj):
     """Buffers cut out of larger ones: every byte around stays."""
     for N, D in ((3, 130), (2, 7), (5, 1023)):
