@@ -582,10 +582,13 @@ def _rows(t: torch.Tensor, what: str):
     return kind, s0 if rows > 1 else n, rows, n
 
 
-def _out_rows(t: Optional[torch.Tensor], rows: int, n: int, out_dtype: int, device, what: str):
-    """The output matrix, allocated where none is given, and its row stride."""
+def _out_rows(t: Optional[torch.Tensor], rows: int, n: int, out_dtype: int, like: torch.Tensor, what: str):
+    """The output matrix, allocated on like's device where none is given, and its row stride."""
     if t is None:
-        return torch.empty((rows, n), dtype=torch.bfloat16 if out_dtype == OUT_BF16 else torch.float32, device=device), n
+        dtype = torch.bfloat16 if out_dtype == OUT_BF16 else torch.float32
+        if dtype == like.dtype:              # 0.3 us of the host's less
+            return like.new_empty((rows, n)), n
+        return torch.empty((rows, n), dtype=dtype, device=like.device), n
     kind, ld, r, c = _rows(t, what)
     assert r == rows and c == n and kind == (SRC_BF16 if out_dtype == OUT_BF16 else SRC_F32), what
     return t, ld
@@ -612,7 +615,7 @@ def norm_fwd(X: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Option
     """nvfp4_norm_fwd: layer norm (NORM_LAYER) or RMS norm (NORM_RMS) of every row of X.  For training pass stats (alloc_stats) and, to keep
     the input in 8 bits, ckpt (alloc_ckpt8); both are filled."""
     kind, ldx, N, D = _rows(X, "X")
-    Y, ldy = _out_rows(Y, N, D, out_dtype, X.device, "Y")
+    Y, ldy = _out_rows(Y, N, D, out_dtype, X, "Y")
     cs = None
     if ckpt is not None:
         _check_ckpt(ckpt, N, D)
@@ -630,7 +633,6 @@ def norm_bwd(dY: torch.Tensor, X, stats: torch.Tensor, gamma: Optional[torch.Ten
     """nvfp4_norm_bwd: (dX, dgamma, dbeta); X is the forward call's input or its Ckpt8.  params=False: dX alone; RMS norm has no dbeta
     unless one is passed."""
     dkind, lddy, N, D = _rows(dY, "dY")
-    dev = dY.device
     if isinstance(X, Ckpt8):
         _check_ckpt(X, N, D)
         kind, ldx, src = SRC_CKPT8, 0, C.byref(X.c_struct())
@@ -639,13 +641,13 @@ def norm_bwd(dY: torch.Tensor, X, stats: torch.Tensor, gamma: Optional[torch.Ten
         assert shape == [N, D], "X: the shape of dY"
         src = _ptr(X)
     _check_stats(stats, N)
-    dX, lddx = _out_rows(dX, N, D, out_dtype, dev, "dX")
+    dX, lddx = _out_rows(dX, N, D, out_dtype, dY, "dX")
     if params:
-        dgamma = torch.empty(D, dtype=torch.float32, device=dev) if dgamma is None else dgamma
+        dgamma = stats.new_empty(D) if dgamma is None else dgamma
         if dbeta is None and norm == NORM_LAYER:
-            dbeta = torch.empty(D, dtype=torch.float32, device=dev)
+            dbeta = stats.new_empty(D)
         if ws is None:
-            ws = alloc_workspace(lib().nvfp4_norm_workspace_bytes(N, D), dev)
+            ws = alloc_workspace(lib().nvfp4_norm_workspace_bytes(N, D), dY.device)
     else:
         dgamma = dbeta = None
     _check(lib().nvfp4_norm_bwd(_ptr(dY), dkind, lddy, src, kind, ldx, _ptr(stats), _param(gamma, D, "gamma"), N, D, norm, _ptr(dX), out_dtype,
@@ -661,7 +663,7 @@ def act_fwd(H: torch.Tensor, act: int = ACT_SWIGLU, out_dtype: int = OUT_BF16, *
     if act == ACT_SWIGLU:
         assert F % 2 == 0, "H: gates and up values"
         F //= 2
-    A, lda = _out_rows(A, N, F, out_dtype, H.device, "A")
+    A, lda = _out_rows(A, N, F, out_dtype, H, "A")
     cs = None
     if ckpt is not None:
         _check_ckpt(ckpt, 2 * N if act == ACT_SWIGLU else N, F)
@@ -681,7 +683,7 @@ def act_bwd(dA: torch.Tensor, H, act: int = ACT_SWIGLU, out_dtype: int = OUT_BF1
         kind, ldh, *shape = _rows(H, "H")
         assert shape == [N, parts * F], "H"
         src = _ptr(H)
-    dH, lddh = _out_rows(dH, N, parts * F, out_dtype, dA.device, "dH")
+    dH, lddh = _out_rows(dH, N, parts * F, out_dtype, dA, "dH")
     _check(lib().nvfp4_act_bwd(_ptr(dA), dkind, ldda, src, kind, ldh, N, F, act, _ptr(dH), out_dtype, lddh, _stream()), "nvfp4_act_bwd")
     return dH
 
@@ -698,7 +700,7 @@ def ckpt8_save(X: torch.Tensor, out: Optional[Ckpt8] = None) -> Ckpt8:
 def ckpt8_load(src: Ckpt8, out_dtype: int = OUT_BF16, *, Y: Optional[torch.Tensor] = None) -> torch.Tensor:
     """nvfp4_ckpt8_load: the activation that a checkpoint holds."""
     _check_ckpt(src, src.rows, src.K)
-    Y, ldy = _out_rows(Y, src.rows, src.K, out_dtype, src.codes.device, "Y")
+    Y, ldy = _out_rows(Y, src.rows, src.K, out_dtype, src.codes, "Y")
     _check(lib().nvfp4_ckpt8_load(C.byref(src.c_struct()), _ptr(Y), out_dtype, ldy, _stream()), "nvfp4_ckpt8_load")
     return Y
 
@@ -707,6 +709,6 @@ def gemv(X: torch.Tensor, W: NVFP4Tensor, out_dtype: int = OUT_BF16, *, Y: Optio
     """nvfp4_gemv: Y = X W^T for the bf16 activations of a few tokens on packed weights (linear_fwd's Wq)."""
     kind, ldx, M, K = _rows(X, "X")
     assert kind == SRC_BF16 and K == W.K, "X: bf16 [M, W.K]"
-    Y, ldy = _out_rows(Y, M, W.rows, out_dtype, X.device, "Y")
+    Y, ldy = _out_rows(Y, M, W.rows, out_dtype, X, "Y")
     _check(lib().nvfp4_gemv(_ptr(X), ldx, M, C.byref(W.c_struct()), _ptr(Y), out_dtype, ldy, _stream()), "nvfp4_gemv")
     return Y
