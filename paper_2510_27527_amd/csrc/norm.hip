@@ -54,25 +54,46 @@ __device__ __forceinline__ void param8(const float *p, int col, int D, float fil
     }
 }
 
+// The parameters of the columns of a row of at least eight to LDS, [halves of a chunk][V TPR chunks], by the TPR threads of a row; `fill` without parameters.  All
+// loads are on their way at once: no lane is asked whether it has columns, one that has none gets zeros in the end.
+template <int TPR, int V> __device__ __forceinline__ void params_to_lds(const float *p, int D, float fill, float4_t *to)
+{
+    const int t = threadIdx.x % TPR;
+    Raw<kF32> w[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        w[v].lo = w[v].hi = float4_t{fill, fill, fill, fill};
+        if (p) {
+            const int col = (t + v * TPR) * kChunk, at = col + kChunk > D ? D - kChunk : col;
+            w[v].lo = load_as<f32x4_at4, false>(p + at);
+            w[v].hi = load_as<f32x4_at4, false>(p + at + 4);
+        }
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int col = (t + v * TPR) * kChunk;
+        if (p) w[v] = settle8(w[v], col, D);
+        to[t + v * TPR] = col < D ? w[v].lo : float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        to[V * TPR + t + v * TPR] = col < D ? w[v].hi : float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+}
+
 // A row lies in the registers of TPR threads, V chunks of eight each; the parameters of a thread's columns stay there for all of its rows,
 // and the next row is on its way while a row is summed and written.
 //                      8192 x 768    16384 x 1024   16384 x 2048   16384 x 4096   8192 x 8192   4096 x 16384
-//   with a checkpoint   11.0  2.9      15.1  5.6      30.8  5.4      65.2  5.2      63.3  5.3      63.7  5.3
-//   without              8.6  2.9      12.1  5.6      24.2  5.5      43.0  6.2      43.8  6.1      43.4  6.2
+//   with a checkpoint   11.0  2.9      15.1  5.6      28.7  5.8      65.2  5.2      63.3  5.3      63.7  5.3
+//   without              8.6  2.9      12.1  5.6      22.2  6.0      43.0  6.2      43.8  6.1      43.4  6.2
 template <int KIND, bool OF32, int TPR, int V>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_fwd_kernel(const NormFwdArgs a)
 {
-    constexpr int ROWS = TPR < 256 ? 256 / TPR : 1;
+    constexpr int ROWS = TPR < 256 ? 256 / TPR : 1, CHUNKS = V * TPR;
+    constexpr bool LDS = TPR == 64 && V > 2;        // parameters there: registers for more waves (V = 2 without: 16384 x 1024 15.1 us, with 16.6)
     __shared__ float2_t red[2][ROWS * TPR / 64];
+    __shared__ float4_t weight[LDS ? 4 * CHUNKS : 1];      // [gamma, beta][halves of a chunk][chunks]
     const int t = threadIdx.x % TPR;
     const int64_t step = (int64_t)gridDim.x * ROWS;
     const float inv_d = 1.0f / (float)a.D;
     float g[V][8], b[V][8];
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        param8(a.gamma, (t + v * TPR) * kChunk, a.D, 1.0f, g[v]);
-        param8(a.beta, (t + v * TPR) * kChunk, a.D, 0.0f, b[v]);
-    }
     Raw<KIND> next[V];
     const auto load = [&](int64_t row) {
 #pragma unroll
@@ -82,7 +103,20 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_fwd_kernel(const N
         }
     };
     int64_t row = (int64_t)blockIdx.x * ROWS + __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);     // the same in all lanes of a wave
-    if (row < a.N) load(row);
+    if constexpr (LDS) {
+        if (row < a.N) load(row);
+        const int slot = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
+        if (slot == 0) params_to_lds<TPR, V>(a.gamma, a.D, 1.0f, weight);
+        if (slot == 1) params_to_lds<TPR, V>(a.beta, a.D, 0.0f, weight + 2 * CHUNKS);
+        __syncthreads();
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            param8(a.gamma, (t + v * TPR) * kChunk, a.D, 1.0f, g[v]);
+            param8(a.beta, (t + v * TPR) * kChunk, a.D, 0.0f, b[v]);
+        }
+        if (row < a.N) load(row);
+    }
     for (; row < a.N; row += step) {       // one row a workgroup where TPR > 64: all of its threads are here
         float x[V][8];
 #pragma unroll
@@ -117,6 +151,13 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_fwd_kernel(const N
         for (int v = 0; v < V; ++v) {
             const int col = (t + v * TPR) * kChunk;
             if (col >= a.D) continue;
+            if constexpr (LDS) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    g[v][i] = weight[i / 4 * CHUNKS + t + v * TPR][i & 3];
+                    b[v][i] = weight[(2 + i / 4) * CHUNKS + t + v * TPR][i & 3];
+                }
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[v][i] = fmaf(x[v][i] * rstd, g[v][i], b[v][i]);
             store8<OF32, true>(a.y.p, a.y.ld, row, col, a.D, x[v]);
@@ -176,11 +217,11 @@ __global__ __launch_bounds__(1024) void norm_fwd_long_kernel(const NormFwdArgs a
 // As the forward kernel, with blockDim.x / TPR rows at once; a thread also keeps the sums of its columns over all of its rows.  In the
 // end those of the workgroup's rows are added through LDS, in their order: one partial sum a workgroup, one workgroup a CU, no atomics.
 //                        8192 x 768    16384 x 1024   16384 x 2048   16384 x 4096   8192 x 8192   4096 x 16384
-//   from a checkpoint     11.7  2.7      17.4  4.8      37.5  4.5      56.8  5.9      62.0  5.4      62.8  5.3
-//   from the input        11.2  3.4      19.1  5.3      41.0  4.9      65.4  6.2      67.4  6.0      70.4  5.7
-//   checkpoint, dx alone   9.6  3.3      15.0  5.6      36.2  4.6      54.6  6.2      58.0  5.8      58.2  5.8
+//   from a checkpoint     11.7  2.7      17.4  4.8      33.7  5.0      56.8  5.9      62.0  5.4      62.8  5.3
+//   from the input        11.2  3.4      19.1  5.3      37.6  5.4      65.4  6.2      67.4  6.0      70.4  5.7
+//   checkpoint, dx alone   9.6  3.3      15.0  5.6      31.3  5.4      54.6  6.2      58.0  5.8      58.2  5.8
 template <int KIND, bool GF32, bool OF32, bool STREAM, int TPR, int V>
-__global__ __launch_bounds__(1024) void norm_bwd_kernel(const NormBwdArgs a)
+__global__ __launch_bounds__(TPR == 64 && V > 2 ? 512 : 1024) void norm_bwd_kernel(const NormBwdArgs a)
 {
     constexpr int GKIND = GF32 ? kF32 : kBf16;
     constexpr int CHUNKS = V * TPR;
@@ -212,12 +253,7 @@ __global__ __launch_bounds__(1024) void norm_bwd_kernel(const NormBwdArgs a)
     int turn = 0;
     int64_t base = (int64_t)blockIdx.x * rows;      // of the workgroup: all of its threads stay together for the sums
     load(base + slot);
-    for (int c = threadIdx.x; c < CHUNKS; c += blockDim.x) {
-        float w[8];
-        param8(a.gamma, c * kChunk, a.D, 1.0f, w);
-        weight[c] = float4_t{w[0], w[1], w[2], w[3]};
-        weight[CHUNKS + c] = float4_t{w[4], w[5], w[6], w[7]};
-    }
+    if (slot == 0) params_to_lds<TPR, V>(a.gamma, a.D, 1.0f, weight);
     __syncthreads();
     for (; base < a.N; base += step) {
         const int64_t row = base + slot;
@@ -406,14 +442,16 @@ constexpr int kMaxHeldRow = 16384;      // longest row that a workgroup's regist
 constexpr int kLongBlocks = 8192;       // most workgroups where a row is longer
 
 bool held(int64_t D) { return D >= kChunk && D <= kMaxHeldRow; }
-// threads that hold a row
-int threads_of_row(int64_t D) { return D <= 1024 ? 64 : D <= 4096 ? 256 : D <= 8192 ? 512 : 1024; }
+// Threads that hold a row.  A wave as long as its registers last: no barrier, and no wave of a workgroup without columns.  us, a wave / 256 threads: with a checkpoint
+// forward 12000 x 1280 17.3 / 22.5, 16384 x 2048 28.7 / 30.2, 1000 x 2048 6.2 / 5.8, 4 x 1280 3.8 / 3.5; backward 19.1 / 24.4, 33.7 / 38.8, 8.7 / 7.4, 4.6 / 3.6.  Few rows
+// keep the wave all the same, so that what a row gives does not depend on the rows around it.
+int threads_of_row(int64_t D) { return D <= 2048 ? 64 : D <= 4096 ? 256 : D <= 8192 ? 512 : 1024; }
 
-// rows that a workgroup of the backward kernel takes at once, as many as give every CU a workgroup and at most 1024 threads, and its workgroups: each leaves
-// a partial sum of D columns, so there is one a CU
+// rows that a workgroup of the backward kernel takes at once, as many as give every CU a workgroup and at most 1024 threads (512 where a wave holds over
+// 1024 elements, for the registers), and its workgroups: each leaves a partial sum of D columns, so there is one a CU
 int64_t bwd_rows(int64_t N, int64_t D)
 {
-    const int64_t most = !held(D) ? 1 : 1024 / threads_of_row(D), want = (N + kMostPartials - 1) / kMostPartials;
+    const int64_t most = !held(D) ? 1 : D > 1024 && D <= 2048 ? 8 : 1024 / threads_of_row(D), want = (N + kMostPartials - 1) / kMostPartials;
     return want < 1 ? 1 : want < most ? want : most;
 }
 int64_t bwd_blocks(int64_t N, int64_t D)
@@ -426,7 +464,7 @@ template <int KIND, bool OF32, int TPR, int V> void run_norm_fwd(const NormFwdAr
 {
     constexpr int THREADS = TPR < 256 ? 256 : TPR, ROWS = THREADS / TPR;
     // 16 waves a CU, which then walk over their rows; with half the registers twice as many are there at once, and two rounds are faster still
-    // (16384 x 2048 34.5 us with 16 waves a CU, 31.4 with 32, 30.2 with 64; 16384 x 1024, which has the registers for 20, 15.2, 16.0, 16.9)
+    // (32768 x 512 17.3 us with 16 waves a CU, 16.2 with 64; 16384 x 1024, which has the registers for 20, 15.2, 16.9)
     constexpr int MOST = 256 * (1024 / THREADS) * (V == 1 ? 4 : 1);
     const int64_t want = (a.N + ROWS - 1) / ROWS;
     norm_fwd_kernel<KIND, OF32, TPR, V><<<(unsigned)(want < MOST ? want : MOST), THREADS, 0, st>>>(a);
@@ -437,7 +475,8 @@ template <int KIND, bool OF32> void run_norm_fwd(const NormFwdArgs &a, hipStream
     if (!held(a.D)) norm_fwd_long_kernel<KIND, OF32><<<(unsigned)(a.N < kLongBlocks ? a.N : kLongBlocks), 1024, 0, st>>>(a);
     else if (a.D <= 512) run_norm_fwd<KIND, OF32, 64, 1>(a, st);
     else if (a.D <= 1024) run_norm_fwd<KIND, OF32, 64, 2>(a, st);
-    else if (a.D <= 2048) run_norm_fwd<KIND, OF32, 256, 1>(a, st);
+    else if (a.D <= 1536) run_norm_fwd<KIND, OF32, 64, 3>(a, st);
+    else if (a.D <= 2048) run_norm_fwd<KIND, OF32, 64, 4>(a, st);
     else if (a.D <= 4096) run_norm_fwd<KIND, OF32, 256, 2>(a, st);
     else if (a.D <= 8192) run_norm_fwd<KIND, OF32, 512, 2>(a, st);
     else run_norm_fwd<KIND, OF32, 1024, 2>(a, st);
@@ -449,7 +488,9 @@ template <int KIND, bool GF32, bool OF32, int TPR, int V> void run_norm_bwd(cons
     const size_t weights = (size_t)V * TPR * kChunk, sums = rows > 1 && (a.part_g || a.part_b) ? 2 * rows * weights : 0;
     const size_t lds = (weights > sums ? weights : sums) * sizeof(float);
     const double each = (GF32 ? 4 : 2) + (KIND == kF32 ? 4 : KIND == kBf16 ? 2 : 1) + (OF32 ? 4 : 2);
-    if (streams((double)a.N * a.D * each)) norm_bwd_kernel<KIND, GF32, OF32, true, TPR, V><<<blocks, rows * TPR, lds, st>>>(a);
+    // From a checkpoint past the caches from half that size on, us of a forward and a backward pass, through / past: 16384 x 1024 (80 MB) 38.0 / 35.2, 4096 x 4096 40.0 / 37.7,
+    // 20000 x 768 38.3 / 36.1, 16384 x 768 (60 MB) 30.5 / 30.3; not so from the input: 16384 x 1024 (96 MB) 33.8 / 34.5, 20000 x 768 32.5 / 34.5
+    if (streams((double)a.N * a.D * each * (KIND == kCkpt8 ? 2 : 1))) norm_bwd_kernel<KIND, GF32, OF32, true, TPR, V><<<blocks, rows * TPR, lds, st>>>(a);
     else norm_bwd_kernel<KIND, GF32, OF32, false, TPR, V><<<blocks, rows * TPR, lds, st>>>(a);
 }
 
@@ -462,7 +503,8 @@ template <int KIND, bool GF32, bool OF32> void run_norm_bwd(const NormBwdArgs &a
     }
     else if (a.D <= 512) run_norm_bwd<KIND, GF32, OF32, 64, 1>(a, blocks, st);
     else if (a.D <= 1024) run_norm_bwd<KIND, GF32, OF32, 64, 2>(a, blocks, st);
-    else if (a.D <= 2048) run_norm_bwd<KIND, GF32, OF32, 256, 1>(a, blocks, st);
+    else if (a.D <= 1536) run_norm_bwd<KIND, GF32, OF32, 64, 3>(a, blocks, st);
+    else if (a.D <= 2048) run_norm_bwd<KIND, GF32, OF32, 64, 4>(a, blocks, st);
     else if (a.D <= 4096) run_norm_bwd<KIND, GF32, OF32, 256, 2>(a, blocks, st);
     else if (a.D <= 8192) run_norm_bwd<KIND, GF32, OF32, 512, 2>(a, blocks, st);
     else run_norm_bwd<KIND, GF32, OF32, 1024, 2>(a, blocks, st);
