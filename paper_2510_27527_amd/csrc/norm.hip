@@ -215,11 +215,12 @@ __global__ __launch_bounds__(1024) void norm_fwd_long_kernel(const NormFwdArgs a
 }
 
 // As the forward kernel, with blockDim.x / TPR rows at once; a thread also keeps the sums of its columns over all of its rows.  In the
-// end those of the workgroup's rows are added through LDS, in their order: one partial sum a workgroup, one workgroup a CU, no atomics.
+// end those of the workgroup's rows are added through LDS, in their order: one partial sum a workgroup, one workgroup a CU, no atomics.  (The figures are of calls
+// that repeat on the same arrays: 16384 x 1024 out of the last-level cache, through it, 17.4.)
 //                        8192 x 768    16384 x 1024   16384 x 2048   16384 x 4096   8192 x 8192   4096 x 16384
-//   from a checkpoint     11.7  2.7      17.4  4.8      33.7  5.0      56.8  5.9      62.0  5.4      62.8  5.3
+//   from a checkpoint     11.7  2.7      18.8  4.5      33.7  5.0      56.8  5.9      62.0  5.4      62.8  5.3
 //   from the input        11.2  3.4      19.1  5.3      37.6  5.4      65.4  6.2      67.4  6.0      70.4  5.7
-//   checkpoint, dx alone   9.6  3.3      15.0  5.6      31.3  5.4      54.6  6.2      58.0  5.8      58.2  5.8
+//   checkpoint, dx alone   9.6  3.3      16.5  5.1      31.3  5.4      54.6  6.2      58.0  5.8      58.2  5.8
 template <int KIND, bool GF32, bool OF32, bool STREAM, int TPR, int V>
 __global__ __launch_bounds__(TPR == 64 && V > 2 ? 512 : 1024) void norm_bwd_kernel(const NormBwdArgs a)
 {
