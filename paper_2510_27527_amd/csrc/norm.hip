@@ -103,6 +103,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_fwd_kernel(const N
         }
     };
     int64_t row = (int64_t)blockIdx.x * ROWS + __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);     // the same in all lanes of a wave
+    int turn = 0;              // half of red that the next sum takes: every sum the other one, of whichever row
     if constexpr (LDS) {
         if (row < a.N) load(row);
         const int slot = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
@@ -129,7 +130,8 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_fwd_kernel(const N
             for (int v = 0; v < V; ++v)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum += x[v][i];
-            row_sum2<TPR>(sum, none, red[0]);
+            row_sum2<TPR>(sum, none, red[turn]);
+            turn ^= 1;
             mean = sum * inv_d;
         }
         if (a.ckpt.codes) {
@@ -144,7 +146,8 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_fwd_kernel(const N
                 x[v][i] -= mean;
                 if ((t + v * TPR) * kChunk + i < a.D) sq = fmaf(x[v][i], x[v][i], sq);
             }
-        row_sum2<TPR>(sq, none, red[1]);
+        row_sum2<TPR>(sq, none, red[turn]);
+        turn ^= 1;
         const float rstd = 1.0f / sqrtf(sq * inv_d + a.eps);
         if (a.stats && t == 0) a.stats[row] = float2_t{mean, rstd};
 #pragma unroll
@@ -174,6 +177,7 @@ __global__ __launch_bounds__(1024) void norm_fwd_long_kernel(const NormFwdArgs a
     __shared__ float2_t red[2][TPR / 64];
     const int t = threadIdx.x;
     const float inv_d = 1.0f / (float)a.D;
+    int turn = 0;
     for (int64_t row = blockIdx.x; row < a.N; row += gridDim.x) {
         float x[8];
         float none = 0.0f, mean = 0.0f, sq = 0.0f;
@@ -184,7 +188,8 @@ __global__ __launch_bounds__(1024) void norm_fwd_long_kernel(const NormFwdArgs a
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum += x[i];
             }
-            row_sum2<TPR>(sum, none, red[0]);
+            row_sum2<TPR>(sum, none, red[turn]);
+            turn ^= 1;
             mean = sum * inv_d;
         }
         for (int col = t * kChunk; col < a.D; col += TPR * kChunk) {
@@ -195,7 +200,8 @@ __global__ __launch_bounds__(1024) void norm_fwd_long_kernel(const NormFwdArgs a
                 if (col + i < a.D) sq = fmaf(d, d, sq);
             }
         }
-        row_sum2<TPR>(sq, none, red[1]);
+        row_sum2<TPR>(sq, none, red[turn]);
+        turn ^= 1;
         const float rstd = 1.0f / sqrtf(sq * inv_d + a.eps);
         if (a.stats && t == 0) a.stats[row] = float2_t{mean, rstd};
         for (int base = 0; base < a.D; base += TPR * kChunk) {     // all lanes of a group stay for the checkpoint

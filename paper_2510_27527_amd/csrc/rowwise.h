@@ -275,8 +275,8 @@ __device__ __forceinline__ float wave_sum(float v)
 }
 
 // Sums of two numbers over the TPR threads that hold a row; every one of them gets both.  red: two floats per wave of the workgroup, all of whose
-// threads call this together where TPR > 64; a workgroup that sums again passes the other half of a doubled array, so that no barrier is
-// needed before the next sum.
+// threads call this together where TPR > 64.  No barrier follows the last read of red: a workgroup's next sum, of the same row or of the next, has to
+// take the other half of a doubled array (the one after it may take this half again, since the barrier between lies behind all reads of it).
 template <int TPR>
 __device__ __forceinline__ void row_sum2(float &a, float &b, float2_t *red)
 {

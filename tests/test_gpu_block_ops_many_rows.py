@@ -1,0 +1,39 @@
+"""GPU tests of the operators around the quantized linears where a workgroup takes more than one row, against the same rows in calls in
+which it takes one, and those against the definitions in 64 bits (block_ops_reference.py)."""
+import pytest
+import torch
+
+import block_ops_reference as ref
+from test_gpu_block_ops import BF, EPS, tj  # noqa: F401  (the fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+# Rows that a workgroup of several waves holds, and rows that it reads again: whole and ragged, each beyond the workgroups of a launch (1024, 512, 256
+# and 8192 of them), so that a workgroup sums one row after another.
+@pytest.mark.parametrize("N,D", [(2600, 2056), (2500, 4096), (1300, 4104), (1200, 8191), (700, 8200), (900, 16384), (16500, 3), (8300, 16390)])
+@pytest.mark.parametrize("layer", [True, False])
+def test_norm_of_more_rows_than_workgroups(tj, N, D, layer):  # noqa: F811
+    B = tj.binding
+    kind = B.NORM_LAYER if layer else B.NORM_RMS
+    g = torch.Generator(device="cuda").manual_seed(D)
+    # rows of very different size: another row's sum in the place of a row's own would show at once
+    x = (torch.randn(N, D, generator=g, device="cuda") * torch.exp2(torch.randint(-8, 9, (N, 1), generator=g, device="cuda").float())).to(BF)
+    gamma = 1 + 0.1 * torch.randn(D, generator=g, device="cuda")
+    stats, kept = tj.alloc_stats(N), tj.alloc_ckpt8(N, D)
+    print("norm", N, D, layer, flush=True)
+    y = tj.norm_fwd(x, gamma, eps=EPS, norm=kind, stats=stats, ckpt=kept)
+    alone = tj.norm_fwd(x, gamma, eps=EPS, norm=kind)
+    assert torch.equal(alone, y)
+    step = 200
+    for at in range(0, N, step):
+        rows = slice(at, min(at + step, N))
+        n = rows.stop - at
+        s, k = tj.alloc_stats(n), tj.alloc_ckpt8(n, D)
+        assert torch.equal(tj.norm_fwd(x[rows], gamma, eps=EPS, norm=kind, stats=s, ckpt=k), y[rows]), at
+        assert torch.equal(s, stats[rows]) and torch.equal(k.codes, kept.codes[rows]) and torch.equal(k.exps, kept.exps[rows]), at
+    last = slice(N - 20, N)
+    (wy, wm, wr), (ey, em, er) = ref.norm_fwd(x[last], gamma, None, EPS, layer, BF)
+    ref.within(y[last], wy, ey, "y")
+    ref.within(stats[last, :1], wm, em + 1e-38, "mean")
+    ref.within(stats[last, 1:], wr, er, "rstd")
