@@ -151,7 +151,7 @@ int nvfp4_act_fwd(const void *H, int src_kind, int64_t ldh, int64_t N, int64_t F
 {
     if (act != NVFP4_ACT_SWIGLU && act != NVFP4_ACT_GELU) return NVFP4_ERR_ENUM;
     const int64_t parts = act == NVFP4_ACT_SWIGLU ? 2 : 1;
-    int rc = F > kMaxCols ? NVFP4_ERR_SHAPE : check_sizes(N, parts * F);
+    int rc = F < 0 || F > kMaxCols ? NVFP4_ERR_SHAPE : check_sizes(N, parts * F);      // within these, 2 F does not overflow
     if (rc) return rc;
     RowSrc h;
     RowDst a;
@@ -172,7 +172,7 @@ int nvfp4_act_bwd(const void *dA, int da_kind, int64_t ldda, const void *H, int 
 {
     if (act != NVFP4_ACT_SWIGLU && act != NVFP4_ACT_GELU) return NVFP4_ERR_ENUM;
     const int64_t parts = act == NVFP4_ACT_SWIGLU ? 2 : 1;
-    int rc = F > kMaxCols ? NVFP4_ERR_SHAPE : check_sizes(N, parts * F);
+    int rc = F < 0 || F > kMaxCols ? NVFP4_ERR_SHAPE : check_sizes(N, parts * F);      // within these, 2 F does not overflow
     if (rc) return rc;
     RowSrc da, h;
     RowDst dh;
