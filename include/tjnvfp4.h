@@ -331,7 +331,8 @@ int nvfp4_norm_fwd(const void *X, int src_kind, int64_t ldx, int64_t N, int64_t 
  * Gradients of nvfp4_norm_fwd from dY (NVFP4_SRC_BF16 or NVFP4_SRC_F32), X (as it was, or its 8-bit checkpoint) and the forward call's stats.
  * With h = (x - mu) r and g = dY gamma: dX = r (g - mean(g) - h mean(g h)) (NVFP4_NORM_RMS: without mean(g)), dgamma = sum over rows of dY h,
  * dbeta = sum over rows of dY (binary32 [D], 16-byte aligned, each optional; zeros for N = 0).  The sums over rows are taken
- * in an order that depends on N and D alone: the same inputs give the same bits.  ws: nvfp4_norm_workspace_bytes(N, D) bytes where dgamma or dbeta is wanted.
+ * in an order that depends on N and D alone: the same inputs give the same bits.  ws: nvfp4_norm_workspace_bytes(N, D) bytes where dgamma or dbeta is wanted
+ * (8 D min(N, 256) or a little more, none for one row: a workspace for the most rows and the widest does for every other call).
  * Errors: NULL, SHAPE, ENUM, ALIGN, MISMATCH (checkpoint of another shape), WORKSPACE.
  */
 int nvfp4_norm_bwd(const void *dY, int dy_kind, int64_t lddy, const void *X, int src_kind, int64_t ldx, const float *stats,

@@ -531,10 +531,12 @@ hipError_t launch_norm_fwd(const RowSrc &x, int64_t N, int64_t D, const float *g
 // columns of a row of partial sums: whole quads, on 16 bytes (D = 1023: 8.9 us of the kernel that adds them without)
 static int64_t padded(int64_t D) { return (D + 3) / 4 * 4; }
 
+// for the most workgroups that N rows have at any width: their number itself falls where a workgroup takes another row (D = 1024: 256 of one row at
+// N = 256, 129 of two at N = 257), and what a large call needs has to do for a small one
 size_t norm_bwd_workspace_bytes(int64_t N, int64_t D)
 {
-    const int64_t G = bwd_blocks(N, D);
-    return G > 1 ? (size_t)(G * 2 * padded(D)) * sizeof(float) : 0;
+    const int64_t most = N < kMostPartials ? N : kMostPartials;
+    return most > 1 ? (size_t)(most * 2 * padded(D)) * sizeof(float) : 0;
 }
 
 hipError_t launch_norm_bwd(const RowSrc &dy, const RowSrc &x, const float *stats, const float *gamma, int64_t N, int64_t D, int layer,
