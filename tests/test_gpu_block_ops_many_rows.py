@@ -37,3 +37,24 @@ def test_norm_of_more_rows_than_workgroups(tj, N, D, layer):  # noqa: F811
     ref.within(y[last], wy, ey, "y")
     ref.within(stats[last, :1], wm, em + 1e-38, "mean")
     ref.within(stats[last, 1:], wr, er, "rstd")
+
+
+# Widths of which no kernel has all columns, D * (1 / D) = 1 in binary32; and rows that end in the middle of what a workgroup takes at once
+@pytest.mark.parametrize("N,D", [(4, 9), (4, 100), (4, 520), (4, 1100), (4, 1600), (4, 3000), (4, 5000), (4, 9000), (4, 20000), (1025, 4096), (600, 8192), (300, 3000), (300, 1000)])
+def test_norm_backward_of_rows_far_from_zero(tj, N, D):  # noqa: F811
+    """Rows of one large power of two: the mean is exact, the deviation zero, and mean / deviation overflows.  No term of a gradient has it."""
+    B = tj.binding
+    import numpy as np
+    assert np.float32(D) * (np.float32(1) / np.float32(D)) == 1
+    g = torch.Generator(device="cuda").manual_seed(D)
+    x = torch.full((N, D), 2.0 ** 110, device="cuda")
+    dy = torch.randn(N, D, generator=g, device="cuda")
+    gamma = 1 + 0.1 * torch.randn(D, generator=g, device="cuda")
+    stats = tj.alloc_stats(N)
+    y = tj.norm_fwd(x, gamma, eps=1e-12, out_dtype=B.OUT_F32, stats=stats)
+    assert not y.any() and (stats[:, 0] == 2.0 ** 110).all() and ((stats[:, 1] - 1e6).abs() <= 1).all()
+    for src in (x, x.to(BF), tj.ckpt8_save(x)):
+        got = tj.norm_bwd(dy, src, stats, gamma, out_dtype=B.OUT_F32)
+        want, bound = ref.norm_bwd(dy, x, stats, gamma, True, torch.float32)
+        for a, w, b, what in zip(got, want, bound, ("dx", "dgamma", "dbeta")):
+            ref.within(a, w, b, what)
