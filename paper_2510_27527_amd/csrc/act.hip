@@ -184,8 +184,9 @@ __global__ __launch_bounds__(kThreads) void act_bwd_kernel(const ActArgs a)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const Sigmoid s = sigmoid(-kLog2e * x[i]);
-                const float du = da[i] * x[i] * s.pos;
-                x[i] = da[i] * u[i] * s.pos * fmaf(x[i], s.neg, 1.0f);
+                // the bounded factors first: da x and da u may overflow where s(x) makes the product small or zero
+                const float du = x[i] * s.pos * da[i];
+                x[i] = s.pos * fmaf(x[i], s.neg, 1.0f) * u[i] * da[i];
                 u[i] = du;
             }
             store8<OF32, false>(a.out.p, a.out.ld, row, col, F, x);

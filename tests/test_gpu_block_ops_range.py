@@ -1,5 +1,5 @@
-"""GPU tests of the operators around the quantized linears where a workgroup takes more than one row, against the same rows in calls in
-which it takes one, and those against the definitions in 64 bits (block_ops_reference.py)."""
+"""GPU tests of the operators around the quantized linears at the ends of their ranges, against their definitions in 64 bits
+(block_ops_reference.py): more rows than workgroups, values whose products in another order would overflow, wide outputs."""
 import pytest
 import torch
 
@@ -58,3 +58,20 @@ def test_norm_backward_of_rows_far_from_zero(tj, N, D):  # noqa: F811
         want, bound = ref.norm_bwd(dy, x, stats, gamma, True, torch.float32)
         for a, w, b, what in zip(got, want, bound, ("dx", "dgamma", "dbeta")):
             ref.within(a, w, b, what)
+
+
+@pytest.mark.parametrize("size", [1.0, 1e9, 1e30])
+@pytest.mark.parametrize("t", [BF, torch.float32])
+def test_nonlinearity_backward_of_large_gradients(tj, t, size):  # noqa: F811
+    """Gates of any size with large gradients and up values: wherever a gradient is a binary32 number it comes out, whatever its factors' other products are."""
+    B = tj.binding
+    gates = torch.tensor([-3e38, -1e30, -1e13, -300.0, -100.0, -50.0, -17.0, -1.0, 0.0, 1.0, 17.0, 300.0, 1e6])
+    ups = torch.tensor([-1e9, -1e5, 1.0, 1e12])
+    g, u = (v.flatten() for v in torch.meshgrid(gates, ups, indexing="ij"))
+    h = torch.cat((g, u))[None].to(t).cuda()
+    da = torch.full((1, g.numel()), size, device="cuda")
+    for act, x in ((B.ACT_SWIGLU, h), (B.ACT_GELU, h[:, :g.numel()].contiguous())):
+        want, bound = ref.act_bwd(da, x, act == B.ACT_SWIGLU, torch.float32)
+        got = tj.act_bwd(da, x, act, B.OUT_F32)
+        fits = (want.abs() < 3e38) & torch.isfinite(want)      # in 64 bits the cube of GELU's argument overflows far out
+        ref.within(got.cpu()[fits], want[fits], bound[fits], "dh")
