@@ -75,3 +75,12 @@ def test_nonlinearity_backward_of_large_gradients(tj, t, size):  # noqa: F811
         got = tj.act_bwd(da, x, act, B.OUT_F32)
         fits = (want.abs() < 3e38) & torch.isfinite(want)      # in 64 bits the cube of GELU's argument overflows far out
         ref.within(got.cpu()[fits], want[fits], bound[fits], "dh")
+
+
+def test_the_stream_of_a_call(tj):  # noqa: F811
+    """The one that is current, on the default stream and beside it."""
+    assert tj.binding._stream() == torch.cuda.current_stream().cuda_stream
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        assert tj.binding._stream() == side.cuda_stream != 0
+    assert tj.binding._stream() == torch.cuda.current_stream().cuda_stream
