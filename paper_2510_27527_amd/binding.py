@@ -552,6 +552,9 @@ def outctl_bwd(dY, Xq: NVFP4Tensor, Wq: NVFP4Tensor, X_hp, W_hp, seed: int, laye
 
 
 # ---- operators around the linears: norms, nonlinearities, 8-bit checkpoints, the linear of single tokens ----
+#
+# They are enqueued on the current device's current stream, and every tensor has to be on that device (`dev` below): a kernel of
+# another device might not reach it.
 
 @dataclass
 class Ckpt8:
@@ -583,42 +586,42 @@ def alloc_stats(N: int, device="cuda") -> torch.Tensor:
 _KINDS = {torch.bfloat16: SRC_BF16, torch.float32: SRC_F32}
 
 
-def _rows(t: torch.Tensor, what: str):
+def _rows(t: torch.Tensor, what: str, dev: int):
     """(kind, row stride, rows, elements of a row) of a bf16 or float32 matrix whose rows are contiguous; the rows may be any distance apart."""
     kind = _KINDS.get(t.dtype)
     shape = t.shape
-    assert kind is not None and len(shape) == 2 and t.is_cuda, what + ": bf16 or float32, 2-D, on the GPU"
+    assert kind is not None and len(shape) == 2 and t.get_device() == dev, what + ": bf16 or float32, 2-D, on the current device"
     rows, n = shape
     s0, s1 = t.stride()
     assert s1 == 1 or n <= 1, what + ": rows of contiguous elements"
     return kind, s0 if rows > 1 else n, rows, n
 
 
-def _out_rows(t: Optional[torch.Tensor], rows: int, n: int, out_dtype: int, like: torch.Tensor, what: str):
+def _out_rows(t: Optional[torch.Tensor], rows: int, n: int, out_dtype: int, like: torch.Tensor, what: str, dev: int):
     """The output matrix, allocated on like's device where none is given, and its row stride."""
     if t is None:
         dtype = torch.bfloat16 if out_dtype == OUT_BF16 else torch.float32
         if dtype == like.dtype:              # 0.3 us of the host's less
             return like.new_empty((rows, n)), n
         return torch.empty((rows, n), dtype=dtype, device=like.device), n
-    kind, ld, r, c = _rows(t, what)
+    kind, ld, r, c = _rows(t, what, dev)
     assert r == rows and c == n and kind == (SRC_BF16 if out_dtype == OUT_BF16 else SRC_F32), what
     return t, ld
 
 
-def _param(t: Optional[torch.Tensor], D: int, what: str):
-    assert t is None or (t.dtype == torch.float32 and t.dim() == 1 and t.numel() == D and t.is_contiguous() and t.is_cuda), what + ": float32 [D]"
+def _param(t: Optional[torch.Tensor], D: int, what: str, dev: int):
+    assert t is None or (t.dtype == torch.float32 and t.dim() == 1 and t.numel() == D and t.is_contiguous() and t.get_device() == dev), what + ": float32 [D], on the current device"
     return _ptr(t)
 
 
-def _check_ckpt(c: Ckpt8, rows: int, K: int):
+def _check_ckpt(c: Ckpt8, rows: int, K: int, dev: int):
     assert c.rows == rows and c.K == K, "checkpoint of another shape"
     for t, shape in ((c.codes, (rows, K)), (c.exps, (rows, -(-K // CKPT_GROUP)))):
-        assert t.dtype == torch.uint8 and tuple(t.shape) == shape and t.is_contiguous() and t.is_cuda, "checkpoint buffers"
+        assert t.dtype == torch.uint8 and tuple(t.shape) == shape and t.is_contiguous() and t.get_device() == dev, "checkpoint buffers, on the current device"
 
 
-def _check_stats(t: torch.Tensor, N: int):
-    assert t.dtype == torch.float32 and tuple(t.shape) == (N, 2) and t.is_contiguous() and t.is_cuda, "stats: float32 [N, 2]"
+def _check_stats(t: torch.Tensor, N: int, dev: int):
+    assert t.dtype == torch.float32 and tuple(t.shape) == (N, 2) and t.is_contiguous() and t.get_device() == dev, "stats: float32 [N, 2], on the current device"
 
 
 def norm_fwd(X: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None, *, eps: float = 1e-5,
@@ -626,16 +629,17 @@ def norm_fwd(X: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Option
              ckpt: Optional[Ckpt8] = None) -> torch.Tensor:
     """nvfp4_norm_fwd: layer norm (NORM_LAYER) or RMS norm (NORM_RMS) of every row of X.  For training pass stats (alloc_stats) and, to keep
     the input in 8 bits, ckpt (alloc_ckpt8); both are filled."""
-    kind, ldx, N, D = _rows(X, "X")
-    Y, ldy = _out_rows(Y, N, D, out_dtype, X, "Y")
+    dev = _current_device()
+    kind, ldx, N, D = _rows(X, "X", dev)
+    Y, ldy = _out_rows(Y, N, D, out_dtype, X, "Y", dev)
     cs = None
     if ckpt is not None:
-        _check_ckpt(ckpt, N, D)
+        _check_ckpt(ckpt, N, D, dev)
         cs = C.byref(ckpt.c_struct())
     if stats is not None:
-        _check_stats(stats, N)
-    _check(lib().nvfp4_norm_fwd(_ptr(X), kind, ldx, N, D, _param(gamma, D, "gamma"), _param(beta, D, "beta"), eps, norm, _ptr(Y), out_dtype,
-                                ldy, _ptr(stats), cs, _stream()), "nvfp4_norm_fwd")
+        _check_stats(stats, N, dev)
+    _check(lib().nvfp4_norm_fwd(_ptr(X), kind, ldx, N, D, _param(gamma, D, "gamma", dev), _param(beta, D, "beta", dev), eps, norm, _ptr(Y), out_dtype,
+                                ldy, _ptr(stats), cs, _raw_stream(dev)), "nvfp4_norm_fwd")
     return Y
 
 
@@ -644,83 +648,92 @@ def norm_bwd(dY: torch.Tensor, X, stats: torch.Tensor, gamma: Optional[torch.Ten
              dbeta: Optional[torch.Tensor] = None, params: bool = True, ws: Optional[torch.Tensor] = None):
     """nvfp4_norm_bwd: (dX, dgamma, dbeta); X is the forward call's input or its Ckpt8.  params=False: dX alone; RMS norm has no dbeta
     unless one is passed."""
-    dkind, lddy, N, D = _rows(dY, "dY")
+    dev = _current_device()
+    dkind, lddy, N, D = _rows(dY, "dY", dev)
     if isinstance(X, Ckpt8):
-        _check_ckpt(X, N, D)
+        _check_ckpt(X, N, D, dev)
         kind, ldx, src = SRC_CKPT8, 0, C.byref(X.c_struct())
     else:
-        kind, ldx, *shape = _rows(X, "X")
+        kind, ldx, *shape = _rows(X, "X", dev)
         assert shape == [N, D], "X: the shape of dY"
         src = _ptr(X)
-    _check_stats(stats, N)
-    dX, lddx = _out_rows(dX, N, D, out_dtype, dY, "dX")
+    _check_stats(stats, N, dev)
+    dX, lddx = _out_rows(dX, N, D, out_dtype, dY, "dX", dev)
     if params:
         dgamma = stats.new_empty(D) if dgamma is None else dgamma
         if dbeta is None and norm == NORM_LAYER:
             dbeta = stats.new_empty(D)
         if ws is None:
             ws = alloc_workspace(lib().nvfp4_norm_workspace_bytes(N, D), dY.device)
+        else:
+            assert ws.get_device() == dev, "ws: on the current device"
     else:
         dgamma = dbeta = None
-    _check(lib().nvfp4_norm_bwd(_ptr(dY), dkind, lddy, src, kind, ldx, _ptr(stats), _param(gamma, D, "gamma"), N, D, norm, _ptr(dX), out_dtype,
-                                lddx, _param(dgamma, D, "dgamma"), _param(dbeta, D, "dbeta"), _ptr(ws), 0 if ws is None else ws.numel(),
-                                _stream()), "nvfp4_norm_bwd")
+    _check(lib().nvfp4_norm_bwd(_ptr(dY), dkind, lddy, src, kind, ldx, _ptr(stats), _param(gamma, D, "gamma", dev), N, D, norm, _ptr(dX), out_dtype,
+                                lddx, _param(dgamma, D, "dgamma", dev), _param(dbeta, D, "dbeta", dev), _ptr(ws), 0 if ws is None else ws.numel(),
+                                _raw_stream(dev)), "nvfp4_norm_bwd")
     return dX, dgamma, dbeta
 
 
 def act_fwd(H: torch.Tensor, act: int = ACT_SWIGLU, out_dtype: int = OUT_BF16, *, A: Optional[torch.Tensor] = None,
             ckpt: Optional[Ckpt8] = None) -> torch.Tensor:
     """nvfp4_act_fwd: SwiGLU of H [N, 2F] (gates, then up values) or GELU (tanh form) of H [N, F]; ckpt (alloc_act_ckpt8) receives H in 8 bits."""
-    kind, ldh, N, F = _rows(H, "H")
+    dev = _current_device()
+    kind, ldh, N, F = _rows(H, "H", dev)
     if act == ACT_SWIGLU:
         assert F % 2 == 0, "H: gates and up values"
         F //= 2
-    A, lda = _out_rows(A, N, F, out_dtype, H, "A")
+    A, lda = _out_rows(A, N, F, out_dtype, H, "A", dev)
     cs = None
     if ckpt is not None:
-        _check_ckpt(ckpt, 2 * N if act == ACT_SWIGLU else N, F)
+        _check_ckpt(ckpt, 2 * N if act == ACT_SWIGLU else N, F, dev)
         cs = C.byref(ckpt.c_struct())
-    _check(lib().nvfp4_act_fwd(_ptr(H), kind, ldh, N, F, act, _ptr(A), out_dtype, lda, cs, _stream()), "nvfp4_act_fwd")
+    _check(lib().nvfp4_act_fwd(_ptr(H), kind, ldh, N, F, act, _ptr(A), out_dtype, lda, cs, _raw_stream(dev)), "nvfp4_act_fwd")
     return A
 
 
 def act_bwd(dA: torch.Tensor, H, act: int = ACT_SWIGLU, out_dtype: int = OUT_BF16, *, dH: Optional[torch.Tensor] = None) -> torch.Tensor:
     """nvfp4_act_bwd: dH from dA and the forward call's input or its Ckpt8."""
-    dkind, ldda, N, F = _rows(dA, "dA")
+    dev = _current_device()
+    dkind, ldda, N, F = _rows(dA, "dA", dev)
     parts = 2 if act == ACT_SWIGLU else 1
     if isinstance(H, Ckpt8):
-        _check_ckpt(H, parts * N, F)
+        _check_ckpt(H, parts * N, F, dev)
         kind, ldh, src = SRC_CKPT8, 0, C.byref(H.c_struct())
     else:
-        kind, ldh, *shape = _rows(H, "H")
+        kind, ldh, *shape = _rows(H, "H", dev)
         assert shape == [N, parts * F], "H"
         src = _ptr(H)
-    dH, lddh = _out_rows(dH, N, parts * F, out_dtype, dA, "dH")
-    _check(lib().nvfp4_act_bwd(_ptr(dA), dkind, ldda, src, kind, ldh, N, F, act, _ptr(dH), out_dtype, lddh, _stream()), "nvfp4_act_bwd")
+    dH, lddh = _out_rows(dH, N, parts * F, out_dtype, dA, "dH", dev)
+    _check(lib().nvfp4_act_bwd(_ptr(dA), dkind, ldda, src, kind, ldh, N, F, act, _ptr(dH), out_dtype, lddh, _raw_stream(dev)), "nvfp4_act_bwd")
     return dH
 
 
 def ckpt8_save(X: torch.Tensor, out: Optional[Ckpt8] = None) -> Ckpt8:
     """nvfp4_ckpt8_save: an activation [N, D] in 8 bits."""
-    kind, ldx, N, D = _rows(X, "X")
+    dev = _current_device()
+    kind, ldx, N, D = _rows(X, "X", dev)
     out = alloc_ckpt8(N, D, X.device) if out is None else out
-    _check_ckpt(out, N, D)
-    _check(lib().nvfp4_ckpt8_save(_ptr(X), kind, ldx, N, D, C.byref(out.c_struct()), _stream()), "nvfp4_ckpt8_save")
+    _check_ckpt(out, N, D, dev)
+    _check(lib().nvfp4_ckpt8_save(_ptr(X), kind, ldx, N, D, C.byref(out.c_struct()), _raw_stream(dev)), "nvfp4_ckpt8_save")
     return out
 
 
 def ckpt8_load(src: Ckpt8, out_dtype: int = OUT_BF16, *, Y: Optional[torch.Tensor] = None) -> torch.Tensor:
     """nvfp4_ckpt8_load: the activation that a checkpoint holds."""
-    _check_ckpt(src, src.rows, src.K)
-    Y, ldy = _out_rows(Y, src.rows, src.K, out_dtype, src.codes, "Y")
-    _check(lib().nvfp4_ckpt8_load(C.byref(src.c_struct()), _ptr(Y), out_dtype, ldy, _stream()), "nvfp4_ckpt8_load")
+    dev = _current_device()
+    _check_ckpt(src, src.rows, src.K, dev)
+    Y, ldy = _out_rows(Y, src.rows, src.K, out_dtype, src.codes, "Y", dev)
+    _check(lib().nvfp4_ckpt8_load(C.byref(src.c_struct()), _ptr(Y), out_dtype, ldy, _raw_stream(dev)), "nvfp4_ckpt8_load")
     return Y
 
 
 def gemv(X: torch.Tensor, W: NVFP4Tensor, out_dtype: int = OUT_BF16, *, Y: Optional[torch.Tensor] = None) -> torch.Tensor:
     """nvfp4_gemv: Y = X W^T for the bf16 activations of a few tokens on packed weights (linear_fwd's Wq)."""
-    kind, ldx, M, K = _rows(X, "X")
+    dev = _current_device()
+    kind, ldx, M, K = _rows(X, "X", dev)
     assert kind == SRC_BF16 and K == W.K, "X: bf16 [M, W.K]"
-    Y, ldy = _out_rows(Y, M, W.rows, out_dtype, X, "Y")
-    _check(lib().nvfp4_gemv(_ptr(X), ldx, M, C.byref(W.c_struct()), _ptr(Y), out_dtype, ldy, _stream()), "nvfp4_gemv")
+    assert W.codes.get_device() == W.scales.get_device() == W.gscale.get_device() == dev, "W: on the current device"
+    Y, ldy = _out_rows(Y, M, W.rows, out_dtype, X, "Y", dev)
+    _check(lib().nvfp4_gemv(_ptr(X), ldx, M, C.byref(W.c_struct()), _ptr(Y), out_dtype, ldy, _raw_stream(dev)), "nvfp4_gemv")
     return Y

@@ -84,3 +84,48 @@ def test_the_stream_of_a_call(tj):  # noqa: F811
     with torch.cuda.stream(side):
         assert tj.binding._stream() == side.cuda_stream != 0
     assert tj.binding._stream() == torch.cuda.current_stream().cuda_stream
+
+
+def calls(tj, t):  # noqa: F811
+    """Every call on the tensors of `t`, by what it reads and writes."""
+    B = tj.binding
+    return {
+        "x y gamma beta stats kept": lambda: tj.norm_fwd(t["x"], t["gamma"], t["beta"], Y=t["y"], stats=t["stats"], ckpt=t["kept"]),
+        "y x gamma stats dx dg db ws": lambda: tj.norm_bwd(t["y"], t["x"], t["stats"], t["gamma"], dX=t["dx"], dgamma=t["dg"], dbeta=t["db"], ws=t["ws"]),
+        "y kept stats": lambda: tj.norm_bwd(t["y"], t["kept"], t["stats"]),
+        "x y kept": lambda: tj.act_fwd(t["x"], B.ACT_GELU, A=t["y"], ckpt=t["kept"]),
+        "y x dx": lambda: tj.act_bwd(t["y"], t["x"], B.ACT_GELU, dH=t["dx"]),
+        "y kept dx": lambda: tj.act_bwd(t["y"], t["kept"], B.ACT_GELU, dH=t["dx"]),
+        "x kept ": lambda: tj.ckpt8_save(t["x"], t["kept"]),
+        "kept y": lambda: tj.ckpt8_load(t["kept"], Y=t["y"]),
+        "x W z": lambda: tj.gemv(t["x"], t["W"], Y=t["z"]),
+    }
+
+
+def test_refuses_tensors_of_another_device(tj, monkeypatch):  # noqa: F811
+    """Every tensor of every call has to be where the call is enqueued; one in the host's memory stands for those that are not."""
+    B = tj.binding
+    N, D, Co = 6, 256, 40
+    e = lambda *s, dtype=BF: torch.zeros(s, dtype=dtype, device="cuda")
+    t = dict(x=e(N, D), y=e(N, D), dx=e(N, D), z=e(N, Co), gamma=e(D, dtype=torch.float32), beta=e(D, dtype=torch.float32), dg=e(D, dtype=torch.float32), db=e(D, dtype=torch.float32),
+             stats=tj.alloc_stats(N), kept=tj.alloc_ckpt8(N, D), ws=tj.alloc_workspace(1 << 20), W=tj.alloc_nvfp4(Co, D))
+    t["kept"].codes.zero_(), t["kept"].exps.fill_(127), t["W"].codes.zero_(), t["W"].scales.zero_(), t["W"].gscale.zero_(), t["stats"].zero_()
+    for call in calls(tj, t).values():
+        call()
+    torch.cuda.synchronize()
+    for names in calls(tj, t):
+        for name in names.split():
+            v = t[name]
+            if isinstance(v, torch.Tensor):
+                moved = [v.cpu()]
+            else:
+                fields = [f for f in ("codes", "exps", "scales", "gscale") if hasattr(v, f)]
+                moved = [type(v)(**{**vars(v), f: getattr(v, f).cpu()}) for f in fields]
+            for m in moved:
+                with pytest.raises(AssertionError, match="current device"):
+                    calls(tj, {**t, name: m})[names]()
+    elsewhere = B._current_device() + 1
+    monkeypatch.setattr(B, "_current_device", lambda: elsewhere)
+    for call in calls(tj, t).values():
+        with pytest.raises(AssertionError, match="current device"):
+            call()
