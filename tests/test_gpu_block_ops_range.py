@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import block_ops_reference as ref
-from test_gpu_block_ops import BF, EPS, tj  # noqa: F401  (the fixture)
+from test_gpu_block_ops import BF, EPS, operand, spread, tj, untouched  # noqa: F401  (tj: the fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -129,3 +129,65 @@ def test_refuses_tensors_of_another_device(tj, monkeypatch):  # noqa: F811
     for call in calls(tj, t).values():
         with pytest.raises(AssertionError, match="current device"):
             call()
+
+
+# Products where a lane takes four rows (one or two tokens; 8192, 16384 or 32768 outputs on by the length of the reduction) and where a workgroup takes two tiles of rows (more
+# tokens; 8177 outputs on), whole and ragged, with every number of waves that shares a reduction; and the borders below them.
+@pytest.mark.parametrize("block", [False, True])
+@pytest.mark.parametrize("C", [4096, 4097, 8176, 8177, 8192, 8193, 16387, 32771])
+def test_gemv_of_wide_outputs(tj, C, block):  # noqa: F811
+    B = tj.binding
+    outer = B.OUTER_BLOCK128 if block else B.OUTER_TENSOR
+    for K in (128, 384, 640, 1024, 1280, 2176) + (() if block else (16, 400, 2064)):
+        W = operand(tj, C, K, outer, C + K, exact=True)
+        w = ref.unpack(W.codes, W.scales, W.gscale, block).cuda().t().contiguous()
+        for M in (1, 2, 3, 16, 17, 33):
+            print("gemv", M, C, K, block, flush=True)
+            # small integers times weights of few bits: nothing is rounded, so every product is there exactly once
+            x = torch.randint(-3, 4, (M, K), generator=torch.Generator().manual_seed(M * K)).to(BF).cuda()
+            buf, y = spread(torch.zeros(M, C, device="cuda"), 3, 5)
+            tj.gemv(x, W, B.OUT_F32, Y=y)
+            want = x.double() @ w
+            assert torch.equal(y.double(), want) and untouched(buf, y)
+            assert torch.equal(tj.gemv(x, W), want.to(BF))
+
+
+@pytest.mark.parametrize("M", [1, 2, 3, 20])
+def test_gemv_of_long_reductions(tj, M):  # noqa: F811
+    """Reductions of every length modulo the waves that share one, a rest of 16 at the end among them."""
+    B = tj.binding
+    for C, K in ((70, 4112), (70, 8208), (8200, 4112), (33, 16400)):
+        W = operand(tj, C, K, B.OUTER_TENSOR, C + K, exact=True)
+        x = torch.randint(-3, 4, (M, K), generator=torch.Generator().manual_seed(K)).to(BF).cuda()
+        want = x.double() @ ref.unpack(W.codes, W.scales, W.gscale, False).cuda().t().contiguous()
+        print("gemv", M, C, K, flush=True)
+        assert torch.equal(tj.gemv(x, W, B.OUT_F32).double(), want)
+
+
+@pytest.mark.parametrize("parts", [1, 2])
+def test_more_rows_than_a_launch_has(tj, parts):  # noqa: F811
+    """Narrow rows by the million: a workgroup walks over several lots of them (beyond 65535 x 16 rows, twice that where a thread takes two)."""
+    B = tj.binding
+    act = B.ACT_SWIGLU if parts == 2 else B.ACT_GELU
+    N, F = 2 * 65535 * 16 + 1001, 8
+    g = torch.Generator(device="cuda").manual_seed(parts)
+    H = torch.randn(N, parts * F, generator=g, device="cuda").to(BF)
+    dA = torch.randn(N, F, generator=g, device="cuda").to(BF)
+    kept = tj.alloc_act_ckpt8(N, F, act)
+    A = tj.act_fwd(H, act, ckpt=kept)
+    dH, dH8 = tj.act_bwd(dA, H, act), tj.act_bwd(dA, kept, act)
+    saved = tj.ckpt8_save(H)
+    loaded = tj.ckpt8_load(saved)
+    for at in list(range(0, N, 100000)) + [N - 3]:
+        rows = slice(at, min(at + 100000, N))
+        n = rows.stop - at
+        h, da, both = H[rows], dA[rows], slice(at * parts, rows.stop * parts)
+        k = tj.alloc_act_ckpt8(n, F, act)
+        assert torch.equal(tj.act_fwd(h, act, ckpt=k), A[rows]), at
+        assert torch.equal(k.codes, kept.codes[both]) and torch.equal(k.exps, kept.exps[both]), at
+        assert torch.equal(tj.act_bwd(da, h, act), dH[rows]) and torch.equal(tj.act_bwd(da, k, act), dH8[rows]), at
+        s = tj.ckpt8_save(h)
+        assert torch.equal(s.codes, saved.codes[rows]) and torch.equal(s.exps, saved.exps[rows]) and torch.equal(tj.ckpt8_load(s), loaded[rows]), at
+    last = slice(N - 50, N)
+    ref.within(A[last], *ref.act_fwd(H[last], parts == 2, BF), "a")
+    ref.within(dH[last], *ref.act_bwd(dA[last], H[last], parts == 2, BF), "dh")
