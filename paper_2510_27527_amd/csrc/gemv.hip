@@ -357,20 +357,32 @@ template <int NT, int RT> void run_gemv(const GemvArgs &a, int outer, int most_w
     else gemv_kernel<NT, RT, false><<<grid, waves * 64, lds, st>>>(a);
 }
 
-// Tiles of 16 rows.  Up to one a CU: a workgroup each, whose eight waves split the reduction (85 KB of LDS).  From two a CU on a workgroup takes two,
-// which share the activations; where that is more than one workgroup a CU, and between one and two tiles a CU, four waves leave room for
-// several (more than one round of large workgroups is what costs most).  us by rows x waves of a workgroup, M x C x K:
-//                                16 x 8   16 x 4   32 x 8   32 x 4
-//   16 x 4096 x 4096, outer        7.3      7.8      8.9     10.1
-//   5 x 5003 x 2064                9.9      7.1      7.5      8.6
-//   16 x 8192 x 8192              19.6     17.4     16.1     18.8
-//   32 x 8192 x 8192              28.0     27.0     22.5     25.2      (32 rows: six waves, 127 KB of LDS, for eight)
-//   16 x 16384 x 16384            62.7     56.5     47.6     42.9
+// Tiles of 16 rows and how they are dealt, us out of memory by rows x waves of a workgroup (0.2 to 2 us less where the last-level cache has the weights):
+//   up to one a CU      a workgroup each, whose eight waves split the reduction (85 KB of LDS)
+//   up to two a CU      a workgroup takes two, which share the activations, and is still alone on its CU with eight waves (six for 32 tokens: 127 KB of LDS)
+//   up to three a CU    one each with four waves: three workgroups (two for 32 tokens) fit on a CU and all run at once
+//   more                two each with four waves
+//                                  M = 5                       M = 16                      M = 32
+//   outputs x reduction    16x4   32x8   32x4          16x4   32x8   32x4          16x4   32x6   32x4
+//    4112 x 2048            5.2    5.3    5.8           5.9    5.9    6.3           7.9    8.3    7.8
+//    5120 x 4096            8.7    8.0    8.9          10.0    9.3   10.3          14.4   13.0   13.2
+//    8000 x 2048            6.1    6.2    6.3           7.2    7.1    7.2           9.4    9.3    8.8
+//    8000 x 8192           14.8   13.8   15.8          17.1   15.7   18.6          25.8   21.7   24.6
+//    8208 x 4096            9.8   13.8   11.5          12.5   15.6   12.2          21.1   22.7   23.4
+//   12288 x 4096           10.8   14.7   12.7          13.7   17.2   14.5          22.6   24.6   25.2
+//   12304 x 4096           13.2   14.7   12.7          16.4   17.3   14.6          25.3   24.7   25.3
+//   16384 x 8192           25.1   25.4   22.5          33.6   29.0   25.9          47.3   40.6   45.7
+// (at its worst the rule gives 7.8 for 7.1: 4112 x 2816, 16 tokens.)  A reduction of few pieces has no work for the waves that two tiles would add: up to two
+// a CU, 5120 x 1024 4.3 / 4.5 (5 tokens, 16 / 32 rows), 4.8 / 4.8 (16), 6.2 / 5.8 (32); 5003 x 768 4.1 / 4.4 (3), 4.6 / 4.6 (16), 5.7 / 5.7 (32).  Three waves a workgroup leave two tiles of 32 tokens room for a second workgroup: 11264 x 768
+// 9.0 / 7.0.
 template <int NT> void run_gemv(const GemvArgs &a, int outer, hipStream_t st)
 {
     const int64_t tiles = (a.C + 15) / 16;
-    if (tiles < 512) run_gemv<NT, 1>(a, outer, tiles <= 256 ? 8 : 4, st);
-    else run_gemv<NT, 2>(a, outer, tiles > 512 ? 4 : NT == 1 ? 8 : 6, st);
+    const int pieces = (a.K + kPiece - 1) / kPiece;
+    if (tiles <= 256) run_gemv<NT, 1>(a, outer, 8, st);
+    else if (tiles <= 512 && pieces >= (NT == 1 ? 5 : 4)) run_gemv<NT, 2>(a, outer, NT == 1 ? 8 : 6, st);
+    else if (tiles <= 512 || (tiles <= 768 && (NT == 1 || pieces >= 4))) run_gemv<NT, 1>(a, outer, 4, st);
+    else run_gemv<NT, 2>(a, outer, 4, st);
 }
 
 template <int M, int LR, int R> void run_few(const GemvArgs &a, int outer, hipStream_t st)
