@@ -417,8 +417,13 @@ template <int M> void run_few(const GemvArgs &a, int outer, hipStream_t st)
 hipError_t launch_gemv(const void *X, int64_t ldx, int64_t M, const GemmOperand &W, int64_t K, const RowDst &y, hipStream_t st)
 {
     const GemvArgs a{static_cast<const uint16_t *>(X), ldx, M, W.codes, W.scales, W.gscale, W.rows, (int)K, y.p, y.ld, y.f32};
-    // us on 8192 x 8192, dot products / matrix instructions: one token 10.4 / 15.8, two 13.4 / 15.8, three 14.9 / 15.8, four 17.8 / 15.4;
-    // on 4096 x 4096 with outer blocks four tokens 8.0 / 6.9
+    // us out of memory, dot products / matrix instructions:
+    //                    1 token        2 tokens       3 tokens       4 tokens
+    //    1024 x 1024    2.5 /  3.6     2.9 /  3.6     3.3 /  3.6     3.9 /  3.7
+    //    4096 x 4096    4.7 /  6.1     5.9 /  6.2     7.1 /  6.2     8.4 /  6.2
+    //    8192 x 8192   10.4 / 13.4    12.9 / 13.4    16.6 / 13.7    18.7 / 13.5
+    //   16384 x 16384  30.4 / 37.2    37.5 / 36.2    47.1 / 36.7    57.3 / 37.1
+    // (1 x 128 outer blocks 0.1 to 5 us more on either side, the same order).  Three tokens gain 0.4 us at most by dot products, on weights of up to 2 MB, and are left to the others.
     if (M == 1) run_few<1>(a, W.outer, st);
     else if (M == 2) run_few<2>(a, W.outer, st);
     else if (M <= 16) run_gemv<1>(a, W.outer, st);
