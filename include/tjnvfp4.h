@@ -359,7 +359,8 @@ int nvfp4_ckpt8_load(const nvfp4_ckpt8 *src, void *Y, int out_dtype, int64_t ldy
 
 /*
  * Y [M x C] = X [M x K] * W^T for the few tokens of a decoding step: X bf16 as it is, W [C x K] an operand in either outer mode
- * (nvfp4_linear_fwd's Wq_ctx, or what nvfp4_quantize gives of axis 0).  The products are exact, the sums binary32.  Meant for M up to some
+ * (nvfp4_linear_fwd's Wq_ctx, or what nvfp4_quantize gives of axis 0).  The products are exact, the sums binary32; gscale of NVFP4_OUTER_TENSOR
+ * multiplies the sum (activations of 1e31 and more can overflow it before that).  Meant for M up to some
  * dozens (the weights are expanded once per 32 tokens); M <= 2^20, C <= 2^26, K <= 2^22.  No workspace: may be captured in a graph.
  * Errors: NULL, SHAPE, ENUM, ALIGN.
  */

@@ -7,7 +7,8 @@
 // Element by element but for the maxima of a checkpoint's groups, which the 16 lanes of a group exchange in registers.  Bound: HBM (a copy of
 // 1 GB reaches 5.1 TB/s here, one of 64 MB, which the last-level cache holds, 6.9); small calls: the launch.
 //
-// Figures: bf16 arrays, us and TB/s over the bytes that a call has to read and write.
+// Figures: bf16 arrays where nothing else stands, us of a kernel in a kernel trace and TB/s over the bytes that a call has to read and write; calls on three sets of arrays in turn
+// (the comparisons of two forms below: on one set).
 #include <type_traits>
 
 #include "rowwise.h"
@@ -116,8 +117,8 @@ __device__ __forceinline__ Raw<KIND> load8_or_0(const RowSrc &s, int64_t row, in
 template <int KIND> struct Pair { Raw<KIND> a, b; };
 template <int KIND, int GKIND> struct Triple { Raw<KIND> a, b; Raw<GKIND> da; };
 
-// SwiGLU with a checkpoint 16384 x 4096 91 us, 5.9 TB/s (alone in its arrays 80.5, 6.7), without 62, 6.5; GELU with a checkpoint 4099 x 2752 11.5, 4.9,
-// 8192 x 8192 52, 6.4; 64 x 8192 3.1
+// SwiGLU with a checkpoint 16384 x 4096 90 us, 6.0 TB/s, without 66, 6.1; GELU with a checkpoint 4099 x 2752 11.3, 5.0, 8192 x 8192 58, 5.8; 64 x 8192 3.3.
+// Binary32: SwiGLU with a checkpoint 8192 x 4096 89, 5.3, GELU 8192 x 8192 115, 5.3.
 template <int KIND, bool OF32, int SIZE, int ACT>
 __global__ __launch_bounds__(kThreads) void act_fwd_kernel(const ActArgs a)
 {
@@ -150,7 +151,8 @@ __global__ __launch_bounds__(kThreads) void act_fwd_kernel(const ActArgs a)
     });
 }
 
-// SwiGLU 16384 x 4096 from a checkpoint 81 us, 6.6 TB/s, from H 107, 6.3; GELU from a checkpoint 4099 x 2752 11.8, 4.8, 8192 x 8192 56, 6.0
+// SwiGLU 16384 x 4096 from a checkpoint 89 us, 6.1 TB/s, from H 114, 5.9; GELU from a checkpoint 4099 x 2752 11.6, 4.9, 8192 x 8192 60, 5.6, from the input 69, 5.9.
+// Binary32 from a checkpoint: SwiGLU 8192 x 4096 91, 5.2, GELU 8192 x 8192 117, 5.2.
 template <int KIND, bool GF32, bool OF32, int SIZE, int ACT>
 __global__ __launch_bounds__(kThreads) void act_bwd_kernel(const ActArgs a)
 {
@@ -199,7 +201,7 @@ __global__ __launch_bounds__(kThreads) void act_bwd_kernel(const ActArgs a)
     });
 }
 
-// 8192 x 8192 35 us, 5.8 TB/s
+// 8192 x 8192 35 us, 5.8 TB/s; binary32 60, 5.6
 template <int KIND, int SIZE>
 __global__ __launch_bounds__(kThreads) void ckpt8_save_kernel(const CopyArgs a)
 {
@@ -212,7 +214,7 @@ __global__ __launch_bounds__(kThreads) void ckpt8_save_kernel(const CopyArgs a)
     });
 }
 
-// 8192 x 8192 31 us, 6.5 TB/s right after it was saved
+// 8192 x 8192 37 us, 5.5 TB/s, right after it was saved 31, 6.5; to binary32 79, 4.2
 template <bool OF32, int SIZE>
 __global__ __launch_bounds__(kThreads) void ckpt8_load_kernel(const CopyArgs a)
 {

@@ -60,8 +60,8 @@ template <int LR> __device__ __forceinline__ float lanes_sum(float v)
 // k, so a wave's loads are contiguous runs of a row, 64 / LR rows at once and R of them in turn against the same activations in
 // registers.  Codes become bf16 pairs unscaled and meet the activations in two-term dot products (exact products, binary32 sums);
 // the sum of a group of 16 is then multiplied by its scale.  `parts` waves share the reduction of their rows.
-// us and TB/s of weights, one token: 8192 x 1024 3.5, 4096 x 4096 with outer blocks 5.2 (mostly the launch and one trip to memory), 8192 x 8192
-// 9.1, 4.2 out of the last-level cache and 11.6, 3.3 out of memory, 16384 x 16384 27.7, 5.5; two tokens 8192 x 8192 12.6.
+// us and TB/s of weights (rows x reduction), one token: 8192 x 1024 3.8, 4096 x 4096 with outer blocks 5.1 (mostly the launch and one trip to memory), 8192 x 8192
+// 9.0, 4.2 out of the last-level cache and 10.6, 3.6 out of memory, with outer blocks 13.2, 3.0, 16384 x 16384 27.5, 5.5; two tokens 8192 x 8192 13.3.
 template <int M, int LR, int R, bool OUTER>
 __global__ __launch_bounds__(256) void gemv_few_kernel(const GemvArgs a, int parts)
 {
@@ -185,8 +185,8 @@ __device__ __forceinline__ u32x4 weights8(uint32_t codes, float scale)
 // 512 bytes of activations of a row in neighbouring lanes - and turns them in an LDS area of its own (16-byte places, exclusive-or with the row
 // against bank conflicts), while the loads of the next piece are on their way.  With outer blocks the sum over 128 k is multiplied by the
 // row's outer scale before it joins the total.
-// us: 5 tokens, 5003 x 2064 7.2; 16 tokens, 4096 x 4096 with outer blocks 7.1, 8192 x 8192 15.6, 16384 x 16384 42 (3.6 TB/s); 8192 x 8192 with 32 tokens
-// 22.9, with 64 39.  Between the launch and the join a wave's pieces follow each other: a trip to memory each, whose time the two waves a SIMD cover in part, and
+// us out of memory: 5 tokens, 5003 x 2064 7.2; 16 tokens, 4096 x 4096 with outer blocks 7.0, 6144 x 4096 8.6, 8192 x 8192 15.0, 16384 x 16384 42 (3.6 TB/s); 8192 x 8192
+// with 32 tokens 23.1, with 64 39.  Between the launch and the join a wave's pieces follow each other: a trip to memory each, whose time the two waves a SIMD cover in part, and
 // 3.4 vector instructions a weight (6.7 us of all SIMDs' time at 8192 x 8192), most of which make the weights bf16.
 constexpr int kPiece = 256;                                                  // k
 template <int NT, int RT> struct GemvStage {

@@ -8,7 +8,8 @@
 // that the variance is taken about the mean without a second read.  All sums are binary32.  Bound: HBM (a copy of 1 GB reaches 5.1 TB/s here,
 // one of 64 MB, which the last-level cache holds, 6.9); calls of a few rows: the launch, 2.2 us.
 //
-// Figures: bf16 rows, us and TB/s over the bytes that a call has to read and write.
+// Figures: bf16 rows where nothing else stands, layer norm, us of a kernel in a kernel trace and TB/s over the bytes that a call has to read and write; calls on three sets of
+// arrays in turn (the comparisons of two forms: on one set).
 #include "rowwise.h"
 
 namespace tj {
@@ -81,8 +82,9 @@ template <int TPR, int V> __device__ __forceinline__ void params_to_lds(const fl
 // A row lies in the registers of TPR threads, V chunks of eight each; the parameters of a thread's columns stay there for all of its rows,
 // and the next row is on its way while a row is summed and written.
 //                      8192 x 768    16384 x 1024   16384 x 2048   16384 x 4096   8192 x 8192   4096 x 16384
-//   with a checkpoint   11.0  2.9      15.1  5.6      28.7  5.8      65.2  5.2      63.3  5.3      63.7  5.3
-//   without              8.6  2.9      12.1  5.6      22.2  6.0      43.0  6.2      43.8  6.1      43.4  6.2
+//   with a checkpoint   10.4  3.0      15.0  5.6      34.8  4.8      67.8  5.0      64.3  5.2      63.3  5.3
+//   without              8.2  3.1      11.8  5.7      25.7  5.2      51.6  5.2      49.0  5.5      49.4  5.4
+// RMS norm with a checkpoint 8192 x 768 9.4, 8192 x 4096 33.0, 5.1; binary32 with one 16384 x 1024 32.7, 4.6, 8192 x 4096 58.0, 5.2, 4096 x 16384 112, 5.4.
 template <int KIND, bool OF32, int TPR, int V>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_fwd_kernel(const NormFwdArgs a)
 {
@@ -169,7 +171,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_fwd_kernel(const N
 }
 
 // rows that no workgroup's registers hold, and rows shorter than a chunk: three sweeps over the row, the later ones from the caches
-// (2048 x 32768 78.9 us, 3.4 TB/s)
+// (2048 x 32768 88 us, 3.1 TB/s, with a checkpoint 102, 3.3)
 template <int KIND, bool OF32>
 __global__ __launch_bounds__(1024) void norm_fwd_long_kernel(const NormFwdArgs a)
 {
@@ -221,12 +223,13 @@ __global__ __launch_bounds__(1024) void norm_fwd_long_kernel(const NormFwdArgs a
 }
 
 // As the forward kernel, with blockDim.x / TPR rows at once; a thread also keeps the sums of its columns over all of its rows.  In the
-// end those of the workgroup's rows are added through LDS, in their order: one partial sum a workgroup, one workgroup a CU, no atomics.  (The figures are of calls
-// that repeat on the same arrays: 16384 x 1024 out of the last-level cache, through it, 17.4.)
+// end those of the workgroup's rows are added through LDS, in their order: one partial sum a workgroup, one workgroup a CU, no atomics.
 //                        8192 x 768    16384 x 1024   16384 x 2048   16384 x 4096   8192 x 8192   4096 x 16384
-//   from a checkpoint     11.7  2.7      18.8  4.5      33.7  5.0      56.8  5.9      62.0  5.4      62.8  5.3
-//   from the input        11.2  3.4      19.1  5.3      37.6  5.4      65.4  6.2      67.4  6.0      70.4  5.7
-//   checkpoint, dx alone   9.6  3.3      16.5  5.1      31.3  5.4      54.6  6.2      58.0  5.8      58.2  5.8
+//   from a checkpoint     12.0  2.6      18.8  4.5      34.1  4.9      62.6  5.4      65.7  5.1      68.6  4.9
+//   from the input        12.2  3.1      19.8  5.1      37.5  5.4      72.6  5.5      74.4  5.4      78.4  5.1
+//   checkpoint, dx alone   9.8  3.2      16.5  5.1      32.6  5.2      60.0  5.6      63.6  5.3      64.3  5.2
+// Binary32 from the input 16384 x 1024 54.2, 3.7, 8192 x 4096 104, 3.9, 4096 x 16384 160, 5.0: with 128 registers a thread, as 1024 threads leave it, these forms (V = 2, binary32
+// arrays) keep up to 28 of a thread's numbers in scratch memory; from a checkpoint 36.5, 4.1, 60.7, 5.0, 120, 5.1.
 template <int KIND, bool GF32, bool OF32, bool STREAM, int TPR, int V>
 __global__ __launch_bounds__(TPR == 64 && V > 2 ? 512 : 1024) void norm_bwd_kernel(const NormBwdArgs a)
 {
@@ -347,7 +350,7 @@ __global__ __launch_bounds__(TPR == 64 && V > 2 ? 512 : 1024) void norm_bwd_kern
     }
 }
 
-// rows longer than that or shorter than a chunk: the gradient of the input by two sweeps over a row (2048 x 32768 110 us, 3.7 TB/s) ...
+// rows longer than that or shorter than a chunk: the gradient of the input by two sweeps over a row (2048 x 32768 108 us, 3.7 TB/s) ...
 template <int KIND, bool GF32, bool OF32>
 __global__ __launch_bounds__(1024) void norm_bwd_long_kernel(const NormBwdArgs a)
 {
@@ -385,7 +388,7 @@ __global__ __launch_bounds__(1024) void norm_bwd_long_kernel(const NormBwdArgs a
     }
 }
 
-// ... and the sums over rows by threads that own eight columns of every gridDim.y-th row (59.0 us, 4.5 TB/s)
+// ... and the sums over rows by threads that own eight columns of every gridDim.y-th row (58.4 us, 4.6 TB/s)
 template <int KIND, bool GF32>
 __global__ __launch_bounds__(256) void norm_params_long_kernel(const NormBwdArgs a)
 {
@@ -410,7 +413,7 @@ __global__ __launch_bounds__(256) void norm_params_long_kernel(const NormBwdArgs
 
 // The partial sums of G <= 256 workgroups, in an order of their own: a workgroup takes 32 columns (a cache line), four neighbouring ones a thread; of
 // the 32 threads of a column each adds every 32nd partial sum (all of its loads are on their way at once), then eight lanes the threads' sums.
-// 256 partial sums of D = 1024 3.9 us, of which the launch and one trip to memory are all but 0.5; 16384 6.9, 32768 13.2.
+// 256 partial sums of D = 1024 3.9 us, of which the launch and one trip to memory are all but 0.5; 16384 6.9, 32768 13.0.
 constexpr int kMostPartials = 256;
 __global__ __launch_bounds__(256) void norm_params_reduce_kernel(const float *part_g, const float *part_b, int64_t part_ld, int G, int D, float *dgamma, float *dbeta)
 {
