@@ -357,7 +357,8 @@ template <int NT, int RT> void run_gemv(const GemvArgs &a, int outer, int most_w
     else gemv_kernel<NT, RT, false><<<grid, waves * 64, lds, st>>>(a);
 }
 
-// Tiles of 16 rows and how they are dealt, us out of memory by rows x waves of a workgroup (0.2 to 2 us less where the last-level cache has the weights):
+// Tiles of 16 rows and how they are dealt, us of a call in a replayed graph, out of memory, by rows x waves of a workgroup (0.2 to 4 us less where the last-level cache
+// has the weights):
 //   up to one a CU      a workgroup each, whose eight waves split the reduction (85 KB of LDS)
 //   up to two a CU      a workgroup takes two, which share the activations, and is still alone on its CU with eight waves (six for 32 tokens: 127 KB of LDS)
 //   up to three a CU    one each with four waves: three workgroups (two for 32 tokens) fit on a CU and all run at once
@@ -417,7 +418,7 @@ template <int M> void run_few(const GemvArgs &a, int outer, hipStream_t st)
 hipError_t launch_gemv(const void *X, int64_t ldx, int64_t M, const GemmOperand &W, int64_t K, const RowDst &y, hipStream_t st)
 {
     const GemvArgs a{static_cast<const uint16_t *>(X), ldx, M, W.codes, W.scales, W.gscale, W.rows, (int)K, y.p, y.ld, y.f32};
-    // us out of memory, dot products / matrix instructions:
+    // us of a call in a replayed graph, out of memory, dot products / matrix instructions:
     //                    1 token        2 tokens       3 tokens       4 tokens
     //    1024 x 1024    2.5 /  3.6     2.9 /  3.6     3.3 /  3.6     3.9 /  3.7
     //    4096 x 4096    4.7 /  6.1     5.9 /  6.2     7.1 /  6.2     8.4 /  6.2
