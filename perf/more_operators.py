@@ -6,7 +6,7 @@
            cache come back; "bits8": E4M3 codes and a power of two per token and head, and the new tokens are read back from it
   attend   queries against the paged cache: every token sees the shared prefix (if there is one), its own sequence's past and itself
   sample   one token per row of logits: temperature, the k largest, the smallest set of probability p, the least share of the
-           largest probability, then the one that a given random number falls on
+           largest probability, then the one that a given random number falls on, from the largest down
 
 A batch is B sequences; sequence b has past_b tokens in the cache and n_b new ones, whose rows follow each other.  The pages of its own tokens
 are listed in row b of a table, those of the prefix in a table of their own; position = prefix length + place in the sequence.  Where
@@ -324,8 +324,9 @@ def _plain_sample(s):
     if s["min_p"] is not None:
         keep &= least
     keep = torch.where(greedy, rank == 0, keep)
-    sums = torch.cumsum(torch.zeros_like(w).scatter_(1, order, w * keep), 1)
-    return {"tokens": (sums <= u * sums[:, -1:]).sum(1)}
+    sums = torch.cumsum(w * keep, 1)
+    at = (sums <= u * sums[:, -1:]).sum(1, keepdim=True)
+    return {"tokens": order.gather(1, at)[:, 0]}
 
 
 def _run_plain(s):
@@ -390,9 +391,7 @@ def _exact_sample(s):
             many = min(many, 1 + int((sums[:-1] < at("top_p", n) * sums[-1]).sum()))
         if s["min_p"] is not None:
             many = min(many, int((w[order] >= at("min_p", n)).sum()))
-        kept = np.sort(order[:many])
-        sums = np.cumsum(w[kept])
-        got.append(int(kept[np.searchsorted(sums, u[n] * sums[-1], side="right")]))
+        got.append(int(order[np.searchsorted(sums[:many], u[n] * sums[many - 1], side="right")]))
     return {"tokens": torch.tensor(got, dtype=torch.int64)}
 
 
