@@ -367,6 +367,108 @@ int nvfp4_ckpt8_load(const nvfp4_ckpt8 *src, void *Y, int out_dtype, int64_t ldy
 int nvfp4_gemv(const void *X, int64_t ldx, int64_t M, const nvfp4_tensor *W, void *Y, int out_dtype, int64_t ldy, void *stream);
 
 /*
+ * Sequences of tokens: rotary positions, a paged cache of keys and values, attention over it, the choice of the next token.  Row arrays are strided as
+ * in the calls above and start at any element; sums, angles and softmax statistics are binary32 or wider, each output is rounded once.
+ *
+ * What device memory holds (lengths, tables, positions, parameters of rows) is not looked at by the host: whatever it is, no call reads or writes outside its
+ * arrays.  Where a length is negative or longer than its table, it is taken as 0 or as the table's room; a page that the cache does not have holds
+ * no tokens: appending to it writes nothing, attention does not see it, loading gives zeros.
+ */
+enum { NVFP4_ROPE_HALF = 0, NVFP4_ROPE_PAIRS = 1 };
+enum { NVFP4_KV_BF16 = 0, NVFP4_KV_8 = 1 };
+enum { NVFP4_ROPE_PLAIN = 0, NVFP4_ROPE_LINEAR = 1, NVFP4_ROPE_BASE = 2, NVFP4_ROPE_PARTS = 3 };
+
+/* Rotary positions of a head of D elements: pair j < R / 2 is turned by the angle position * freqs[j] (the product of the binary32 frequency and the integer, exact):
+ *   (a, b) -> scale (a cos - b sin, b cos + a sin)
+ * NVFP4_ROPE_HALF: pair j is elements (j, R / 2 + j); NVFP4_ROPE_PAIRS: (2j, 2j + 1).  Elements from R on stay as they are. */
+typedef struct nvfp4_rotation {
+    const float *freqs;  /* device [R / 2], 4-byte aligned */
+    int64_t R;           /* even, 0 <= R <= D */
+    int32_t form;        /* NVFP4_ROPE_HALF / NVFP4_ROPE_PAIRS */
+    float scale;         /* 1 but for contexts scaled so */
+} nvfp4_rotation;
+
+/* Frequencies base^(-2j / R), j < R / 2, into HOST memory, scaled for contexts `factor` times as long as the `trained` tokens:
+ *   PLAIN   as they are                       LINEAR  all divided by factor
+ *   BASE    base * factor^(R / (R - 2)) in place of base: the fastest stays, the slowest is divided by factor (R > 2)
+ *   PARTS   by the turns t_j = trained * freq / (2 pi): divided by factor below `low` turns, as they are above `high`, between the two in proportion
+ * low and high are read by PARTS alone (usual: 1 and 32).  Errors: NULL, SHAPE (R odd or outside 0 .. 2^20), ENUM (scaling; base or factor not finite and above 0;
+ * trained <= 0 or not 0 <= low < high for PARTS).  Host-only helper. */
+int nvfp4_rope_frequencies(int64_t R, double base, int scaling, double factor, double trained, double low, double high, float *freqs);
+
+/*
+ * Y = X with the H heads of D elements of every row turned by pos[n] (device int32 [N], 4-byte aligned); inverse != 0: the transposed rotation (angles negated, the same scale), which
+ * takes the gradient of Y to the gradient of X.  X is NVFP4_SRC_BF16 or _F32.  Y may be X itself, with X's type and stride; else it must not overlap X.
+ * H * D <= 2^22, D <= 4096, N <= 2^24.  Errors: NULL, SHAPE, ENUM, ALIGN.
+ */
+int nvfp4_rope(const void *X, int src_kind, int64_t ldx, const int32_t *pos, int64_t N, int64_t H, int64_t D, const nvfp4_rotation *rotation, int inverse,
+               void *Y, int out_dtype, int64_t ldy, void *stream);
+
+/* A cache of keys and values in pages of `page` tokens: k, v [pages][H][page][D], 16-byte aligned.
+ *   NVFP4_KV_BF16  bf16
+ *   NVFP4_KV_8     E4M3 codes; k_exps, v_exps [pages][H][page][ceil(D / 128)]: every token's head is a row of an 8-bit checkpoint (nvfp4_ckpt8)
+ * page: a power of two from 16 to 65536; D: a multiple of 16 up to 256; pages < 2^31, at most 2^40 elements. */
+typedef struct nvfp4_kvcache {
+    void *k, *v;
+    uint8_t *k_exps, *v_exps;   /* NVFP4_KV_8 */
+    int64_t pages, H, page, D;
+    int32_t kind;
+    int32_t reserved;
+} nvfp4_kvcache;
+
+/* A batch of B sequences and the rows of a call.  Rows starts[b] .. starts[b + 1] - 1 are the last tokens of sequence b, of whose own tokens the cache then has lens[b]
+ * (the call's among them): row starts[b] + i is own token p = lens[b] - n_b + i.  Own token p lies in page table[b][p / page], slot p % page.  Before the own tokens every sequence has the
+ * `prefix` tokens of the pages prefix_table[0 ..]: row positions are prefix + p.  starts NULL: one row each (N = B).  Rows that belong to no
+ * sequence, and rows with p < 0 when they are appended or loaded, are left as they were.  Device memory, int32, 4-byte aligned. */
+typedef struct nvfp4_kvbatch {
+    const int32_t *table;         /* [B][width] */
+    const int32_t *lens;          /* [B] */
+    const int32_t *starts;        /* [B + 1] ascending, or NULL */
+    const int32_t *prefix_table;  /* [ceil(prefix / page)], NULL where prefix is 0 */
+    int64_t B, width, prefix;     /* B <= 65536; width * page + prefix < 2^31 - 65536 */
+} nvfp4_kvbatch;
+
+/*
+ * Writes keys K [N x H D] (turned at their positions; rotation NULL: as they are) and values V [N x H D] of the batch's rows into the cache.  Q (optional) [N x Hq D]: turned in the same way into Qo.
+ * K, V and Q are src_kind; Qo is out_dtype.  Two rows with one place (a page named twice) leave one of the two there, element by element either's.
+ * Errors: NULL, SHAPE, ENUM, ALIGN, MISMATCH (starts NULL and N != B).
+ */
+int nvfp4_kv_append(const void *Q, int64_t ldq, int64_t Hq, const void *K, int64_t ldk, const void *V, int64_t ldv, int src_kind, int64_t N,
+                    const nvfp4_kvcache *cache, const nvfp4_kvbatch *batch, const nvfp4_rotation *rotation, void *Qo, int out_dtype, int64_t ldqo,
+                    void *stream);
+/* The batch's rows of the cache (keys turned as they lie there): K, V [N x H D].  Errors as above. */
+int nvfp4_kv_load(const nvfp4_kvcache *cache, const nvfp4_kvbatch *batch, int64_t N, void *K, int64_t ldk, void *V, int64_t ldv, int out_dtype, void *stream);
+
+/*
+ * Attention of the batch's rows Q [N x Hq D] (bf16) over the cache: head h of row (b, p) sees the prefix and own tokens 0 .. p through head h / (Hq / H) of keys and values,
+ *   out = sum_t softmax_t(scale q . k_t) v_t        (zeros where it sees nothing)
+ * Out [N x Hq D] bf16.  Scores and sums are binary32; the weights of the values are rounded to bf16 for the matrix instructions.  A NaN or infinity in a key or value stays with the
+ * rows that see it.  The prefix is read once for all rows of a tile, whatever the number of sequences.
+ * Hq a multiple of H, N * Hq <= 2^30; scale finite.  ws: nvfp4_attn_workspace_bytes of the same sizes (16-byte aligned; from N, B, width and prefix alone, not from lengths, so that
+ * one does for all steps of a batch).  Same inputs, same bits.  Errors: NULL, SHAPE, ENUM, ALIGN, MISMATCH, WORKSPACE.
+ */
+int nvfp4_attn(const void *Q, int64_t ldq, int64_t N, int64_t Hq, const nvfp4_kvcache *cache, const nvfp4_kvbatch *batch, float scale, void *Out, int64_t ldo,
+               void *ws, size_t ws_bytes, void *stream);
+size_t nvfp4_attn_workspace_bytes(int64_t N, int64_t Hq, int64_t H, int64_t D, int64_t page, int64_t B, int64_t width, int64_t prefix);
+
+/*
+ * One token per row of logits [N x V] (NVFP4_SRC_BF16 or _F32), from given numbers u [N], 0 <= u < 1 (below 0 or NaN counts as 0, 1 and more as the largest below 1):
+ *   order   by logit, largest first, equal ones by index
+ *   top_k   the first top_k of the order (< 1 or > V: all)
+ *   top_p   of those the shortest run from the first on whose probabilities, w = exp((x - max) / temperature) over their sum, reach top_p: a token is kept if those before
+ *           it sum to less than top_p (<= 0: the first alone; >= 1 or NaN: all)
+ *   min_p   of those the ones with w >= min_p (NaN: all; > 1 counts as 1)
+ * and of what is left, in this order, the first token whose sum of w with those before it exceeds u times the sum of all.  temperature <= 0 or NaN: the first of the order.
+ * NaN logits count as -infinity, which is never drawn; several +infinities share the probability; a row without anything else than -infinity gives -1.
+ * temperature, top_k, top_p, min_p: device [N], each optional (1, and no limit).  w and its sums are fixed-point numbers with 2^43 for the largest weight: sums do not depend on
+ * their order, and weights under 2^-44 of the largest are 0.  u and the tokens (int64) are device [N].  1 <= V <= 2^20, N <= 2^24.
+ * ws: nvfp4_sample_workspace_bytes(N, V), 16-byte aligned.  Errors: NULL, SHAPE, ENUM, ALIGN, WORKSPACE.
+ */
+int nvfp4_sample(const void *logits, int src_kind, int64_t ld, int64_t N, int64_t V, const float *u, const float *temperature, const int32_t *top_k,
+                 const float *top_p, const float *min_p, int64_t *tokens, void *ws, size_t ws_bytes, void *stream);
+size_t nvfp4_sample_workspace_bytes(int64_t N, int64_t V);
+
+/*
  * Scratch bytes an operation needs.  op = NVFP4_OP_*.  QUANTIZE: (N, D) = (R, C) of the source, C ignored.
  * GEMM: Out is [N x C] with reduction length D.  LINEAR_*: as in the calls above.  Returns 0 for a bad op.
  *

@@ -25,10 +25,14 @@ OUT_BF16, OUT_F32 = 0, 1
 OP_QUANTIZE, OP_GEMM, OP_LINEAR_FWD, OP_LINEAR_BWD_DX, OP_LINEAR_BWD_DW, OP_LINEAR_BWD = 0, 1, 2, 3, 4, 5
 NORM_LAYER, NORM_RMS = 0, 1
 ACT_SWIGLU, ACT_GELU = 0, 1
+ROPE_HALF, ROPE_PAIRS = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_PARTS = 0, 1, 2, 3
+KV_BF16, KV_8 = 0, 1
 CKPT_GROUP = 128               # elements of a row that share a power of two in an 8-bit checkpoint
 
 EXPORTS = ["nvfp4_quantize", "nvfp4_quantize_dual", "nvfp4_gemm_nt", "nvfp4_gemm_nt_static", "nvfp4_linear_fwd", "nvfp4_linear_bwd_dx", "nvfp4_linear_bwd_dw", "nvfp4_linear_bwd", "nvfp4_osci_update", "nvfp4_osci_suppress", "nvfp4_osci_select", "nvfp4_osci_update_sparse", "nvfp4_osci_suppress_sparse", "nvfp4_osci_select_workspace_bytes", "nvfp4_outctl_fwd", "nvfp4_outctl_bwd", "nvfp4_outctl_workspace_bytes", "nvfp4_outctl_dw_plan", "nvfp4_backward_plan", "nvfp4_backward_product_plan",
            "nvfp4_norm_fwd", "nvfp4_norm_bwd", "nvfp4_norm_workspace_bytes", "nvfp4_act_fwd", "nvfp4_act_bwd", "nvfp4_ckpt8_save", "nvfp4_ckpt8_load", "nvfp4_gemv",
+           "nvfp4_rope_frequencies", "nvfp4_rope", "nvfp4_kv_append", "nvfp4_kv_load", "nvfp4_attn", "nvfp4_attn_workspace_bytes", "nvfp4_sample", "nvfp4_sample_workspace_bytes",
            "nvfp4_workspace_bytes", "nvfp4_gemm_plan", "nvfp4_gemm_plan_kernel", "nvfp4_amax_bf16", "nvfp4_stream_key", "nvfp4_strerror", "nvfp4_version"]
 
 
@@ -51,6 +55,20 @@ class CQcfg(C.Structure):
 
 class CCkpt8(C.Structure):
     _fields_ = [("codes", C.c_void_p), ("exps", C.c_void_p), ("rows", C.c_int64), ("K", C.c_int64)]
+
+
+class CRotation(C.Structure):
+    _fields_ = [("freqs", C.c_void_p), ("R", C.c_int64), ("form", C.c_int32), ("scale", C.c_float)]
+
+
+class CKvCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_exps", C.c_void_p), ("v_exps", C.c_void_p), ("pages", C.c_int64), ("H", C.c_int64), ("page", C.c_int64),
+                ("D", C.c_int64), ("kind", C.c_int32), ("reserved", C.c_int32)]
+
+
+class CKvBatch(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("lens", C.c_void_p), ("starts", C.c_void_p), ("prefix_table", C.c_void_p), ("B", C.c_int64), ("width", C.c_int64),
+                ("prefix", C.c_int64)]
 
 
 class CProductPlan(C.Structure):
@@ -134,6 +152,23 @@ def lib():
         L.nvfp4_ckpt8_load.argtypes = [vp, vp, i32, i64, vp]
         L.nvfp4_gemv.restype = i32
         L.nvfp4_gemv.argtypes = [vp, i64, i64, vp, vp, i32, i64, vp]
+        dbl, rot, kvc, kvb = C.c_double, C.POINTER(CRotation), C.POINTER(CKvCache), C.POINTER(CKvBatch)
+        L.nvfp4_rope_frequencies.restype = i32
+        L.nvfp4_rope_frequencies.argtypes = [i64, dbl, i32, dbl, dbl, dbl, dbl, vp]
+        L.nvfp4_rope.restype = i32
+        L.nvfp4_rope.argtypes = [vp, i32, i64, vp, i64, i64, i64, rot, i32, vp, i32, i64, vp]
+        L.nvfp4_kv_append.restype = i32
+        L.nvfp4_kv_append.argtypes = [vp, i64, i64, vp, i64, vp, i64, i32, i64, kvc, kvb, rot, vp, i32, i64, vp]
+        L.nvfp4_kv_load.restype = i32
+        L.nvfp4_kv_load.argtypes = [kvc, kvb, i64, vp, i64, vp, i64, i32, vp]
+        L.nvfp4_attn.restype = i32
+        L.nvfp4_attn.argtypes = [vp, i64, i64, i64, kvc, kvb, C.c_float, vp, i64, vp, sz, vp]
+        L.nvfp4_attn_workspace_bytes.restype = sz
+        L.nvfp4_attn_workspace_bytes.argtypes = [i64] * 8
+        L.nvfp4_sample.restype = i32
+        L.nvfp4_sample.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.nvfp4_sample_workspace_bytes.restype = sz
+        L.nvfp4_sample_workspace_bytes.argtypes = [i64, i64]
         L.nvfp4_workspace_bytes.restype = sz
         L.nvfp4_workspace_bytes.argtypes = [i32, i64, i64, i64, i32]
         L.nvfp4_gemm_plan.restype = i32
@@ -737,3 +772,165 @@ def gemv(X: torch.Tensor, W: NVFP4Tensor, out_dtype: int = OUT_BF16, *, Y: Optio
     Y, ldy = _out_rows(Y, M, W.rows, out_dtype, X, "Y", dev)
     _check(lib().nvfp4_gemv(_ptr(X), ldx, M, C.byref(W.c_struct()), _ptr(Y), out_dtype, ldy, _raw_stream(dev)), "nvfp4_gemv")
     return Y
+
+
+# ---- operators on sequences of tokens: rotary positions, the paged cache of keys and values, attention over it, sampling ----
+#
+# As above: on the current device's current stream, every tensor on that device.
+
+def rope_frequencies(R: int, base: float = 10000.0, *, scaling: int = ROPE_PLAIN, factor: float = 1.0, trained: float = 0.0, low: float = 1.0, high: float = 32.0,
+                     device="cuda") -> torch.Tensor:
+    """nvfp4_rope_frequencies: float32 [R / 2], scaled for contexts `factor` times as long as the trained ones."""
+    f = torch.empty(max(R, 0) // 2, dtype=torch.float32)
+    _check(lib().nvfp4_rope_frequencies(R, base, scaling, factor, trained, low, high, f.data_ptr()), "nvfp4_rope_frequencies")
+    return f.to(device)
+
+
+@dataclass
+class Rope:
+    """Rotary positions of a head's first 2 * freqs.numel() elements."""
+    freqs: torch.Tensor      # float32 [R / 2]
+    form: int = ROPE_HALF
+    scale: float = 1.0       # of cosine and sine
+
+    def c_struct(self, dev: int) -> CRotation:
+        f = self.freqs
+        assert f.dtype == torch.float32 and f.dim() == 1 and f.is_contiguous() and f.get_device() == dev, "freqs: float32 [R / 2], on the current device"
+        return CRotation(_ptr(f), 2 * f.numel(), self.form, self.scale)
+
+
+@dataclass
+class KVCache:
+    """Pages of keys and values: [pages, heads, tokens of a page, D], bf16, or E4M3 codes (uint8) with exponents [.., ceil(D / 128)]."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_exps: Optional[torch.Tensor] = None
+    v_exps: Optional[torch.Tensor] = None
+
+    def c_struct(self, dev: int) -> CKvCache:
+        k, v, ke, ve = self.k, self.v, self.k_exps, self.v_exps
+        kind = KV_BF16 if k.dtype == torch.bfloat16 else KV_8
+        assert k.dim() == 4 and k.dtype in (torch.bfloat16, torch.uint8) and k.shape == v.shape and k.dtype == v.dtype, "cache: bf16 or uint8 [pages, heads, page, D], keys and values alike"
+        assert k.is_contiguous() and v.is_contiguous() and k.get_device() == v.get_device() == dev, "cache: contiguous, on the current device"
+        pages, heads, page, D = k.shape
+        if kind == KV_8:
+            for e in (ke, ve):
+                assert e is not None and e.dtype == torch.uint8 and tuple(e.shape) == (pages, heads, page, -(-D // CKPT_GROUP)) and e.is_contiguous() and e.get_device() == dev, "exponents of an 8-bit cache, on the current device"
+        else:
+            assert ke is None and ve is None, "exponents: of an 8-bit cache alone"
+        return CKvCache(_ptr(k), _ptr(v), _ptr(ke), _ptr(ve), pages, heads, page, D, kind, 0)
+
+
+def alloc_kv_cache(pages: int, heads: int, page: int, D: int, kind: int = KV_BF16, device="cuda") -> KVCache:
+    if kind == KV_BF16:
+        return KVCache(*(torch.empty((pages, heads, page, D), dtype=torch.bfloat16, device=device) for _ in range(2)))
+    u8 = lambda n: [torch.empty((pages, heads, page, n), dtype=torch.uint8, device=device) for _ in range(2)]
+    return KVCache(*u8(D), *u8(-(-D // CKPT_GROUP)))
+
+
+@dataclass
+class KVBatch:
+    """A batch of sequences (nvfp4_kvbatch): int32 tensors on the device."""
+    table: torch.Tensor                           # [B, width]: pages of the sequences' own tokens
+    lens: torch.Tensor                            # [B]: own tokens, the call's among them
+    starts: Optional[torch.Tensor] = None         # [B + 1]: rows of the call; None: one each
+    prefix_table: Optional[torch.Tensor] = None   # pages of the tokens that all sequences share
+    prefix: int = 0                               # how many those are
+
+    def c_struct(self, dev: int, page: int) -> CKvBatch:
+        ok = lambda t, *shape: t.dtype == torch.int32 and tuple(t.shape) == shape and t.is_contiguous() and t.get_device() == dev
+        table, lens, starts, prefix = self.table, self.lens, self.starts, self.prefix_table
+        B, width = table.shape
+        assert ok(table, B, width) and ok(lens, B), "table [B, width] and lens [B]: int32, contiguous, on the current device"
+        assert starts is None or ok(starts, B + 1), "starts: int32 [B + 1], on the current device"
+        assert self.prefix <= 0 or (prefix is not None and ok(prefix, prefix.numel()) and prefix.numel() * page >= self.prefix), "prefix_table: int32, pages of the whole prefix, on the current device"
+        return CKvBatch(_ptr(table), _ptr(lens), _ptr(starts), _ptr(prefix), B, width, self.prefix)
+
+
+def rope(X: torch.Tensor, pos: torch.Tensor, rotation: Rope, heads: int, out_dtype: int = OUT_BF16, *, inverse: bool = False,
+         Y: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """nvfp4_rope: the heads of every row of X [N, heads * D] turned by pos (int32 [N]); inverse: the gradient's way back.  Y may be X."""
+    dev = _current_device()
+    kind, ldx, N, width = _rows(X, "X", dev)
+    assert heads > 0 and width % heads == 0, "X: rows of whole heads"
+    assert pos.dtype == torch.int32 and tuple(pos.shape) == (N,) and pos.is_contiguous() and pos.get_device() == dev, "pos: int32 [N], on the current device"
+    Y, ldy = _out_rows(Y, N, width, out_dtype, X, "Y", dev)
+    _check(lib().nvfp4_rope(_ptr(X), kind, ldx, _ptr(pos), N, heads, width // heads, C.byref(rotation.c_struct(dev)), int(inverse), _ptr(Y), out_dtype, ldy,
+                            _raw_stream(dev)), "nvfp4_rope")
+    return Y
+
+
+def kv_append(K: torch.Tensor, V: torch.Tensor, cache: KVCache, batch: KVBatch, rotation: Optional[Rope] = None, *, Q: Optional[torch.Tensor] = None,
+              out_dtype: int = OUT_BF16, Qo: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """nvfp4_kv_append: keys (turned at their positions) and values [N, heads * D] of the batch's rows into the cache; Q [N, any heads * D] turned in the same way is returned."""
+    dev = _current_device()
+    cc = cache.c_struct(dev)
+    cb = batch.c_struct(dev, cc.page)
+    kind, ldk, N, width = _rows(K, "K", dev)
+    vkind, ldv, *shape = _rows(V, "V", dev)
+    assert width == cc.H * cc.D and shape == [N, width] and vkind == kind, "K, V: one type, [N, heads * D] of the cache"
+    ldq = Hq = ldo = 0
+    if Q is not None:
+        qkind, ldq, rows, qwidth = _rows(Q, "Q", dev)
+        assert rows == N and qwidth % cc.D == 0 and qkind == kind, "Q: the type and rows of K, whole heads"
+        Hq = qwidth // cc.D
+        Qo, ldo = _out_rows(Qo, N, qwidth, out_dtype, Q, "Qo", dev)
+    else:
+        assert Qo is None, "Qo: the output of Q"
+    _check(lib().nvfp4_kv_append(_ptr(Q), ldq, Hq, _ptr(K), ldk, _ptr(V), ldv, kind, N, C.byref(cc), C.byref(cb),
+                                 C.byref(rotation.c_struct(dev)) if rotation is not None else None, _ptr(Qo), out_dtype, ldo, _raw_stream(dev)), "nvfp4_kv_append")
+    return Qo
+
+
+def kv_load(cache: KVCache, batch: KVBatch, N: int, out_dtype: int = OUT_BF16, *, K: Optional[torch.Tensor] = None, V: Optional[torch.Tensor] = None):
+    """nvfp4_kv_load: (K, V) [N, heads * D] of the batch's N rows as the cache holds them."""
+    dev = _current_device()
+    cc = cache.c_struct(dev)
+    cb = batch.c_struct(dev, cc.page)
+    K, ldk = _out_rows(K, N, cc.H * cc.D, out_dtype, cache.k, "K", dev)
+    V, ldv = _out_rows(V, N, cc.H * cc.D, out_dtype, cache.k, "V", dev)
+    _check(lib().nvfp4_kv_load(C.byref(cc), C.byref(cb), N, _ptr(K), ldk, _ptr(V), ldv, out_dtype, _raw_stream(dev)), "nvfp4_kv_load")
+    return K, V
+
+
+def attn_workspace_bytes(N: int, Hq: int, cache: KVCache, batch: KVBatch) -> int:
+    pages, heads, page, D = cache.k.shape
+    return int(lib().nvfp4_attn_workspace_bytes(N, Hq, heads, D, page, *batch.table.shape, batch.prefix))
+
+
+def attn(Q: torch.Tensor, cache: KVCache, batch: KVBatch, heads: int, *, scale: Optional[float] = None, Out: Optional[torch.Tensor] = None,
+         ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """nvfp4_attn: the batch's rows Q [N, heads * D] (bf16) over the cache; scale: 1 / sqrt(D) unless given.  Rows that belong to no sequence are not written."""
+    dev = _current_device()
+    cc = cache.c_struct(dev)
+    cb = batch.c_struct(dev, cc.page)
+    kind, ldq, N, width = _rows(Q, "Q", dev)
+    assert kind == SRC_BF16 and width == heads * cc.D, "Q: bf16 [N, heads * D]"
+    Out, ldo = _out_rows(Out, N, width, OUT_BF16, Q, "Out", dev)
+    if ws is None:
+        ws = alloc_workspace(lib().nvfp4_attn_workspace_bytes(N, heads, cc.H, cc.D, cc.page, cb.B, cb.width, cb.prefix), Q.device)
+    else:
+        assert ws.get_device() == dev, "ws: on the current device"
+    _check(lib().nvfp4_attn(_ptr(Q), ldq, N, heads, C.byref(cc), C.byref(cb), cc.D ** -0.5 if scale is None else scale, _ptr(Out), ldo, _ptr(ws), ws.numel() * ws.element_size(),
+                            _raw_stream(dev)), "nvfp4_attn")
+    return Out
+
+
+def sample(logits: torch.Tensor, u: torch.Tensor, *, temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
+           top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None, tokens: Optional[torch.Tensor] = None,
+           ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """nvfp4_sample: a token (int64 [N]) per row of logits [N, V] from u (float32 [N], 0 <= u < 1); the other parameters are [N], float32 (top_k: int32)."""
+    dev = _current_device()
+    kind, ld, N, V = _rows(logits, "logits", dev)
+    for t, what, dtype in ((u, "u", torch.float32), (temperature, "temperature", torch.float32), (top_k, "top_k", torch.int32), (top_p, "top_p", torch.float32),
+                           (min_p, "min_p", torch.float32), (tokens, "tokens", torch.int64)):
+        assert t is None or (t.dtype == dtype and tuple(t.shape) == (N,) and t.is_contiguous() and t.get_device() == dev), what + ": %s [N], on the current device" % dtype
+    if tokens is None:
+        tokens = torch.empty(N, dtype=torch.int64, device=logits.device)
+    if ws is None:
+        ws = alloc_workspace(lib().nvfp4_sample_workspace_bytes(N, V), logits.device)
+    else:
+        assert ws.get_device() == dev, "ws: on the current device"
+    _check(lib().nvfp4_sample(_ptr(logits), kind, ld, N, V, _ptr(u), _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(tokens), _ptr(ws),
+                              ws.numel() * ws.element_size(), _raw_stream(dev)), "nvfp4_sample")
+    return tokens

@@ -1,0 +1,566 @@
+// Attention of a batch's rows over the paged cache of keys and values.
+//
+//   s_t = scale q . k_t,  m = max s,  l = sum 2^(s_t - m),  out = sum 2^(s_t - m) v_t / l       (s in units of log2)
+//
+// A tile is 16 rows of one key head: (new token, query head) pairs of one sequence, or of the whole batch against the shared prefix.  The tokens that a tile sees are cut into
+// parts, so that few rows fill the GPU as well; a part leaves (m, l, unnormalised out) and a second kernel joins them:
+//   out = sum_p 2^(m_p - m) out_p / sum_p 2^(m_p - m) l_p.
+// Where a tile has one part only, and there is no prefix, the first kernel writes the output itself.
+#include "rowwise.h"
+#include "seq_ops.h"
+
+namespace tj {
+
+namespace {
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+
+constexpr int kThreads = 256;
+constexpr int kWaves = 4;
+constexpr int kTile = 16;                 // rows of a tile
+constexpr int kUnit = 64;                 // tokens in which the parts' lengths are counted
+constexpr int kBlock = 32;                // tokens that a wave takes at once
+constexpr int kMinUnits = 2;              // of a part: a block for every wave
+constexpr int kGroups = 2048;             // workgroups that the own tokens of a batch are spread over, and the prefix
+
+struct Args {
+    const uint16_t *q;
+    int64_t ldq;
+    uint16_t *out;
+    int64_t ldo;
+    int N, Hq, G;                         // rows, query heads, query heads of a key head
+    KvCache c;
+    KvBatch b;
+    float scale2;                         // scale * log2 e
+    int target;                           // parts that a key head's own tokens are to be cut into; 0: none are cut
+    int slots;                            // own parts of a key head, at most
+    int prefix_units, prefix_parts;       // units of a part of the prefix, and how many there are
+    float *part_o;                        // [slot][key head][16][D], own parts first
+    float2_t *part_ml;                    // [slot][key head][16]
+};
+
+// What a workgroup has to know of the batch: how many units a part has, and where a part lies.
+struct Place {
+    int b, tile, part, parts;             // sequence; tile and part in it; parts of its tiles
+    int64_t base;                         // first slot of the sequence
+};
+
+__device__ __forceinline__ int units(int tokens) { return (tokens + kUnit - 1) / kUnit; }
+__device__ __forceinline__ int tiles_of(int rows, int G) { return (rows * G + kTile - 1) / kTile; }
+
+__device__ __forceinline__ int64_t block_sum_scan(int64_t v, int64_t *lds, int64_t &before)      // sum over the workgroup; before: over the threads in front
+{
+    int64_t incl = v;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int64_t t = __shfl_up((long long)incl, o, 64);
+        if ((int)(threadIdx.x & 63) >= o) incl += t;
+    }
+    const int w = threadIdx.x >> 6;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 63) lds[w] = incl;
+    __syncthreads();
+    int64_t total = 0;
+    before = incl - v;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+        if (i < w) before += lds[i];
+        total += lds[i];
+    }
+    return total;
+}
+
+// Units of a part of the own tokens: all tiles' units over the parts wanted.  Then where slot `slot` lies (slot >= 0), or where sequence `seq` starts.
+// Every thread of the workgroup calls it; false: there is no such slot.
+__device__ bool find(const Args &a, int slot, int seq, Place &p, int &part_units, int64_t *lds)
+{
+    __shared__ Place found;
+    const int per = (a.b.B + kThreads - 1) / kThreads, b0 = threadIdx.x * per, b1 = min(b0 + per, a.b.B);
+    if (threadIdx.x == 0) found.b = -1;
+    part_units = 1 << 25;                                      // more than any sequence has
+    if (a.target > 0) {
+        int64_t sum = 0;
+        for (int b = b0; b < b1; ++b) {
+            int first, count;
+            rows_of(a.b, b, a.N, first, count);
+            sum += (int64_t)tiles_of(count, a.G) * units(tokens_of(a.b, a.c, b));
+        }
+        int64_t before;
+        const int64_t total = block_sum_scan(sum, lds, before), wanted = (total + a.target - 1) / a.target;
+        part_units = wanted < kMinUnits ? kMinUnits : wanted < part_units ? (int)wanted : part_units;
+    }
+    int64_t sum = 0, at;
+    for (int b = b0; b < b1; ++b) {
+        int first, count;
+        rows_of(a.b, b, a.N, first, count);
+        sum += (int64_t)tiles_of(count, a.G) * max(1, (units(tokens_of(a.b, a.c, b)) + part_units - 1) / part_units);
+    }
+    block_sum_scan(sum, lds, at);
+    for (int b = b0; b < b1; ++b) {
+        int first, count;
+        rows_of(a.b, b, a.N, first, count);
+        const int parts = max(1, (units(tokens_of(a.b, a.c, b)) + part_units - 1) / part_units);
+        const int64_t n = (int64_t)tiles_of(count, a.G) * parts;
+        if (slot >= 0 ? slot >= at && slot < at + n : b == seq) {
+            const int in = slot >= 0 ? (int)(slot - at) : 0;
+            found = Place{b, in / parts, in % parts, parts, at};
+            break;
+        }
+        at += n;
+    }
+    __syncthreads();
+    p = found;
+    return p.b >= 0;
+}
+
+__device__ __forceinline__ float max16_32(float v)             // over the four lanes that hold a row
+{
+    const auto a = __builtin_amdgcn_permlane16_swap(f2u(v), f2u(v), false, false);
+    v = fmaxf(u2f(a[0]), u2f(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(f2u(v), f2u(v), false, false);
+    return fmaxf(u2f(b[0]), u2f(b[1]));
+}
+__device__ __forceinline__ float sum16_32(float v)
+{
+    const auto a = __builtin_amdgcn_permlane16_swap(f2u(v), f2u(v), false, false);
+    v = u2f(a[0]) + u2f(a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(f2u(v), f2u(v), false, false);
+    return u2f(b[0]) + u2f(b[1]);
+}
+
+// ---- a block of 32 tokens in registers ---------------------------------------------------------
+// Products: scores^T [tokens x rows] = K Q^T and out^T [D x rows] += V^T P^T, 16 x 16 x 32 each.  The tokens of a block are dealt to the rows of the two score tiles so that lane
+// (g, row) (g = lane / 16) ends up with tokens 8g .. 8g + 7 of its row, which is what the second product takes from it.  Values come as rows of tokens
+// and are turned in registers: eight tokens x D / 16 elements a lane.
+template <int DP, bool BITS8> struct Tokens {
+    static constexpr int KC = DP / 32;                   // steps of the first product
+    static constexpr int DV = DP / 16;                   // elements of a value that a lane holds
+    u32x4 k[2][BITS8 ? KC / 2 : KC];                     // [tile][step]: eight elements a step (8 bits: sixteen, two steps)
+    uint32_t v[8][BITS8 ? DV / 4 : DV / 2];              // [token][elements]
+    uint32_t ke[2];                                      // 8 bits: exponents of the lane's token of each tile, a byte a group
+    uint32_t ve[4];                                      // and of tokens 8g ..
+    uint32_t ok;                                         // bit h: tokens 16h .. of the block lie in a page of the cache
+    int t0;
+};
+
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+template <int DP, bool BITS8>
+__device__ __forceinline__ void load_tokens(const KvCache &c, const int *table, int table_len, int head, int t0, int lane, Tokens<DP, BITS8> &r)
+{
+    using T = Tokens<DP, BITS8>;
+    const int m = lane & 15, g = lane >> 4;
+    const int i0 = t0 >> c.page_log2, i1 = (t0 + 16) >> c.page_log2;
+    const int p0 = uniform(i0 < table_len ? table[i0] : -1), p1 = uniform(i1 < table_len ? table[i1] : -1);
+    const bool ok0 = p0 >= 0 && p0 < c.pages, ok1 = p1 >= 0 && p1 < c.pages;
+    r.ok = (uint32_t)ok0 | (uint32_t)ok1 << 1;
+    r.t0 = t0;
+    // tokens of this head in front of the two halves' first
+    const int64_t s0 = (((int64_t)(ok0 ? p0 : 0) * c.heads + head) << c.page_log2) + (t0 & ((1 << c.page_log2) - 1));
+    const int64_t s1 = (((int64_t)(ok1 ? p1 : 0) * c.heads + head) << c.page_log2) + ((t0 + 16) & ((1 << c.page_log2) - 1)) - 16;
+    constexpr int E = BITS8 ? 1 : 2;
+    const char *const k = static_cast<const char *>(c.k), *const v = static_cast<const char *>(c.v);
+    const int tk = (m >> 2) * 8 + (m & 3);               // token of the first tile's row m, the second has the one four further on
+    const char *const kp = k + ((m < 8 ? s0 : s1) + tk) * (c.D * E);
+    const char *const vp = v + ((g < 2 ? s0 : s1) + 8 * g) * (c.D * E) + T::DV * m * E;
+    constexpr int STEP = 4 * 16 / E;                     // elements that four lanes take with 16 bytes each
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int s = 0; s < (BITS8 ? T::KC / 2 : T::KC); ++s) {
+            const int d = STEP * s + (16 / E) * g;
+            r.k[t][s] = u32x4{0, 0, 0, 0};
+            if (d < c.D) r.k[t][s] = *reinterpret_cast<const u32x4 *>(kp + (4 * t * c.D + d) * E);
+        }
+    const bool there = T::DV * m < c.D;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        constexpr int W = BITS8 ? T::DV / 4 : T::DV / 2;
+        const uint32_t *const p = reinterpret_cast<const uint32_t *>(vp + i * c.D * E);
+#pragma unroll
+        for (int w = 0; w < W; ++w) r.v[i][w] = 0;
+        if (there) {
+            if constexpr (W % 4 == 0) {
+#pragma unroll
+                for (int w = 0; w < W; w += 4) {
+                    const u32x4 x = *reinterpret_cast<const u32x4 *>(p + w);
+                    r.v[i][w] = x[0], r.v[i][w + 1] = x[1], r.v[i][w + 2] = x[2], r.v[i][w + 3] = x[3];
+                }
+            } else if constexpr (W == 2) {
+                const u32x2 x = *reinterpret_cast<const u32x2 *>(p);
+                r.v[i][0] = x[0], r.v[i][1] = x[1];
+            } else {
+                r.v[i][0] = p[0];
+            }
+        }
+    }
+    if constexpr (BITS8) {
+        const uint8_t *const ke = c.k_exps + ((m < 8 ? s0 : s1) + tk) * c.groups, *const ve = c.v_exps + ((g < 2 ? s0 : s1) + 8 * g) * c.groups;
+        if constexpr (DP <= 128) {
+            r.ke[0] = ke[0], r.ke[1] = ke[4];
+            const u32x2 x = *reinterpret_cast<const u32x2 *>(ve);
+            r.ve[0] = x[0], r.ve[1] = x[1];
+        } else {
+            r.ke[0] = *reinterpret_cast<const uint16_t *>(ke), r.ke[1] = *reinterpret_cast<const uint16_t *>(ke + 8);
+            const u32x4 x = *reinterpret_cast<const u32x4 *>(ve);
+            r.ve[0] = x[0], r.ve[1] = x[1], r.ve[2] = x[2], r.ve[3] = x[3];
+        }
+    }
+}
+
+// two of a word's four E4M3 codes times a power of two as bf16: exact
+__device__ __forceinline__ uint32_t bf16_of_codes(uint32_t w, bool high, float power)
+{
+    return high ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, power, true))
+                : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, power, false));
+}
+__device__ __forceinline__ float power_of(uint32_t bytes, int at) { return u2f(((bytes >> (8 * at)) & 0xFF) << 23); }
+
+__device__ __forceinline__ bool bf16_pair_finite(uint32_t w) { return (w & 0x7F80u) != 0x7F80u && (w & 0x7F800000u) != 0x7F800000u; }
+
+// state of 16 rows: lane (g, row) holds m and a part of l of its row, and out[j][i] = element DV (4g + i) + j of the row
+template <int DP> struct Rows {
+    float m, l;
+    float4_t o[DP / 16];
+};
+
+// o += values^T x weights; p: the weights of the lane's eight tokens
+template <int DP>
+__device__ __forceinline__ void add_values(u32x4 p, const uint32_t (&v)[8][DP / 32], float4_t (&o)[DP / 16])
+{
+#pragma unroll
+    for (int j = 0; j < DP / 16; ++j) {
+        u32x4 f;                                           // element j of the lane's for its eight tokens
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            f[i] = __builtin_amdgcn_perm(v[2 * i + 1][j / 2], v[2 * i][j / 2], j & 1 ? 0x07060302u : 0x05040100u);
+        o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, f), __builtin_bit_cast(bf16x8_t, p), o[j], 0, 0, 0);
+    }
+}
+
+// One block: scores, running maximum and sum, values.  limit: tokens that the lane's row sees; [low, high]: the least and the most that a row of the tile sees.
+template <int DP, bool BITS8>
+__device__ __forceinline__ void take_block(const Tokens<DP, BITS8> &r, const u32x4 (&q)[DP / 32], float scale2, int limit, int low, int high, int lane, Rows<DP> &s)
+{
+    constexpr int KC = DP / 32, DV = DP / 16;
+    const int g = lane >> 4;
+    float4_t sc[2] = {float4_t{0, 0, 0, 0}, float4_t{0, 0, 0, 0}};
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int c = 0; c < KC; ++c) {
+            u32x4 k;
+            if constexpr (BITS8) {
+                const uint32_t w0 = r.k[t][c / 2][2 * (c & 1)], w1 = r.k[t][c / 2][2 * (c & 1) + 1];
+                const float power = power_of(r.ke[t], c / 4);
+                k = u32x4{bf16_of_codes(w0, false, power), bf16_of_codes(w0, true, power), bf16_of_codes(w1, false, power), bf16_of_codes(w1, true, power)};
+            } else {
+                k = r.k[t][c];
+            }
+            sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, k), __builtin_bit_cast(bf16x8_t, q[c]), sc[t], 0, 0, 0);
+        }
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        x[i] = sc[i >> 2][i & 3] * scale2;
+    }
+    const bool whole = r.t0 + kBlock <= low && r.ok == 3;
+    const bool mine = (r.ok >> (g >> 1)) & 1;
+    if (!whole) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (!mine || r.t0 + 8 * g + i >= limit) x[i] = -INFINITY;
+    }
+    float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+    top = max16_32(top);
+    if (__any(top > s.m)) {
+        const float m = fmaxf(s.m, top);
+        const float by = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(s.m - m);
+        s.l *= by;
+#pragma unroll
+        for (int j = 0; j < DV; ++j) s.o[j] *= by;
+        s.m = m;
+    }
+    const float m = s.m == -INFINITY ? 0.0f : s.m;
+    float w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        w[i] = __builtin_amdgcn_exp2f(x[i] - m);
+        s.l += w[i];
+    }
+    uint32_t v[8][DP / 32];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d) {
+            if constexpr (BITS8) {
+                // heads of more than 128 elements have two groups; the second begins with lane 8's elements
+                const float power = DP > 128 ? power_of(r.ve[i / 2], 2 * (i & 1) + ((lane & 15) >> 3)) : power_of(r.ve[i / 4], i & 3);
+                v[i][d] = bf16_of_codes(r.v[i][d / 2], d & 1, power);
+            } else {
+                v[i][d] = r.v[i][d];
+            }
+        }
+    const u32x4 p = {bf16_pair(w[0], w[1]), bf16_pair(w[2], w[3]), bf16_pair(w[4], w[5]), bf16_pair(w[6], w[7])};
+    if (!whole) {
+        // Tokens that no row of the tile sees may hold anything: zeros in their place.  Values that are not finite reach the rows that see them and no others: then row by row.
+        bool odd = false;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d) {
+                if (!mine || r.t0 + 8 * g + i >= high) v[i][d] = 0;
+                else odd |= !bf16_pair_finite(v[i][d]);
+            }
+        if (__any(odd)) {
+            for (int n = 0; n < kTile; ++n) {
+                const int sees = __shfl(limit, n, 64);
+                uint32_t u[8][DP / 32];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int d = 0; d < DP / 32; ++d) u[i][d] = r.t0 + 8 * g + i < sees ? v[i][d] : 0;
+                float4_t o[DP / 16];
+#pragma unroll
+                for (int j = 0; j < DV; ++j) o[j] = float4_t{0, 0, 0, 0};
+                add_values<DP>(p, u, o);
+                if ((lane & 15) == n)
+#pragma unroll
+                    for (int j = 0; j < DV; ++j) s.o[j] += o[j];
+            }
+            return;
+        }
+    }
+    add_values<DP>(p, v, s.o);
+}
+
+// PREFIX: tiles of all rows against the shared tokens; else of a sequence's rows against its own
+template <int DP, bool BITS8, bool PREFIX>
+__global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attn_kernel(Args a)
+{
+    constexpr int DV = DP / 16, LD = DP + 4;
+    __shared__ int64_t lds[kWaves];
+    __shared__ __align__(16) float part[kWaves][kTile][LD];
+    __shared__ float2_t part_ml[kWaves][kTile];
+    const int head = blockIdx.x % a.c.heads, item = blockIdx.x / a.c.heads;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    const int row = lane & 15, g = lane >> 4;
+
+    int first, count, tile, begin, end, limit, low, high, parts, table_len;
+    const int *table;
+    if constexpr (PREFIX) {
+        tile = item / a.prefix_parts;
+        parts = 2;                                           // never alone: the own tokens follow
+        begin = item % a.prefix_parts * a.prefix_units * kUnit;
+        end = min(begin + a.prefix_units * kUnit, a.b.prefix);
+        first = 0, count = a.N;
+        low = high = limit = a.b.prefix;
+        table = a.b.prefix_table;
+        table_len = (a.b.prefix + (1 << a.c.page_log2) - 1) >> a.c.page_log2;
+    } else {
+        Place p;
+        int part_units;
+        if (!find(a, item, -1, p, part_units, lds)) return;
+        rows_of(a.b, p.b, a.N, first, count);
+        const int len = tokens_of(a.b, a.c, p.b);
+        tile = p.tile, parts = a.b.prefix ? 2 : p.parts;
+        begin = p.part * part_units * kUnit;
+        // the row's token and those before it
+        const auto sees = [&](int r) { return max(0, len - count + min(r / a.G, count - 1) + 1); };
+        limit = sees(tile * kTile + row);
+        low = sees(tile * kTile), high = sees(tile * kTile + kTile - 1);
+        end = min(p.part == p.parts - 1 ? len : begin + part_units * kUnit, high);
+        table = a.b.table + (int64_t)p.b * a.b.width;
+        table_len = a.b.width;
+    }
+    const int rows = count * a.G, r = tile * kTile + row;
+    const bool valid = r < rows;
+    // queries of the tile's rows: elements 32c + 8g .. of step c (8 bits: as the codes' sixteen elements are dealt)
+    u32x4 q[DP / 32];
+    {
+        const uint16_t *const p = a.q + (int64_t)(first + (valid ? r / a.G : 0)) * a.ldq + (int64_t)(head * a.G + (valid ? r % a.G : 0)) * a.c.D;
+#pragma unroll
+        for (int c = 0; c < DP / 32; ++c) {
+            const int d = BITS8 ? 64 * (c / 2) + 16 * g + 8 * (c & 1) : 32 * c + 8 * g;
+            q[c] = u32x4{0, 0, 0, 0};
+            if (valid && d < a.c.D) q[c] = *reinterpret_cast<const bf16x8_at2 *>(p + d);
+        }
+    }
+    Rows<DP> s;
+    s.m = -INFINITY, s.l = 0.0f;
+#pragma unroll
+    for (int j = 0; j < DV; ++j) s.o[j] = float4_t{0, 0, 0, 0};
+    // the waves take blocks in turn; one block is on its way while another is worked on
+    Tokens<DP, BITS8> x, y;
+    int t = begin + wave * kBlock;
+    constexpr int STEP = kWaves * kBlock;
+    if (t < end) load_tokens<DP, BITS8>(a.c, table, table_len, head, t, lane, x);
+    while (t < end) {
+        if (t + STEP < end) load_tokens<DP, BITS8>(a.c, table, table_len, head, t + STEP, lane, y);
+        take_block<DP, BITS8>(x, q, a.scale2, min(limit, end), min(low, end), min(high, end), lane, s);
+        t += STEP;
+        if (t >= end) break;
+        if (t + STEP < end) load_tokens<DP, BITS8>(a.c, table, table_len, head, t + STEP, lane, x);
+        take_block<DP, BITS8>(y, q, a.scale2, min(limit, end), min(low, end), min(high, end), lane, s);
+        t += STEP;
+    }
+    // the four waves' shares: out = sum 2^(m_w - m) out_w
+    s.l = sum16_32(s.l);
+    if (s.l != s.l) s.m = INFINITY;                          // no part that has seen a NaN counts as empty, or is outweighed
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < DV; ++j) part[wave][row][DV * (4 * g + i) + j] = s.o[j][i];
+    if (g == 0) part_ml[wave][row] = float2_t{s.m, s.l};
+    __syncthreads();
+    const int orow = threadIdx.x >> 4, od = (threadIdx.x & 15) * DV;
+    float m = -INFINITY, l = 0.0f, o[DV] = {};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) m = fmaxf(m, part_ml[w][orow].x);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        const float2_t ml = part_ml[w][orow];
+        const float by = ml.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml.x - m);
+        l += ml.y * by;
+#pragma unroll
+        for (int j = 0; j < DV; ++j) o[j] += ml.x == -INFINITY ? 0.0f : part[w][orow][od + j] * by;
+    }
+    const int at = tile * kTile + orow;
+    if (at >= rows || od >= a.c.D) return;
+    if (parts == 1) {
+        const float by = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;                        // nothing seen: zeros; NaN stays
+        uint16_t *const p = a.out + (int64_t)(first + at / a.G) * a.ldo + (int64_t)(head * a.G + at % a.G) * a.c.D + od;
+#pragma unroll
+        for (int j = 0; j < DV; j += 2) {
+            const uint32_t w = bf16_pair(o[j] * by, o[j + 1] * by);
+            p[j] = (uint16_t)w, p[j + 1] = (uint16_t)(w >> 16);
+        }
+    } else {
+        const int64_t slot = ((int64_t)(PREFIX ? a.slots + item : item) * a.c.heads + head) * kTile + orow;
+        float *const p = a.part_o + slot * a.c.D + od;
+#pragma unroll
+        for (int j = 0; j < DV; j += 4) *reinterpret_cast<float4_t *>(p + j) = float4_t{o[j], o[j + 1], o[j + 2], o[j + 3]};
+        if (od == 0) a.part_ml[slot] = float2_t{m, l};
+    }
+}
+
+// Joins the parts of a row and query head: D / 4 lanes a part, the parts dealt to the lane groups, their shares added through LDS.
+template <int DP>
+__global__ __launch_bounds__(kThreads) void attn_join_kernel(Args a)
+{
+    constexpr int L = DP / 4, GROUPS = kThreads / L;          // lanes of a part; parts at once
+    __shared__ int64_t lds[kWaves];
+    __shared__ float4_t sums[GROUPS][L];
+    __shared__ float2_t mls[GROUPS];
+    const int head = blockIdx.x % a.Hq, n = blockIdx.x / a.Hq;
+    const int b = sequence_of(a.b, n);
+    if (b < 0) return;
+    int first, count;
+    rows_of(a.b, b, a.N, first, count);
+    if (n < first || n >= first + count) return;
+    Place p;
+    int part_units;
+    find(a, -1, b, p, part_units, lds);
+    if (p.parts == 1 && !a.b.prefix) return;                  // written already
+    if (p.base + (int64_t)tiles_of(count, a.G) * p.parts > a.slots) return;      // starts that name rows twice
+    const int kv = head / a.G, in_seq = (n - first) * a.G + head % a.G, in_all = n * a.G + head % a.G;
+    const int total = p.parts + a.prefix_parts;
+    const int lane = threadIdx.x % L, group = threadIdx.x / L;
+    const auto slot_of = [&](int i) {                         // row of the i-th part: own parts first
+        return i < p.parts ? ((p.base + in_seq / kTile * p.parts + i) * a.c.heads + kv) * kTile + in_seq % kTile
+                           : ((int64_t)(a.slots + in_all / kTile * a.prefix_parts + i - p.parts) * a.c.heads + kv) * kTile + in_all % kTile;
+    };
+    float m = -INFINITY, l = 0.0f;
+    float4_t o = {0, 0, 0, 0};
+    for (int i = group; i < total; i += GROUPS) {
+        const int64_t slot = slot_of(i);
+        const float2_t ml = a.part_ml[slot];
+        const float4_t v = 4 * lane < a.c.D ? *reinterpret_cast<const float4_t *>(a.part_o + slot * a.c.D + 4 * lane) : float4_t{0, 0, 0, 0};
+        const float top = fmaxf(m, ml.x);
+        if (top == -INFINITY) continue;
+        const float old = __builtin_amdgcn_exp2f(m - top), by = __builtin_amdgcn_exp2f(ml.x - top);
+        l = l * old + ml.y * by;
+        o = ml.x == -INFINITY ? o * old : o * old + v * by;
+        m = top;
+    }
+    sums[group][lane] = o;
+    if (lane == 0) mls[group] = float2_t{m, l};
+    __syncthreads();
+    if (group != 0 || 4 * lane >= a.c.D) return;
+    for (int i = 0; i < GROUPS; ++i) m = fmaxf(m, mls[i].x);
+    l = 0.0f;
+    o = float4_t{0, 0, 0, 0};
+    for (int i = 0; i < GROUPS; ++i) {
+        const float2_t ml = mls[i];
+        if (ml.x == -INFINITY) continue;
+        const float by = __builtin_amdgcn_exp2f(ml.x - m);
+        l += ml.y * by;
+        o += sums[i][lane] * by;
+    }
+    const float by = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
+    uint16_t *const out = a.out + (int64_t)n * a.ldo + (int64_t)head * a.c.D + 4 * lane;
+    const uint32_t w0 = bf16_pair(o[0] * by, o[1] * by), w1 = bf16_pair(o[2] * by, o[3] * by);
+    out[0] = (uint16_t)w0, out[1] = (uint16_t)(w0 >> 16), out[2] = (uint16_t)w1, out[3] = (uint16_t)(w1 >> 16);
+}
+
+// ---- how a call is cut -------------------------------------------------------------------------
+
+struct Cut {
+    int target, prefix_units, prefix_parts;
+    int64_t slots, items, prefix_items;        // of a key head
+};
+
+Cut cut_of(int64_t N, int Hq, int heads, int B, int64_t prefix)
+{
+    Cut p;
+    const int64_t G = Hq / heads, tiles = (N * G + kTile - 1) / kTile;
+    // Enough tiles of several rows: nothing is cut.  Else the own tokens are cut into about kGroups parts, also where there are that many sequences: their lengths differ.
+    const bool cut = N <= 2 * B || tiles * heads < kGroups;
+    p.target = cut ? (int)((kGroups + heads - 1) / heads) : 0;
+    p.items = p.target + (N * G) / kTile + B;            // every tile at least once, and the cuts
+    p.slots = cut || prefix ? p.items : 0;
+    p.prefix_units = p.prefix_parts = 0;
+    p.prefix_items = 0;
+    if (prefix > 0) {
+        const int64_t units = (prefix + kUnit - 1) / kUnit, want = (kGroups / 2 + tiles * heads - 1) / (tiles * heads);
+        int64_t part = (units + want - 1) / want;
+        part = part < kMinUnits ? kMinUnits : part;
+        p.prefix_units = (int)part;
+        p.prefix_parts = (int)((units + part - 1) / part);
+        p.prefix_items = tiles * p.prefix_parts;
+    }
+    return p;
+}
+
+int64_t rows_of_parts(const Cut &p, int heads) { return (p.slots + p.prefix_items) * heads * kTile; }
+
+template <int DP, bool BITS8>
+hipError_t run(const Args &a, const Cut &p, hipStream_t st)
+{
+    if (p.prefix_items > 0) attn_kernel<DP, BITS8, true><<<(unsigned)(p.prefix_items * a.c.heads), kThreads, 0, st>>>(a);
+    attn_kernel<DP, BITS8, false><<<(unsigned)(p.items * a.c.heads), kThreads, 0, st>>>(a);
+    if (p.slots > 0) attn_join_kernel<DP><<<(unsigned)((int64_t)a.N * a.Hq), kThreads, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t attn_workspace_bytes(int64_t N, int Hq, int heads, int D, int B, int64_t prefix)
+{
+    const int64_t rows = rows_of_parts(cut_of(N, Hq, heads, B, prefix), heads);
+    return (size_t)(rows * D * 4 + rows * 8);
+}
+
+hipError_t launch_attn(const uint16_t *q, int64_t ldq, int64_t N, int Hq, const KvCache &c, const KvBatch &b, float scale, uint16_t *out, int64_t ldo, void *ws,
+                       hipStream_t st)
+{
+    const Cut p = cut_of(N, Hq, c.heads, b.B, b.prefix);
+    Args a{q, ldq, out, ldo, (int)N, Hq, Hq / c.heads, c, b, scale * 1.44269504088896340736f, p.target, (int)p.slots, p.prefix_units, p.prefix_parts, nullptr, nullptr};
+    a.part_o = static_cast<float *>(ws);
+    a.part_ml = reinterpret_cast<float2_t *>(a.part_o + rows_of_parts(p, c.heads) * c.D);
+    if (c.D <= 64) return c.bits8 ? run<64, true>(a, p, st) : run<64, false>(a, p, st);
+    if (c.D <= 128) return c.bits8 ? run<128, true>(a, p, st) : run<128, false>(a, p, st);
+    return c.bits8 ? run<256, true>(a, p, st) : run<256, false>(a, p, st);
+}
+
+}  // namespace tj

@@ -1,0 +1,503 @@
+// The choice of one token per row of logits x [N x V] from a given number u.
+//
+//   w = exp((x - max) / T);  order: by x from the largest down, equal ones by index;  kept: a run of the order from its first token on, as long as top_k,
+//   top_p and min_p let it be;  W = sum of the kept w;  the token is the first whose sum of w with those before it exceeds u W.
+//
+// Nothing is sorted.  The order is cut into bins 1/32 of a unit of x / T wide (a function of x that never falls as x grows, whatever it is rounded to), and a bin's weight and number of tokens say which bin a
+// border lies in: one kernel makes the bins of slices of a row, a second joins them, and takes from the row the tokens of the few bins that matter.  Inside a bin a place is found by further
+// cuts, of the 64-bit number (x, index) that the order goes by.
+//
+// Weights are fixed-point numbers, 2^43 for the largest: their sums do not depend on the order of the additions, which LDS atomics leave open.
+#include "rowwise.h"
+#include "seq_ops.h"
+
+namespace tj {
+
+namespace {
+
+constexpr int kThreads = 1024;
+constexpr int kWaves = kThreads / 64;
+constexpr int kBins = 1024;                   // the last one: 31.9 and more below the largest, where weights are 0
+constexpr int kCuts = 1024;                   // cuts of a bin
+constexpr int kFew = 64;                      // tokens among which a wave finds the place
+constexpr int kList = 4096;                   // tokens that are taken out of a row; where there are more, they stay in it
+constexpr int kMaxSlices = 8;
+constexpr double kOne = 8796093022208.0;      // 2^43
+
+// what a slice leaves
+struct Slice {
+    float top;                // its largest logit
+    int index;                // where that is first
+};
+
+struct Weight {
+    double top, step;         // largest logit, log2 e / T
+    // round(2^43 * 2^(-(top - x) step)); the Taylor series of 2^-f about f = 1/2 to degree 11 is off by 2^-46
+    __device__ __forceinline__ uint64_t operator()(float x) const
+    {
+        const double y = (top - (double)x) * step;
+        if (!(y < 45.0)) return 0;
+        const double n = floor(y), z = (0.5 - (y - n)) * 0.69314718055994530942;
+        double p = 1.0 / 39916800;
+        p = fma(p, z, 1.0 / 3628800);
+        p = fma(p, z, 1.0 / 362880);
+        p = fma(p, z, 1.0 / 40320);
+        p = fma(p, z, 1.0 / 5040);
+        p = fma(p, z, 1.0 / 720);
+        p = fma(p, z, 1.0 / 120);
+        p = fma(p, z, 1.0 / 24);
+        p = fma(p, z, 1.0 / 6);
+        p = fma(p, z, 0.5);
+        p = fma(p, z, 1.0);
+        p = fma(p, z, 1.0);
+        // times 2^(43 - n) / sqrt 2, and rounded to an integer in the low bits of a number from 2^52 on; the largest weight is 2^43 itself
+        if (y == 0.0) return (uint64_t)kOne;
+        const double scale = __longlong_as_double((long long)(1023 + 43 - (int)n) << 52) * 0.70710678118654752440;
+        return (uint64_t)__double_as_longlong(fma(p, scale, 4503599627370496.0)) & 0xFFFFFFFFFFFFFull;
+    }
+};
+
+// bin number of a logit, counted from the row's own zero upwards
+__device__ __forceinline__ float bin_of(float x, float per_unit)
+{
+    return floorf(fminf(fmaxf(x * per_unit, -0x1p30f), 0x1p30f));
+}
+__device__ __forceinline__ int bin_below(float anchor, float x, float per_unit)
+{
+    return (int)fminf(anchor - bin_of(x, per_unit), (float)(kBins - 1));
+}
+// bins per unit of x: 32 / T, and no more than 2^20, with which the last bin's weights are 0 still
+__device__ __forceinline__ float bins_per_unit(float T) { return fminf(32.0f / T, 0x1p20f); }
+
+__device__ __forceinline__ float temperature_of(const SampleArgs &a, int64_t n) { return a.temperature ? a.temperature[n] : 1.0f; }
+__device__ __forceinline__ bool is_greedy(float T) { return !(T > 0.0f); }
+
+// A logit as the order sees it: NaN as -infinity, -0 as 0; where the largest is +infinity, 0 for it and -infinity for everything else.
+__device__ __forceinline__ float seen(float x, bool infinite)
+{
+    if (infinite) return x == INFINITY ? 0.0f : -INFINITY;
+    return x != x ? -INFINITY : x + 0.0f;
+}
+
+// eight logits from `at` on, -infinity behind the end
+template <bool F32> __device__ __forceinline__ void logits8(const SampleArgs &a, int64_t row, int at, int end, float (&v)[8])
+{
+    const RowSrc s{a.logits, nullptr, a.ld, 0, F32 ? kF32 : kBf16};
+    if (at + 8 <= end) {
+        widen(load8<F32 ? kF32 : kBf16, true, false>(s, row, at, at + 8), v);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        v[i] = -INFINITY;
+        if (at + i < end) {
+            if constexpr (F32) v[i] = static_cast<const float *>(a.logits)[row * a.ld + at + i];
+            else v[i] = u2f((uint32_t) static_cast<const uint16_t *>(a.logits)[row * a.ld + at + i] << 16);
+        }
+    }
+}
+
+// the larger logit, of equal ones the one that comes first
+__device__ __forceinline__ void larger(float &x, int &at, float y, int where)
+{
+    if (y > x || (y == x && where < at)) x = y, at = where;
+}
+
+// ws of a row: slices, then their bins' weights, then their bins' numbers of tokens
+__host__ __device__ __forceinline__ size_t row_bytes(int slices) { return (size_t)slices * (sizeof(Slice) + kBins * 12); }
+struct RowSpace {
+    uint64_t *sums;
+    uint32_t *counts;
+    Slice *slices;
+};
+__device__ __forceinline__ RowSpace row_space(char *ws, int64_t row, int slices)
+{
+    char *const p = ws + row * row_bytes(slices);
+    return RowSpace{reinterpret_cast<uint64_t *>(p), reinterpret_cast<uint32_t *>(p + (size_t)slices * kBins * 8), reinterpret_cast<Slice *>(p + (size_t)slices * kBins * 12)};
+}
+
+template <bool F32> __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs a, char *ws, int slices, int slice_len)
+{
+    __shared__ uint64_t sums[kBins];
+    __shared__ uint32_t counts[kBins];
+    __shared__ float tops[kWaves];
+    __shared__ int where[kWaves];
+    const int64_t row = blockIdx.x / slices;
+    const int slice = blockIdx.x % slices, begin = slice * slice_len, end = min((int)a.V, begin + slice_len);
+    const RowSpace out = row_space(ws, row, slices);
+    float top = -INFINITY;
+    int at = 0x7FFFFFFF;
+    for (int i = begin + 8 * threadIdx.x; i < end; i += 8 * kThreads) {
+        float v[8];
+        logits8<F32>(a, row, i, end, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (v[j] > top) top = v[j], at = i + j;
+    }
+    for (int o = 1; o < 64; o <<= 1) larger(top, at, __shfl_xor(top, o, 64), __shfl_xor(at, o, 64));
+    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top, where[threadIdx.x >> 6] = at;
+    sums[threadIdx.x] = 0;
+    counts[threadIdx.x] = 0;
+    __syncthreads();
+    top = tops[0], at = where[0];
+    for (int w = 1; w < kWaves; ++w) larger(top, at, tops[w], where[w]);
+    if (threadIdx.x == 0) out.slices[slice] = Slice{top, at};
+    const float T = temperature_of(a, row);
+    if (is_greedy(T) || top == -INFINITY) return;
+    const bool infinite = top == INFINITY, count = a.top_k != nullptr;
+    if (infinite) top = 0.0f;
+    const Weight weight{(double)top, 1.44269504088896340736 / (double)T};
+    const float per_unit = bins_per_unit(T), anchor = bin_of(top, per_unit);
+    for (int i = begin + 8 * threadIdx.x; i < end; i += 8 * kThreads) {
+        float v[8];
+        logits8<F32>(a, row, i, end, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float x = seen(v[j], infinite);
+            if (x == -INFINITY) continue;
+            const int b = bin_below(anchor, x, per_unit);
+            if (b >= kBins - 1) continue;
+            atomicAdd(reinterpret_cast<unsigned long long *>(&sums[b]), (unsigned long long)weight(x));
+            if (count) atomicAdd(&counts[b], 1u);
+        }
+    }
+    __syncthreads();
+    out.sums[slice * kBins + threadIdx.x] = sums[threadIdx.x];
+    if (count) out.counts[slice * kBins + threadIdx.x] = counts[threadIdx.x];
+}
+
+// (weight, number of tokens) up to and with each thread's; all threads of the workgroup call it
+__device__ __forceinline__ void scan(double &w, uint32_t &c, double *lw, uint32_t *lc)
+{
+    for (int o = 1; o < 64; o <<= 1) {
+        const double x = __shfl_up(w, o, 64);
+        const uint32_t y = __shfl_up(c, o, 64);
+        if ((int)(threadIdx.x & 63) >= o) w += x, c += y;
+    }
+    const int wave = threadIdx.x >> 6;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 63) lw[wave] = w, lc[wave] = c;
+    __syncthreads();
+    double x = 0.0;
+    uint32_t y = 0;
+    for (int i = 0; i < kWaves; ++i)
+        if (i < wave) x += lw[i], y += lc[i];
+    w += x, c += y;
+}
+
+// A row as its second kernel sees it.
+struct Row {
+    Weight weight;
+    float per_unit, anchor;
+    bool infinite;
+    int64_t row;
+    int listed;                // tokens in the list; -1: there were more than it holds, and they are looked up in the row
+};
+
+struct Shared {
+    double ends[kBins];        // weight of the row's tokens up to and with each bin
+    uint32_t count_ends[kBins];
+    uint64_t sums[kCuts];
+    uint32_t counts[kCuts];
+    uint32_t keys[kList], index[kList];
+    double lw[kWaves];
+    uint32_t lc[kWaves];
+    uint64_t low, high;
+    uint64_t few[kFew], few_weight[kFew];
+    double found[2];
+    int bins[8];
+    uint32_t n;
+    int token;
+};
+
+// ascending with the order: larger logits have smaller numbers
+__device__ __forceinline__ uint32_t key_of(float x)
+{
+    const uint32_t b = f2u(x);
+    return b & 0x80000000u ? b : ~(b | 0x80000000u);
+}
+__device__ __forceinline__ float logit_of(uint32_t k) { return u2f(k & 0x80000000u ? k : ~k & 0x7FFFFFFFu); }
+
+// do(place in the order as a number, logit) for every token of bin `bin`
+template <bool F32, typename Do> __device__ __forceinline__ void each(const SampleArgs &a, const Row &r, Shared &s, int bin, Do &&what)
+{
+    if (r.listed >= 0) {
+        for (int i = threadIdx.x; i < r.listed; i += kThreads) {
+            const float x = logit_of(s.keys[i]);
+            if (bin_below(r.anchor, x, r.per_unit) == bin) what((uint64_t)s.keys[i] << 32 | s.index[i], x);
+        }
+    } else {
+        for (int i = 8 * threadIdx.x; i < (int)a.V; i += 8 * kThreads) {
+            float v[8];
+            logits8<F32>(a, r.row, i, (int)a.V, v);
+            for (int j = 0; j < 8; ++j) {
+                const float x = seen(v[j], r.infinite);
+                if (x != -INFINITY && bin_below(r.anchor, x, r.per_unit) == bin) what((uint64_t)key_of(x) << 32 | (uint32_t)(i + j), x);
+            }
+        }
+    }
+}
+
+// The token of bin `bin` that `target` falls on: by weight the first with which the sum of weights exceeds it, by rank the target-th of the order (counted from 0).  s.found: the
+// weight of what comes before it, and with it; s.token: which it is.  All threads of the workgroup call it.
+template <bool F32, bool RANK> __device__ void locate(const SampleArgs &a, const Row &r, Shared &s, int bin, double target)
+{
+    double before = bin ? s.ends[bin - 1] : 0.0;
+    uint32_t rank = bin ? s.count_ends[bin - 1] : 0;
+    __syncthreads();
+    if (threadIdx.x == 0) s.low = ~0ull, s.high = 0;
+    __syncthreads();
+    unsigned long long least = ~0ull, most = 0;
+    each<F32>(a, r, s, bin, [&](uint64_t k, float) {
+        least = k < least ? k : least;
+        most = k > most ? k : most;
+    });
+    for (int o = 1; o < 64; o <<= 1) {
+        const unsigned long long x = __shfl_xor(least, o, 64), y = __shfl_xor(most, o, 64);
+        least = x < least ? x : least;
+        most = y > most ? y : most;
+    }
+    if ((threadIdx.x & 63) == 0 && least <= most) {
+        atomicMin(reinterpret_cast<unsigned long long *>(&s.low), least);
+        atomicMax(reinterpret_cast<unsigned long long *>(&s.high), most);
+    }
+    __syncthreads();
+    uint64_t low = s.low;
+    const uint64_t span = s.high - low;
+    int shift = span >> 10 ? 54 - __clzll((long long)span) : 0;           // span >> shift < 1024
+    for (;;) {
+        s.sums[threadIdx.x] = 0;
+        s.counts[threadIdx.x] = 0;
+        if (threadIdx.x == 0) s.bins[7] = -1;
+        __syncthreads();
+        each<F32>(a, r, s, bin, [&](uint64_t k, float x) {
+            const uint64_t c = (k - low) >> shift;
+            if (k < low || c >= kCuts) return;
+            atomicAdd(reinterpret_cast<unsigned long long *>(&s.sums[c]), (unsigned long long)r.weight(x));
+            atomicAdd(&s.counts[c], 1u);
+        });
+        __syncthreads();
+        const uint32_t here = s.counts[threadIdx.x];
+        double w = (double)s.sums[threadIdx.x];
+        const double own = w;
+        uint32_t c = here;
+        scan(w, c, s.lw, s.lc);
+        w += before;
+        c += rank;
+        // the cut in which the sum passes the target; the last one that weighs anything where none does
+        const bool passes = RANK ? (double)c > target : w > target, passed = RANK ? (double)(c - here) > target : w - own > target;
+        if (here && passes && !passed) atomicMax(&s.bins[7], kCuts + (kCuts - (int)threadIdx.x));
+        else if (RANK ? here > 0 : own > 0.0) atomicMax(&s.bins[7], (int)threadIdx.x);
+        __syncthreads();
+        const int cut = s.bins[7] >= kCuts ? 2 * kCuts - s.bins[7] : s.bins[7];
+        if ((int)threadIdx.x == cut) s.found[0] = w - own, s.n = c - here;
+        __syncthreads();
+        before = s.found[0];
+        rank = s.n;
+        low += (uint64_t)cut << shift;
+        const uint32_t tokens = s.counts[cut];
+        __syncthreads();
+        if (tokens <= kFew) break;                           // with shift = 0 there is one
+        shift = shift > 10 ? shift - 10 : 0;
+    }
+    if (threadIdx.x == 0) s.n = 0;
+    __syncthreads();
+    each<F32>(a, r, s, bin, [&](uint64_t k, float x) {
+        if (k < low || (k - low) >> shift) return;
+        const uint32_t i = atomicAdd(&s.n, 1u);
+        s.few[i] = k;
+        s.few_weight[i] = r.weight(x);
+    });
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        const int n = (int)s.n, i = threadIdx.x;
+        uint64_t sum = 0, behind = 0;
+        uint32_t at = 0;
+        if (i < n) {
+            for (int j = 0; j < n; ++j) {
+                if (s.few[j] < s.few[i]) sum += s.few_weight[j], ++at;
+                else behind += s.few_weight[j];
+            }
+            const double b = before + (double)sum, e = before + (double)(sum + s.few_weight[i]);
+            // the first that passes the target; if none does, the last that weighs anything
+            const bool passes = RANK ? (double)(rank + at) == target : e > target && !(b > target && at > 0);
+            const bool last = !RANK && e <= target && s.few_weight[i] > 0 && behind == s.few_weight[i];
+            if (passes || last) s.found[0] = b, s.found[1] = e, s.token = (int)(uint32_t)s.few[i];
+        }
+    }
+    __syncthreads();
+}
+
+template <bool F32> __global__ __launch_bounds__(kThreads) void sample_choose_kernel(SampleArgs a, char *ws, int slices)
+{
+    __shared__ Shared s;
+    const int64_t row = blockIdx.x;
+    const int t = threadIdx.x;
+    const RowSpace in = row_space(ws, row, slices);
+    float top = -INFINITY;
+    int at = 0x7FFFFFFF;
+    for (int i = 0; i < slices; ++i) larger(top, at, in.slices[i].top, in.slices[i].index);
+    const float T = temperature_of(a, row);
+    if (top == -INFINITY || is_greedy(T)) {
+        if (t == 0) a.tokens[row] = top == -INFINITY ? -1 : at;
+        return;
+    }
+    Row r;
+    r.infinite = top == INFINITY;
+    if (r.infinite) top = 0.0f;
+    r.weight = Weight{(double)top, 1.44269504088896340736 / (double)T};
+    r.per_unit = bins_per_unit(T);
+    r.anchor = bin_of(top, r.per_unit);
+    r.row = row;
+    r.listed = 0;
+    // The slices' bins, moved to where they lie below the row's largest and scaled by their own.
+    double w = 0.0;
+    uint32_t c = 0;
+    for (int i = 0; i < slices; ++i) {
+        float st = in.slices[i].top;
+        if (st == -INFINITY || (r.infinite && st != INFINITY)) continue;
+        if (r.infinite) st = 0.0f;
+        const float off = r.anchor - bin_of(st, r.per_unit);
+        if (!(off < (float)(kBins - 1))) continue;
+        const int b = t - (int)off;
+        if (b < 0 || t >= kBins - 1) continue;
+        w += (double)in.sums[i * kBins + b] * exp2(-(r.weight.top - (double)st) * r.weight.step);
+        if (a.top_k) c += in.counts[i * kBins + b];
+    }
+    const double own = w;
+    const uint32_t own_count = c;
+    scan(w, c, s.lw, s.lc);
+    s.ends[t] = w;
+    s.count_ends[t] = c;
+    if (t < 8) s.bins[t] = -1;
+    if (t == 0) s.n = 0;
+    __syncthreads();
+    const double total = s.ends[kBins - 1];
+    const uint32_t tokens = s.count_ends[kBins - 1];
+    const double begin = t ? s.ends[t - 1] : 0.0;
+    // bins[i]: the bin that a sum falls in, the last one with weight where it is beyond all
+    const auto bin_at = [&](int i, double sum) {
+        if (own > 0.0 && begin <= sum && (sum < w || w >= total)) atomicMax(&s.bins[i], t);
+    };
+    const int k = a.top_k ? a.top_k[row] : 0;
+    const bool by_k = k >= 1 && (uint32_t)k < tokens;
+    float p = a.top_p ? a.top_p[row] : 1.0f;
+    const bool by_p = p < 1.0f;
+    if (by_p && !(p > 0.0f)) p = 0.0f;
+    float m = a.min_p ? a.min_p[row] : 0.0f;
+    const bool by_m = m > 0.0f;
+    if (m > 1.0f) m = 1.0f;
+    float uf = a.u[row];
+    uf = uf > 0.0f ? fminf(uf, 0x1.fffffep-1f) : 0.0f;
+    const double u = (double)uf;
+    // 0: the bin of the k-th token
+    if (by_k && own_count && c - own_count < (uint32_t)k && (uint32_t)k <= c) s.bins[0] = t;
+    __syncthreads();
+    const int kbin = s.bins[0];
+    const double least_k = by_k ? (kbin ? s.ends[kbin - 1] : 0.0) : total, most_k = by_k ? s.ends[kbin] : total;
+    // 1, 2: the first and the last bin in which the border of top_p can lie
+    if (by_p) bin_at(1, (double)p * least_k), bin_at(2, (double)p * most_k);
+    // 3, 4: of min_p, whose border is at log2(1 / m) / step below the largest; one bin more on either side, for the roundings
+    int m0 = kBins - 2, m1 = kBins - 2;
+    if (by_m) {
+        const float edge = (float)(r.weight.top + log2((double)m) / r.weight.step);
+        const int e = edge == edge ? bin_below(r.anchor, edge, r.per_unit) : 0;
+        m0 = max(0, min(e - 1, kBins - 2)), m1 = max(0, min(e + 1, kBins - 2));
+    }
+    __syncthreads();
+    const int p0 = s.bins[1], p1 = s.bins[2];
+    double least = least_k, most = most_k;
+    if (by_p) least = fmin(least, p0 ? s.ends[p0 - 1] : 0.0), most = fmin(most, s.ends[p1]);
+    if (by_m) least = fmin(least, m0 ? s.ends[m0 - 1] : 0.0), most = fmin(most, s.ends[m1]);
+    least = fmax(least, kOne), most = fmax(most, kOne);
+    bin_at(5, u * least * (1.0 - 0x1p-40));
+    bin_at(6, u * most * (1.0 + 0x1p-40));
+    __syncthreads();
+    const int u0 = s.bins[5], u1 = s.bins[6];
+    const auto wanted = [&](int b) {
+        return (b >= u0 && b <= u1) || (by_k && b == kbin) || (by_p && b >= p0 && b <= p1) || (by_m && b >= m0 && b <= m1);
+    };
+    // those bins' tokens, out of the row; as many as there are where they fit
+    for (int i = 8 * t; i < (int)a.V; i += 8 * kThreads) {
+        float v[8];
+        logits8<F32>(a, row, i, (int)a.V, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float x = seen(v[j], r.infinite);
+            if (x == -INFINITY || !wanted(bin_below(r.anchor, x, r.per_unit))) continue;
+            const uint32_t to = atomicAdd(&s.n, 1u);
+            if (to < kList) s.keys[to] = key_of(x), s.index[to] = (uint32_t)(i + j);
+        }
+    }
+    __syncthreads();
+    r.listed = s.n <= kList ? (int)s.n : -1;
+    __syncthreads();
+    // what the filters leave, as a sum of weights
+    double kept = total;
+    if (by_k) {
+        locate<F32, true>(a, r, s, kbin, (double)(k - 1));
+        kept = s.found[1];
+    }
+    if (by_p) {
+        const double target = (double)p * kept;
+        __syncthreads();
+        if (t == 0) s.bins[1] = -1;
+        __syncthreads();
+        bin_at(1, target);
+        __syncthreads();
+        locate<F32, false>(a, r, s, min(max(s.bins[1], p0), p1), target);
+        kept = fmin(kept, s.found[0] == target ? s.found[0] : s.found[1]);
+    }
+    if (by_m) {
+        // the tokens of the bins around the border that are heavy enough, after all those in front of them
+        uint64_t sum = 0;
+        for (int b = m0; b <= m1; ++b)
+            each<F32>(a, r, s, b, [&](uint64_t, float x) {
+                if (exp2(-(r.weight.top - (double)x) * r.weight.step) >= (double)m) sum += r.weight(x);
+            });
+        double all = (double)sum;
+        uint32_t none = 0;
+        scan(all, none, s.lw, s.lc);
+        if (t == kThreads - 1) s.found[0] = all + (m0 ? s.ends[m0 - 1] : 0.0);
+        __syncthreads();
+        kept = fmin(kept, s.found[0]);
+    }
+    kept = fmax(kept, kOne);                                 // the first token stays
+    const double target = u * kept;
+    __syncthreads();
+    if (t == 0) s.bins[5] = -1;
+    __syncthreads();
+    bin_at(5, target);
+    __syncthreads();
+    locate<F32, false>(a, r, s, min(max(s.bins[5], u0), u1), target);
+    if (t == 0) a.tokens[row] = s.token;
+}
+
+// Slices of a row: enough workgroups for two a CU, as long as a slice gives each thread eight logits.
+int slices_of(int64_t N, int64_t V)
+{
+    int64_t s = 512 / N;
+    const int64_t most = V / (8 * kThreads);
+    s = s < most ? s : most;
+    return (int)(s < 1 ? 1 : s > kMaxSlices ? kMaxSlices : s);
+}
+
+template <bool F32> hipError_t run(const SampleArgs &a, char *ws, hipStream_t st)
+{
+    const int slices = slices_of(a.N, a.V);
+    const int len = (int)(((a.V + slices - 1) / slices + 7) / 8 * 8);
+    sample_bins_kernel<F32><<<(unsigned)(a.N * slices), kThreads, 0, st>>>(a, ws, slices, len);
+    sample_choose_kernel<F32><<<(unsigned)a.N, kThreads, 0, st>>>(a, ws, slices);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t sample_workspace_bytes(int64_t N, int64_t V) { return (size_t)N * row_bytes(slices_of(N, V)); }
+
+hipError_t launch_sample(const SampleArgs &a, void *ws, hipStream_t st)
+{
+    return a.f32 ? run<true>(a, static_cast<char *>(ws), st) : run<false>(a, static_cast<char *>(ws), st);
+}
+
+}  // namespace tj
