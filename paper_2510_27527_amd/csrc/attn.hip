@@ -132,78 +132,89 @@ __device__ __forceinline__ float sum16_32(float v)
 // Products: scores^T [tokens x rows] = K Q^T and out^T [D x rows] += V^T P^T, 16 x 16 x 32 each.  The tokens of a block are dealt to the rows of the two score tiles so that lane
 // (g, row) (g = lane / 16) ends up with tokens 8g .. 8g + 7 of its row, which is what the second product takes from it.  Values come as rows of tokens
 // and are turned in registers: eight tokens x D / 16 elements a lane.
-template <int DP, bool BITS8> struct Tokens {
-    static constexpr int KC = DP / 32;                   // steps of the first product
-    static constexpr int DV = DP / 16;                   // elements of a value that a lane holds
-    u32x4 k[2][BITS8 ? KC / 2 : KC];                     // [tile][step]: eight elements a step (8 bits: sixteen, two steps)
-    uint32_t v[8][BITS8 ? DV / 4 : DV / 2];              // [token][elements]
-    uint32_t ke[2];                                      // 8 bits: exponents of the lane's token of each tile, a byte a group
-    uint32_t ve[4];                                      // and of tokens 8g ..
-    uint32_t ok;                                         // bit h: tokens 16h .. of the block lie in a page of the cache
-    int t0;
+template <int DP, bool BITS8> struct Keys {
+    static constexpr int STEPS = BITS8 ? DP / 64 : DP / 32;
+    u32x4 k[2][STEPS];                                   // [tile][step]: eight elements a step of the product (8 bits: sixteen, two steps)
+    uint32_t e[2];                                       // 8 bits: exponents of the lane's token of each tile, a byte a group
+};
+template <int DP, bool BITS8> struct Values {
+    static constexpr int WORDS = BITS8 ? DP / 64 : DP / 32;
+    uint32_t v[8][WORDS];                                // [token][elements]
+    uint32_t e[4];                                       // 8 bits: exponents of the eight tokens
+};
+// Where the two halves of a block lie: first byte of the head's tokens 0 .. 15 and, less 16 tokens, 16 .. 31, counted in tokens; bit h of ok: half h lies in a page of the cache.
+struct Spot {
+    int64_t s0, s1;
+    uint32_t ok;
 };
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
-template <int DP, bool BITS8>
-__device__ __forceinline__ void load_tokens(const KvCache &c, const int *table, int table_len, int head, int t0, int lane, Tokens<DP, BITS8> &r)
+__device__ __forceinline__ Spot spot_of(const KvCache &c, int head, int t0, int p0, int p1)
 {
-    using T = Tokens<DP, BITS8>;
+    const int mask = (1 << c.page_log2) - 1;
+    return Spot{(((int64_t)(p0 < 0 ? 0 : p0) * c.heads + head) << c.page_log2) + (t0 & mask), (((int64_t)(p1 < 0 ? 0 : p1) * c.heads + head) << c.page_log2) + ((t0 + 16) & mask) - 16,
+                (uint32_t)(p0 >= 0) | (uint32_t)(p1 >= 0) << 1};
+}
+
+template <int DP, bool BITS8> __device__ __forceinline__ void load_keys(const KvCache &c, Spot s, int lane, Keys<DP, BITS8> &r)
+{
+    constexpr int E = BITS8 ? 1 : 2, STEP = 64 / E;      // elements that four lanes take with 16 bytes each
     const int m = lane & 15, g = lane >> 4;
-    const int i0 = t0 >> c.page_log2, i1 = (t0 + 16) >> c.page_log2;
-    const int p0 = uniform(i0 < table_len ? table[i0] : -1), p1 = uniform(i1 < table_len ? table[i1] : -1);
-    const bool ok0 = p0 >= 0 && p0 < c.pages, ok1 = p1 >= 0 && p1 < c.pages;
-    r.ok = (uint32_t)ok0 | (uint32_t)ok1 << 1;
-    r.t0 = t0;
-    // tokens of this head in front of the two halves' first
-    const int64_t s0 = (((int64_t)(ok0 ? p0 : 0) * c.heads + head) << c.page_log2) + (t0 & ((1 << c.page_log2) - 1));
-    const int64_t s1 = (((int64_t)(ok1 ? p1 : 0) * c.heads + head) << c.page_log2) + ((t0 + 16) & ((1 << c.page_log2) - 1)) - 16;
-    constexpr int E = BITS8 ? 1 : 2;
-    const char *const k = static_cast<const char *>(c.k), *const v = static_cast<const char *>(c.v);
-    const int tk = (m >> 2) * 8 + (m & 3);               // token of the first tile's row m, the second has the one four further on
-    const char *const kp = k + ((m < 8 ? s0 : s1) + tk) * (c.D * E);
-    const char *const vp = v + ((g < 2 ? s0 : s1) + 8 * g) * (c.D * E) + T::DV * m * E;
-    constexpr int STEP = 4 * 16 / E;                     // elements that four lanes take with 16 bytes each
+    const int64_t near = s.s0, far = s.s1;
+    const int64_t token = (m < 8 ? near : far) + (m >> 2) * 8 + (m & 3);        // of the first tile's row m; the second has the one four further on
+    const char *const p = static_cast<const char *>(c.k) + token * (c.D * E);
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int s = 0; s < (BITS8 ? T::KC / 2 : T::KC); ++s) {
-            const int d = STEP * s + (16 / E) * g;
-            r.k[t][s] = u32x4{0, 0, 0, 0};
-            if (d < c.D) r.k[t][s] = *reinterpret_cast<const u32x4 *>(kp + (4 * t * c.D + d) * E);
+        for (int i = 0; i < Keys<DP, BITS8>::STEPS; ++i) {
+            const int d = STEP * i + (16 / E) * g;
+            r.k[t][i] = u32x4{0, 0, 0, 0};
+            if (d < c.D) r.k[t][i] = *reinterpret_cast<const u32x4 *>(p + (4 * t * c.D + d) * E);
         }
-    const bool there = T::DV * m < c.D;
+    if constexpr (BITS8) {
+        const uint8_t *const e = c.k_exps + token * c.groups;
+        if constexpr (DP <= 128) r.e[0] = e[0], r.e[1] = e[4];
+        else r.e[0] = *reinterpret_cast<const uint16_t *>(e), r.e[1] = *reinterpret_cast<const uint16_t *>(e + 8);
+    }
+}
+
+template <int DP, bool BITS8> __device__ __forceinline__ void load_values(const KvCache &c, Spot s, int lane, Values<DP, BITS8> &r)
+{
+    constexpr int E = BITS8 ? 1 : 2, DV = DP / 16, W = Values<DP, BITS8>::WORDS;
+    const int m = lane & 15, g = lane >> 4;
+    const int64_t near = s.s0, far = s.s1;
+    const int64_t token = (g < 2 ? near : far) + 8 * g;
+    const char *const p = static_cast<const char *>(c.v) + token * (c.D * E) + DV * m * E;
+    const bool there = DV * m < c.D;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        constexpr int W = BITS8 ? T::DV / 4 : T::DV / 2;
-        const uint32_t *const p = reinterpret_cast<const uint32_t *>(vp + i * c.D * E);
+        const uint32_t *const x = reinterpret_cast<const uint32_t *>(p + i * c.D * E);
 #pragma unroll
         for (int w = 0; w < W; ++w) r.v[i][w] = 0;
         if (there) {
             if constexpr (W % 4 == 0) {
 #pragma unroll
                 for (int w = 0; w < W; w += 4) {
-                    const u32x4 x = *reinterpret_cast<const u32x4 *>(p + w);
-                    r.v[i][w] = x[0], r.v[i][w + 1] = x[1], r.v[i][w + 2] = x[2], r.v[i][w + 3] = x[3];
+                    const u32x4 y = *reinterpret_cast<const u32x4 *>(x + w);
+                    r.v[i][w] = y[0], r.v[i][w + 1] = y[1], r.v[i][w + 2] = y[2], r.v[i][w + 3] = y[3];
                 }
             } else if constexpr (W == 2) {
-                const u32x2 x = *reinterpret_cast<const u32x2 *>(p);
-                r.v[i][0] = x[0], r.v[i][1] = x[1];
+                const u32x2 y = *reinterpret_cast<const u32x2 *>(x);
+                r.v[i][0] = y[0], r.v[i][1] = y[1];
             } else {
-                r.v[i][0] = p[0];
+                r.v[i][0] = x[0];
             }
         }
     }
     if constexpr (BITS8) {
-        const uint8_t *const ke = c.k_exps + ((m < 8 ? s0 : s1) + tk) * c.groups, *const ve = c.v_exps + ((g < 2 ? s0 : s1) + 8 * g) * c.groups;
+        const uint8_t *const e = c.v_exps + token * c.groups;
         if constexpr (DP <= 128) {
-            r.ke[0] = ke[0], r.ke[1] = ke[4];
-            const u32x2 x = *reinterpret_cast<const u32x2 *>(ve);
-            r.ve[0] = x[0], r.ve[1] = x[1];
+            const u32x2 y = *reinterpret_cast<const u32x2 *>(e);
+            r.e[0] = y[0], r.e[1] = y[1];
         } else {
-            r.ke[0] = *reinterpret_cast<const uint16_t *>(ke), r.ke[1] = *reinterpret_cast<const uint16_t *>(ke + 8);
-            const u32x4 x = *reinterpret_cast<const u32x4 *>(ve);
-            r.ve[0] = x[0], r.ve[1] = x[1], r.ve[2] = x[2], r.ve[3] = x[3];
+            const u32x4 y = *reinterpret_cast<const u32x4 *>(e);
+            r.e[0] = y[0], r.e[1] = y[1], r.e[2] = y[2], r.e[3] = y[3];
         }
     }
 }
@@ -218,58 +229,46 @@ __device__ __forceinline__ float power_of(uint32_t bytes, int at) { return u2f((
 
 __device__ __forceinline__ bool bf16_pair_finite(uint32_t w) { return (w & 0x7F80u) != 0x7F80u && (w & 0x7F800000u) != 0x7F800000u; }
 
+__device__ __forceinline__ float4_t mfma(u32x4 a, u32x4 b, float4_t c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+
 // state of 16 rows: lane (g, row) holds m and a part of l of its row, and out[j][i] = element DV (4g + i) + j of the row
 template <int DP> struct Rows {
     float m, l;
     float4_t o[DP / 16];
 };
 
-// o += values^T x weights; p: the weights of the lane's eight tokens
-template <int DP>
-__device__ __forceinline__ void add_values(u32x4 p, const uint32_t (&v)[8][DP / 32], float4_t (&o)[DP / 16])
-{
-#pragma unroll
-    for (int j = 0; j < DP / 16; ++j) {
-        u32x4 f;                                           // element j of the lane's for its eight tokens
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            f[i] = __builtin_amdgcn_perm(v[2 * i + 1][j / 2], v[2 * i][j / 2], j & 1 ? 0x07060302u : 0x05040100u);
-        o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, f), __builtin_bit_cast(bf16x8_t, p), o[j], 0, 0, 0);
-    }
-}
-
-// One block: scores, running maximum and sum, values.  limit: tokens that the lane's row sees; [low, high]: the least and the most that a row of the tile sees.
 template <int DP, bool BITS8>
-__device__ __forceinline__ void take_block(const Tokens<DP, BITS8> &r, const u32x4 (&q)[DP / 32], float scale2, int limit, int low, int high, int lane, Rows<DP> &s)
+__device__ __forceinline__ void score(const Keys<DP, BITS8> &r, const u32x4 (&q)[DP / 32], float4_t (&sc)[2])
 {
-    constexpr int KC = DP / 32, DV = DP / 16;
-    const int g = lane >> 4;
-    float4_t sc[2] = {float4_t{0, 0, 0, 0}, float4_t{0, 0, 0, 0}};
+    sc[0] = sc[1] = float4_t{0, 0, 0, 0};
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int c = 0; c < KC; ++c) {
-            u32x4 k;
+        for (int c = 0; c < DP / 32; ++c) {
             if constexpr (BITS8) {
                 const uint32_t w0 = r.k[t][c / 2][2 * (c & 1)], w1 = r.k[t][c / 2][2 * (c & 1) + 1];
-                const float power = power_of(r.ke[t], c / 4);
-                k = u32x4{bf16_of_codes(w0, false, power), bf16_of_codes(w0, true, power), bf16_of_codes(w1, false, power), bf16_of_codes(w1, true, power)};
+                const float power = power_of(r.e[t], c / 4);
+                sc[t] = mfma(u32x4{bf16_of_codes(w0, false, power), bf16_of_codes(w0, true, power), bf16_of_codes(w1, false, power), bf16_of_codes(w1, true, power)}, q[c], sc[t]);
             } else {
-                k = r.k[t][c];
+                sc[t] = mfma(r.k[t][c], q[c], sc[t]);
             }
-            sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, k), __builtin_bit_cast(bf16x8_t, q[c]), sc[t], 0, 0, 0);
         }
+}
+
+// Weights of the lane's eight tokens in bf16 from their scores; the running maximum and sum, and what was summed under an older maximum scaled to the new one.
+// whole: every row sees the whole block, else the lane's row sees its tokens below `sees`.
+template <int DP> __device__ __forceinline__ u32x4 weigh(const float4_t (&sc)[2], float scale2, bool whole, int sees, Rows<DP> &s)
+{
     float x[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        x[i] = sc[i >> 2][i & 3] * scale2;
-    }
-    const bool whole = r.t0 + kBlock <= low && r.ok == 3;
-    const bool mine = (r.ok >> (g >> 1)) & 1;
+    for (int i = 0; i < 8; ++i) x[i] = sc[i >> 2][i & 3] * scale2;
     if (!whole) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (!mine || r.t0 + 8 * g + i >= limit) x[i] = -INFINITY;
+            if (i >= sees) x[i] = -INFINITY;
     }
     float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
     top = max16_32(top);
@@ -278,7 +277,7 @@ __device__ __forceinline__ void take_block(const Tokens<DP, BITS8> &r, const u32
         const float by = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(s.m - m);
         s.l *= by;
 #pragma unroll
-        for (int j = 0; j < DV; ++j) s.o[j] *= by;
+        for (int j = 0; j < DP / 16; ++j) s.o[j] *= by;
         s.m = m;
     }
     const float m = s.m == -INFINITY ? 0.0f : s.m;
@@ -288,50 +287,62 @@ __device__ __forceinline__ void take_block(const Tokens<DP, BITS8> &r, const u32
         w[i] = __builtin_amdgcn_exp2f(x[i] - m);
         s.l += w[i];
     }
-    uint32_t v[8][DP / 32];
+    return u32x4{bf16_pair(w[0], w[1]), bf16_pair(w[2], w[3]), bf16_pair(w[4], w[5]), bf16_pair(w[6], w[7])};
+}
+
+// element j of the lane's DV for its eight tokens
+template <int DP, bool BITS8> __device__ __forceinline__ u32x4 turned(const Values<DP, BITS8> &r, int j, int lane)
+{
+    u32x4 f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int d = 0; d < DP / 32; ++d) {
-            if constexpr (BITS8) {
-                // heads of more than 128 elements have two groups; the second begins with lane 8's elements
-                const float power = DP > 128 ? power_of(r.ve[i / 2], 2 * (i & 1) + ((lane & 15) >> 3)) : power_of(r.ve[i / 4], i & 3);
-                v[i][d] = bf16_of_codes(r.v[i][d / 2], d & 1, power);
-            } else {
-                v[i][d] = r.v[i][d];
-            }
-        }
-    const u32x4 p = {bf16_pair(w[0], w[1]), bf16_pair(w[2], w[3]), bf16_pair(w[4], w[5]), bf16_pair(w[6], w[7])};
-    if (!whole) {
-        // Tokens that no row of the tile sees may hold anything: zeros in their place.  Values that are not finite reach the rows that see them and no others: then row by row.
-        bool odd = false;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int d = 0; d < DP / 32; ++d) {
-                if (!mine || r.t0 + 8 * g + i >= high) v[i][d] = 0;
-                else odd |= !bf16_pair_finite(v[i][d]);
-            }
-        if (__any(odd)) {
-            for (int n = 0; n < kTile; ++n) {
-                const int sees = __shfl(limit, n, 64);
-                uint32_t u[8][DP / 32];
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-#pragma unroll
-                    for (int d = 0; d < DP / 32; ++d) u[i][d] = r.t0 + 8 * g + i < sees ? v[i][d] : 0;
-                float4_t o[DP / 16];
-#pragma unroll
-                for (int j = 0; j < DV; ++j) o[j] = float4_t{0, 0, 0, 0};
-                add_values<DP>(p, u, o);
-                if ((lane & 15) == n)
-#pragma unroll
-                    for (int j = 0; j < DV; ++j) s.o[j] += o[j];
-            }
-            return;
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (BITS8) {
+            // heads of more than 128 elements have two groups; the second begins with lane 8's elements
+            const auto wide = [&](int t) {
+                const float power = DP > 128 ? power_of(r.e[t / 2], 2 * (t & 1) + ((lane & 15) >> 3)) : power_of(r.e[t / 4], t & 3);
+                return bf16_of_codes(r.v[t][j / 4], (j & 2) != 0, power);
+            };
+            f[i] = __builtin_amdgcn_perm(wide(2 * i + 1), wide(2 * i), j & 1 ? 0x07060302u : 0x05040100u);
+        } else {
+            f[i] = __builtin_amdgcn_perm(r.v[2 * i + 1][j / 2], r.v[2 * i][j / 2], j & 1 ? 0x07060302u : 0x05040100u);
         }
     }
-    add_values<DP>(p, v, s.o);
+    return f;
+}
+
+// zeros for the tokens from `keep` on of a lane's eight, in pairs
+__device__ __forceinline__ u32x4 first_tokens(u32x4 f, int keep)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = keep >= 2 * i + 2 ? f[i] : keep == 2 * i + 1 ? f[i] & 0xFFFFu : 0;
+    return f;
+}
+
+// out += values^T x weights.  Tokens that no row of the tile sees (from `there` on, of the lane's eight) may hold anything: zeros in their place.  Values that are not finite
+// reach the rows that see them (tokens below `sees`, the lane's own row's) and no others: a product of each row's own then.
+template <int DP, bool BITS8> __device__ __forceinline__ void add_values(const Values<DP, BITS8> &r, u32x4 p, bool whole, int there, int sees, int lane, Rows<DP> &s)
+{
+    if (whole) {
+#pragma unroll
+        for (int j = 0; j < DP / 16; ++j) s.o[j] = mfma(turned<DP, BITS8>(r, j, lane), p, s.o[j]);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < DP / 16; ++j) {
+        const u32x4 f = first_tokens(turned<DP, BITS8>(r, j, lane), there);
+        bool fine = true;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) fine &= bf16_pair_finite(f[i]);
+        if (__all(fine)) {
+            s.o[j] = mfma(f, p, s.o[j]);
+        } else {
+            for (int n = 0; n < kTile; ++n) {
+                const int row_sees = __shfl(sees, (lane & 48) + n, 64);       // this lane's tokens that row n sees
+                const float4_t o = mfma(first_tokens(f, row_sees), p, float4_t{0, 0, 0, 0});
+                if ((lane & 15) == n) s.o[j] += o;
+            }
+        }
+    }
 }
 
 // PREFIX: tiles of all rows against the shared tokens; else of a sequence's rows against its own
@@ -390,19 +401,46 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attn_kernel(Args a
     s.m = -INFINITY, s.l = 0.0f;
 #pragma unroll
     for (int j = 0; j < DV; ++j) s.o[j] = float4_t{0, 0, 0, 0};
-    // the waves take blocks in turn; one block is on its way while another is worked on
-    Tokens<DP, BITS8> x, y;
-    int t = begin + wave * kBlock;
-    constexpr int STEP = kWaves * kBlock;
-    if (t < end) load_tokens<DP, BITS8>(a.c, table, table_len, head, t, lane, x);
-    while (t < end) {
-        if (t + STEP < end) load_tokens<DP, BITS8>(a.c, table, table_len, head, t + STEP, lane, y);
-        take_block<DP, BITS8>(x, q, a.scale2, min(limit, end), min(low, end), min(high, end), lane, s);
-        t += STEP;
-        if (t >= end) break;
-        if (t + STEP < end) load_tokens<DP, BITS8>(a.c, table, table_len, head, t + STEP, lane, x);
-        take_block<DP, BITS8>(y, q, a.scale2, min(limit, end), min(low, end), min(high, end), lane, s);
-        t += STEP;
+    // The waves take blocks in turn.  The keys of the next block are on their way from the moment that the scores have taken this one's, its values from when the products have.
+    // Page numbers come 64 at once: lane 2i + h has half h of the wave's i-th block from now.
+    constexpr int STRIDE = kWaves * kBlock, AHEAD = 32;
+    const int t0 = begin + wave * kBlock;
+    const int blocks = end > t0 ? (end - t0 + STRIDE - 1) / STRIDE : 0;
+    limit = min(limit, end), low = min(low, end), high = min(high, end);
+    int pages = -1, held = AHEAD;
+    const auto next_spot = [&](int t) {
+        if (held == AHEAD) {
+            const int i = (t + (lane >> 1) * STRIDE + (lane & 1) * 16) >> a.c.page_log2;
+            pages = i < table_len ? table[i] : -1;
+            pages = pages < a.c.pages ? pages : -1;
+            held = 0;
+        }
+        const int p0 = __builtin_amdgcn_readlane(pages, 2 * held), p1 = __builtin_amdgcn_readlane(pages, 2 * held + 1);
+        ++held;
+        return spot_of(a.c, head, t, p0, p1);
+    };
+    Keys<DP, BITS8> k;
+    Values<DP, BITS8> v;
+    Spot now = {0, 0, 0};
+    if (blocks > 0) {
+        now = next_spot(t0);
+        load_keys<DP, BITS8>(a.c, now, lane, k);
+        load_values<DP, BITS8>(a.c, now, lane, v);
+    }
+    for (int i = 0; i < blocks; ++i) {
+        const int t = t0 + i * STRIDE;
+        float4_t sc[2];
+        score<DP, BITS8>(k, q, sc);
+        const uint32_t ok = now.ok;
+        if (i + 1 < blocks) {
+            now = next_spot(t + STRIDE);
+            load_keys<DP, BITS8>(a.c, now, lane, k);
+        }
+        const bool whole = t + kBlock <= low && ok == 3, mine = ok >> (g >> 1) & 1;
+        const int sees = mine ? limit - t - 8 * g : 0, there = mine ? high - t - 8 * g : 0;
+        const u32x4 p = weigh<DP>(sc, a.scale2, whole, sees, s);
+        add_values<DP, BITS8>(v, p, whole, there, sees, lane, s);
+        if (i + 1 < blocks) load_values<DP, BITS8>(a.c, now, lane, v);
     }
     // the four waves' shares: out = sum 2^(m_w - m) out_w
     s.l = sum16_32(s.l);
