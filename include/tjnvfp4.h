@@ -444,7 +444,7 @@ int nvfp4_kv_load(const nvfp4_kvcache *cache, const nvfp4_kvbatch *batch, int64_
  *   out = sum_t softmax_t(scale q . k_t) v_t        (zeros where it sees nothing)
  * Out [N x Hq D] bf16.  Scores and sums are binary32; the weights of the values are rounded to bf16 for the matrix instructions.  A NaN or infinity in a key or value stays with the
  * rows that see it.  The prefix is read once for all rows of a tile, whatever the number of sequences.
- * Hq a multiple of H, N * Hq <= 2^30; scale finite.  ws: nvfp4_attn_workspace_bytes of the same sizes (16-byte aligned; from N, B, width and prefix alone, not from lengths, so that
+ * Hq a multiple of H, N * Hq <= 2^30; scale finite and above 0.  ws: nvfp4_attn_workspace_bytes of the same sizes (16-byte aligned; from N, B, width and prefix alone, not from lengths, so that
  * one does for all steps of a batch).  Same inputs, same bits.  Errors: NULL, SHAPE, ENUM, ALIGN, MISMATCH, WORKSPACE.
  */
 int nvfp4_attn(const void *Q, int64_t ldq, int64_t N, int64_t Hq, const nvfp4_kvcache *cache, const nvfp4_kvbatch *batch, float scale, void *Out, int64_t ldo,

@@ -176,7 +176,7 @@ size_t nvfp4_attn_workspace_bytes(int64_t N, int64_t Hq, int64_t H, int64_t D, i
     if (N <= 0 || N > kMaxRows || H < 1 || H > kMaxWidth || Hq < 1 || Hq % H != 0 || Hq > kMaxHeadRows / N || !is_head_dim(D) || !is_page(page) || B <= 0 ||
         check_counts(B, width, prefix, page))
         return 0;
-    return attn_workspace_bytes(N, (int)Hq, (int)H, (int)D, (int)B, prefix);
+    return attn_workspace_bytes(N, (int)Hq, (int)H, (int)D, (int)B, width * page, prefix);
 }
 
 int nvfp4_attn(const void *Q, int64_t ldq, int64_t N, int64_t Hq, const nvfp4_kvcache *cache, const nvfp4_kvbatch *batch, float scale, void *Out, int64_t ldo,
@@ -197,7 +197,7 @@ int nvfp4_attn(const void *Q, int64_t ldq, int64_t N, int64_t Hq, const nvfp4_kv
     if (rc) return rc;
     rc = make_dst(Out, NVFP4_OUT_BF16, ldo, N, Hq * c.D, &out);
     if (rc) return rc;
-    if (!isfinite(scale)) return NVFP4_ERR_ENUM;
+    if (!isfinite(scale) || !(scale > 0.0f)) return NVFP4_ERR_ENUM;
     const size_t need = nvfp4_attn_workspace_bytes(N, Hq, c.heads, c.D, (int64_t)1 << c.page_log2, b.B, b.width, b.prefix);
     if (need && (!ws || ws_bytes < need)) return NVFP4_ERR_WORKSPACE;
     if (need && !aligned(ws, 16)) return NVFP4_ERR_ALIGN;

@@ -1,117 +1,12 @@
-// Attention of a batch's rows over the paged cache of keys and values.
-//
-//   s_t = scale q . k_t,  m = max s,  l = sum 2^(s_t - m),  out = sum 2^(s_t - m) v_t / l       (s in units of log2)
-//
-// A tile is 16 rows of one key head: (new token, query head) pairs of one sequence, or of the whole batch against the shared prefix.  The tokens that a tile sees are cut into
-// parts, so that few rows fill the GPU as well; a part leaves (m, l, unnormalised out) and a second kernel joins them:
-//   out = sum_p 2^(m_p - m) out_p / sum_p 2^(m_p - m) l_p.
-// Where a tile has one part only, and there is no prefix, the first kernel writes the output itself.
-#include "rowwise.h"
-#include "seq_ops.h"
+// Attention of a batch's rows over the paged cache of keys and values: tiles of 16 rows, and what joins the parts of all tiles.  (Formulas: attn_common.h.)
+#include "attn_common.h"
 
 namespace tj {
 
 namespace {
 
-typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
-
-constexpr int kThreads = 256;
-constexpr int kWaves = 4;
 constexpr int kTile = 16;                 // rows of a tile
-constexpr int kUnit = 64;                 // tokens in which the parts' lengths are counted
 constexpr int kBlock = 32;                // tokens that a wave takes at once
-constexpr int kMinUnits = 2;              // of a part: a block for every wave
-constexpr int kGroups = 2048;             // workgroups that the own tokens of a batch are spread over, and the prefix
-
-struct Args {
-    const uint16_t *q;
-    int64_t ldq;
-    uint16_t *out;
-    int64_t ldo;
-    int N, Hq, G;                         // rows, query heads, query heads of a key head
-    KvCache c;
-    KvBatch b;
-    float scale2;                         // scale * log2 e
-    int target;                           // parts that a key head's own tokens are to be cut into; 0: none are cut
-    int slots;                            // own parts of a key head, at most
-    int prefix_units, prefix_parts;       // units of a part of the prefix, and how many there are
-    float *part_o;                        // [slot][key head][16][D], own parts first
-    float2_t *part_ml;                    // [slot][key head][16]
-};
-
-// What a workgroup has to know of the batch: how many units a part has, and where a part lies.
-struct Place {
-    int b, tile, part, parts;             // sequence; tile and part in it; parts of its tiles
-    int64_t base;                         // first slot of the sequence
-};
-
-__device__ __forceinline__ int units(int tokens) { return (tokens + kUnit - 1) / kUnit; }
-__device__ __forceinline__ int tiles_of(int rows, int G) { return (rows * G + kTile - 1) / kTile; }
-
-__device__ __forceinline__ int64_t block_sum_scan(int64_t v, int64_t *lds, int64_t &before)      // sum over the workgroup; before: over the threads in front
-{
-    int64_t incl = v;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int64_t t = __shfl_up((long long)incl, o, 64);
-        if ((int)(threadIdx.x & 63) >= o) incl += t;
-    }
-    const int w = threadIdx.x >> 6;
-    __syncthreads();
-    if ((threadIdx.x & 63) == 63) lds[w] = incl;
-    __syncthreads();
-    int64_t total = 0;
-    before = incl - v;
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i) {
-        if (i < w) before += lds[i];
-        total += lds[i];
-    }
-    return total;
-}
-
-// Units of a part of the own tokens: all tiles' units over the parts wanted.  Then where slot `slot` lies (slot >= 0), or where sequence `seq` starts.
-// Every thread of the workgroup calls it; false: there is no such slot.
-__device__ bool find(const Args &a, int slot, int seq, Place &p, int &part_units, int64_t *lds)
-{
-    __shared__ Place found;
-    const int per = (a.b.B + kThreads - 1) / kThreads, b0 = threadIdx.x * per, b1 = min(b0 + per, a.b.B);
-    if (threadIdx.x == 0) found.b = -1;
-    part_units = 1 << 25;                                      // more than any sequence has
-    if (a.target > 0) {
-        int64_t sum = 0;
-        for (int b = b0; b < b1; ++b) {
-            int first, count;
-            rows_of(a.b, b, a.N, first, count);
-            sum += (int64_t)tiles_of(count, a.G) * units(tokens_of(a.b, a.c, b));
-        }
-        int64_t before;
-        const int64_t total = block_sum_scan(sum, lds, before), wanted = (total + a.target - 1) / a.target;
-        part_units = wanted < kMinUnits ? kMinUnits : wanted < part_units ? (int)wanted : part_units;
-    }
-    int64_t sum = 0, at;
-    for (int b = b0; b < b1; ++b) {
-        int first, count;
-        rows_of(a.b, b, a.N, first, count);
-        sum += (int64_t)tiles_of(count, a.G) * max(1, (units(tokens_of(a.b, a.c, b)) + part_units - 1) / part_units);
-    }
-    block_sum_scan(sum, lds, at);
-    for (int b = b0; b < b1; ++b) {
-        int first, count;
-        rows_of(a.b, b, a.N, first, count);
-        const int parts = max(1, (units(tokens_of(a.b, a.c, b)) + part_units - 1) / part_units);
-        const int64_t n = (int64_t)tiles_of(count, a.G) * parts;
-        if (slot >= 0 ? slot >= at && slot < at + n : b == seq) {
-            const int in = slot >= 0 ? (int)(slot - at) : 0;
-            found = Place{b, in / parts, in % parts, parts, at};
-            break;
-        }
-        at += n;
-    }
-    __syncthreads();
-    p = found;
-    return p.b >= 0;
-}
 
 __device__ __forceinline__ float max16_32(float v)             // over the four lanes that hold a row
 {
@@ -147,8 +42,6 @@ struct Spot {
     int64_t s0, s1;
     uint32_t ok;
 };
-
-__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 __device__ __forceinline__ Spot spot_of(const KvCache &c, int head, int t0, int p0, int p1)
 {
@@ -218,16 +111,6 @@ template <int DP, bool BITS8> __device__ __forceinline__ void load_values(const 
         }
     }
 }
-
-// two of a word's four E4M3 codes times a power of two as bf16: exact
-__device__ __forceinline__ uint32_t bf16_of_codes(uint32_t w, bool high, float power)
-{
-    return high ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, power, true))
-                : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, power, false));
-}
-__device__ __forceinline__ float power_of(uint32_t bytes, int at) { return u2f(((bytes >> (8 * at)) & 0xFF) << 23); }
-
-__device__ __forceinline__ bool bf16_pair_finite(uint32_t w) { return (w & 0x7F80u) != 0x7F80u && (w & 0x7F800000u) != 0x7F800000u; }
 
 __device__ __forceinline__ float4_t mfma(u32x4 a, u32x4 b, float4_t c)
 {
@@ -310,14 +193,6 @@ template <int DP, bool BITS8> __device__ __forceinline__ u32x4 turned(const Valu
     return f;
 }
 
-// zeros for the tokens from `keep` on of a lane's eight, in pairs
-__device__ __forceinline__ u32x4 first_tokens(u32x4 f, int keep)
-{
-#pragma unroll
-    for (int i = 0; i < 4; ++i) f[i] = keep >= 2 * i + 2 ? f[i] : keep == 2 * i + 1 ? f[i] & 0xFFFFu : 0;
-    return f;
-}
-
 // out += values^T x weights.  Tokens that no row of the tile sees (from `there` on, of the lane's eight) may hold anything: zeros in their place.  Values that are not finite
 // reach the rows that see them (tokens below `sees`, the lane's own row's) and no others: a product of each row's own then.
 template <int DP, bool BITS8> __device__ __forceinline__ void add_values(const Values<DP, BITS8> &r, u32x4 p, bool whole, int there, int sees, int lane, Rows<DP> &s)
@@ -336,6 +211,7 @@ template <int DP, bool BITS8> __device__ __forceinline__ void add_values(const V
         if (__all(fine)) {
             s.o[j] = mfma(f, p, s.o[j]);
         } else {
+#pragma unroll 1
             for (int n = 0; n < kTile; ++n) {
                 const int row_sees = __shfl(sees, (lane & 48) + n, 64);       // this lane's tokens that row n sees
                 const float4_t o = mfma(first_tokens(f, row_sees), p, float4_t{0, 0, 0, 0});
@@ -347,7 +223,7 @@ template <int DP, bool BITS8> __device__ __forceinline__ void add_values(const V
 
 // PREFIX: tiles of all rows against the shared tokens; else of a sequence's rows against its own
 template <int DP, bool BITS8, bool PREFIX>
-__global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attn_kernel(Args a)
+__global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attn_kernel(AttnArgs a)
 {
     constexpr int DV = DP / 16, LD = DP + 4;
     __shared__ int64_t lds[kWaves];
@@ -356,35 +232,13 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attn_kernel(Args a
     const int head = blockIdx.x % a.c.heads, item = blockIdx.x / a.c.heads;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const int row = lane & 15, g = lane >> 4;
-
-    int first, count, tile, begin, end, limit, low, high, parts, table_len;
-    const int *table;
-    if constexpr (PREFIX) {
-        tile = item / a.prefix_parts;
-        parts = 2;                                           // never alone: the own tokens follow
-        begin = item % a.prefix_parts * a.prefix_units * kUnit;
-        end = min(begin + a.prefix_units * kUnit, a.b.prefix);
-        first = 0, count = a.N;
-        low = high = limit = a.b.prefix;
-        table = a.b.prefix_table;
-        table_len = (a.b.prefix + (1 << a.c.page_log2) - 1) >> a.c.page_log2;
-    } else {
-        Place p;
-        int part_units;
-        if (!find(a, item, -1, p, part_units, lds)) return;
-        rows_of(a.b, p.b, a.N, first, count);
-        const int len = tokens_of(a.b, a.c, p.b);
-        tile = p.tile, parts = a.b.prefix ? 2 : p.parts;
-        begin = p.part * part_units * kUnit;
-        // the row's token and those before it
-        const auto sees = [&](int r) { return max(0, len - count + min(r / a.G, count - 1) + 1); };
-        limit = sees(tile * kTile + row);
-        low = sees(tile * kTile), high = sees(tile * kTile + kTile - 1);
-        end = min(p.part == p.parts - 1 ? len : begin + part_units * kUnit, high);
-        table = a.b.table + (int64_t)p.b * a.b.width;
-        table_len = a.b.width;
-    }
-    const int rows = count * a.G, r = tile * kTile + row;
+    Work w;
+    if (!work_of<PREFIX>(a, item, lds, w)) return;
+    const int first = w.first, r = w.tile * kTile + row, rows = w.count * a.G;
+    int high = sees_of<PREFIX>(a, w, w.tile * kTile + kTile - 1);
+    const int begin = w.begin, end = min(w.end, high);
+    high = end;
+    const int limit = min(sees_of<PREFIX>(a, w, r), end), low = min(sees_of<PREFIX>(a, w, w.tile * kTile), end);
     const bool valid = r < rows;
     // queries of the tile's rows: elements 32c + 8g .. of step c (8 bits: as the codes' sixteen elements are dealt)
     u32x4 q[DP / 32];
@@ -406,12 +260,11 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attn_kernel(Args a
     constexpr int STRIDE = kWaves * kBlock, AHEAD = 32;
     const int t0 = begin + wave * kBlock;
     const int blocks = end > t0 ? (end - t0 + STRIDE - 1) / STRIDE : 0;
-    limit = min(limit, end), low = min(low, end), high = min(high, end);
     int pages = -1, held = AHEAD;
     const auto next_spot = [&](int t) {
         if (held == AHEAD) {
             const int i = (t + (lane >> 1) * STRIDE + (lane & 1) * 16) >> a.c.page_log2;
-            pages = i < table_len ? table[i] : -1;
+            pages = i < w.table_len ? w.table[i] : -1;
             pages = pages < a.c.pages ? pages : -1;
             held = 0;
         }
@@ -454,19 +307,19 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attn_kernel(Args a
     const int orow = threadIdx.x >> 4, od = (threadIdx.x & 15) * DV;
     float m = -INFINITY, l = 0.0f, o[DV] = {};
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) m = fmaxf(m, part_ml[w][orow].x);
+    for (int i = 0; i < kWaves; ++i) m = fmaxf(m, part_ml[i][orow].x);
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        const float2_t ml = part_ml[w][orow];
+    for (int i = 0; i < kWaves; ++i) {
+        const float2_t ml = part_ml[i][orow];
         const float by = ml.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml.x - m);
         l += ml.y * by;
 #pragma unroll
-        for (int j = 0; j < DV; ++j) o[j] += ml.x == -INFINITY ? 0.0f : part[w][orow][od + j] * by;
+        for (int j = 0; j < DV; ++j) o[j] += ml.x == -INFINITY ? 0.0f : part[i][orow][od + j] * by;
     }
-    const int at = tile * kTile + orow;
+    const int at = w.tile * kTile + orow;
     if (at >= rows || od >= a.c.D) return;
-    if (parts == 1) {
-        const float by = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;                        // nothing seen: zeros; NaN stays
+    if (w.parts == 1) {
+        const float by = over(l);
         uint16_t *const p = a.out + (int64_t)(first + at / a.G) * a.ldo + (int64_t)(head * a.G + at % a.G) * a.c.D + od;
 #pragma unroll
         for (int j = 0; j < DV; j += 2) {
@@ -474,17 +327,17 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attn_kernel(Args a
             p[j] = (uint16_t)w, p[j + 1] = (uint16_t)(w >> 16);
         }
     } else {
-        const int64_t slot = ((int64_t)(PREFIX ? a.slots + item : item) * a.c.heads + head) * kTile + orow;
-        float *const p = a.part_o + slot * a.c.D + od;
+        const int64_t slot = (w.slot * a.c.heads + head) * kTile + orow;
+        float *const p = (PREFIX ? a.prefix_o : a.own_o) + slot * a.c.D + od;
 #pragma unroll
         for (int j = 0; j < DV; j += 4) *reinterpret_cast<float4_t *>(p + j) = float4_t{o[j], o[j + 1], o[j + 2], o[j + 3]};
-        if (od == 0) a.part_ml[slot] = float2_t{m, l};
+        if (od == 0) (PREFIX ? a.prefix_ml : a.own_ml)[slot] = float2_t{m, l};
     }
 }
 
 // Joins the parts of a row and query head: D / 4 lanes a part, the parts dealt to the lane groups, their shares added through LDS.
 template <int DP>
-__global__ __launch_bounds__(kThreads) void attn_join_kernel(Args a)
+__global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs a)
 {
     constexpr int L = DP / 4, GROUPS = kThreads / L;          // lanes of a part; parts at once
     __shared__ int64_t lds[kWaves];
@@ -500,20 +353,20 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(Args a)
     int part_units;
     find(a, -1, b, p, part_units, lds);
     if (p.parts == 1 && !a.b.prefix) return;                  // written already
-    if (p.base + (int64_t)tiles_of(count, a.G) * p.parts > a.slots) return;      // starts that name rows twice
+    if (p.base + (int64_t)tiles_of(count, a.G, a.own_rows) * p.parts > a.slots) return;      // starts that name rows twice
     const int kv = head / a.G, in_seq = (n - first) * a.G + head % a.G, in_all = n * a.G + head % a.G;
     const int total = p.parts + a.prefix_parts;
     const int lane = threadIdx.x % L, group = threadIdx.x / L;
-    const auto slot_of = [&](int i) {                         // row of the i-th part: own parts first
-        return i < p.parts ? ((p.base + in_seq / kTile * p.parts + i) * a.c.heads + kv) * kTile + in_seq % kTile
-                           : ((int64_t)(a.slots + in_all / kTile * a.prefix_parts + i - p.parts) * a.c.heads + kv) * kTile + in_all % kTile;
-    };
+    // the row's place among the parts of its tile: own parts, parts of the prefix
+    const int64_t own = ((p.base + (int64_t)(in_seq / a.own_rows) * p.parts) * a.c.heads + kv) * a.own_rows + in_seq % a.own_rows;
+    const int64_t pre = a.prefix_parts ? ((int64_t)(in_all / a.prefix_rows) * a.prefix_parts * a.c.heads + kv) * a.prefix_rows + in_all % a.prefix_rows : 0;
     float m = -INFINITY, l = 0.0f;
     float4_t o = {0, 0, 0, 0};
     for (int i = group; i < total; i += GROUPS) {
-        const int64_t slot = slot_of(i);
-        const float2_t ml = a.part_ml[slot];
-        const float4_t v = 4 * lane < a.c.D ? *reinterpret_cast<const float4_t *>(a.part_o + slot * a.c.D + 4 * lane) : float4_t{0, 0, 0, 0};
+        const bool mine = i < p.parts;
+        const int64_t slot = mine ? own + (int64_t)i * a.c.heads * a.own_rows : pre + (int64_t)(i - p.parts) * a.c.heads * a.prefix_rows;
+        const float2_t ml = (mine ? a.own_ml : a.prefix_ml)[slot];
+        const float4_t v = 4 * lane < a.c.D ? *reinterpret_cast<const float4_t *>((mine ? a.own_o : a.prefix_o) + slot * a.c.D + 4 * lane) : float4_t{0, 0, 0, 0};
         const float top = fmaxf(m, ml.x);
         if (top == -INFINITY) continue;
         const float old = __builtin_amdgcn_exp2f(m - top), by = __builtin_amdgcn_exp2f(ml.x - top);
@@ -535,7 +388,7 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(Args a)
         l += ml.y * by;
         o += sums[i][lane] * by;
     }
-    const float by = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
+    const float by = over(l);
     uint16_t *const out = a.out + (int64_t)n * a.ldo + (int64_t)head * a.c.D + 4 * lane;
     const uint32_t w0 = bf16_pair(o[0] * by, o[1] * by), w1 = bf16_pair(o[2] * by, o[3] * by);
     out[0] = (uint16_t)w0, out[1] = (uint16_t)(w0 >> 16), out[2] = (uint16_t)w1, out[3] = (uint16_t)(w1 >> 16);
@@ -544,25 +397,38 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(Args a)
 // ---- how a call is cut -------------------------------------------------------------------------
 
 struct Cut {
-    int target, prefix_units, prefix_parts;
+    int target, min_units, own_rows, prefix_rows, prefix_units, prefix_parts;
     int64_t slots, items, prefix_items;        // of a key head
 };
 
-Cut cut_of(int64_t N, int Hq, int heads, int B, int64_t prefix)
+constexpr int kGroups = 2048;             // workgroups that a batch's own tokens are spread over where tiles have 16 rows
+constexpr int kWideGroups = 512;          // and more: two a CU
+
+int rows_of_tile(int64_t rows, int D) { return rows < 64 || D > 128 ? kTile : kWideRows; }
+
+Cut cut_of(int64_t N, int Hq, int heads, int D, int B, int64_t tokens, int64_t prefix)
 {
     Cut p;
-    const int64_t G = Hq / heads, tiles = (N * G + kTile - 1) / kTile;
-    // Enough tiles of several rows: nothing is cut.  Else the own tokens are cut into about kGroups parts, also where there are that many sequences: their lengths differ.
-    const bool cut = N <= 2 * B || tiles * heads < kGroups;
-    p.target = cut ? (int)((kGroups + heads - 1) / heads) : 0;
-    p.items = p.target + (N * G) / kTile + B;            // every tile at least once, and the cuts
+    const int64_t G = Hq / heads;
+    p.own_rows = rows_of_tile((N + B - 1) / B * G, D);
+    p.min_units = p.own_rows == kTile ? 2 : 4;
+    const int64_t tiles = N * G / p.own_rows + B, units = (tokens + kUnit - 1) / kUnit;
+    // Enough tiles of several rows: nothing is cut.  Else the own tokens are cut, also where there are many sequences: their lengths differ.
+    const int64_t groups = p.own_rows == kTile ? kGroups : kWideGroups;
+    const bool cut = (N <= 2 * B || tiles * heads < groups) && units > p.min_units;
+    p.target = cut ? (int)((groups + heads - 1) / heads) : 0;
+    const int64_t most = cut ? (units + p.min_units - 1) / p.min_units : 1;                // parts of a tile
+    p.items = tiles * most < tiles + p.target ? tiles * most : tiles + p.target;           // every tile at least once, and the cuts
     p.slots = cut || prefix ? p.items : 0;
-    p.prefix_units = p.prefix_parts = 0;
+    p.prefix_rows = p.prefix_units = p.prefix_parts = 0;
     p.prefix_items = 0;
     if (prefix > 0) {
-        const int64_t units = (prefix + kUnit - 1) / kUnit, want = (kGroups / 2 + tiles * heads - 1) / (tiles * heads);
+        p.prefix_rows = rows_of_tile(N * G, D);
+        const int64_t tiles = (N * G + p.prefix_rows - 1) / p.prefix_rows, wanted = p.prefix_rows == kTile ? kGroups / 2 : kWideGroups;
+        const int64_t units = (prefix + kUnit - 1) / kUnit, want = (wanted + tiles * heads - 1) / (tiles * heads);
         int64_t part = (units + want - 1) / want;
-        part = part < kMinUnits ? kMinUnits : part;
+        const int least = p.prefix_rows == kTile ? 2 : 4;
+        part = part < least ? least : part;
         p.prefix_units = (int)part;
         p.prefix_parts = (int)((units + part - 1) / part);
         p.prefix_items = tiles * p.prefix_parts;
@@ -570,32 +436,46 @@ Cut cut_of(int64_t N, int Hq, int heads, int B, int64_t prefix)
     return p;
 }
 
-int64_t rows_of_parts(const Cut &p, int heads) { return (p.slots + p.prefix_items) * heads * kTile; }
+int64_t own_parts(const Cut &p, int heads) { return p.slots * heads * p.own_rows; }              // rows of them
+int64_t prefix_parts(const Cut &p, int heads) { return p.prefix_items * heads * p.prefix_rows; }
 
-template <int DP, bool BITS8>
-hipError_t run(const Args &a, const Cut &p, hipStream_t st)
+template <int DP, bool BITS8> hipError_t run(const AttnArgs &a, const Cut &p, hipStream_t st)
 {
-    if (p.prefix_items > 0) attn_kernel<DP, BITS8, true><<<(unsigned)(p.prefix_items * a.c.heads), kThreads, 0, st>>>(a);
-    attn_kernel<DP, BITS8, false><<<(unsigned)(p.items * a.c.heads), kThreads, 0, st>>>(a);
+    if (p.prefix_items > 0) {
+        if (p.prefix_rows > kTile) {
+            const hipError_t e = launch_attn_wide(a, true, p.prefix_items, st);
+            if (e != hipSuccess) return e;
+        } else {
+            attn_kernel<DP, BITS8, true><<<(unsigned)(p.prefix_items * a.c.heads), kThreads, 0, st>>>(a);
+        }
+    }
+    if (p.own_rows > kTile) {
+        const hipError_t e = launch_attn_wide(a, false, p.items, st);
+        if (e != hipSuccess) return e;
+    } else {
+        attn_kernel<DP, BITS8, false><<<(unsigned)(p.items * a.c.heads), kThreads, 0, st>>>(a);
+    }
     if (p.slots > 0) attn_join_kernel<DP><<<(unsigned)((int64_t)a.N * a.Hq), kThreads, 0, st>>>(a);
     return hipGetLastError();
 }
 
 }  // namespace
 
-size_t attn_workspace_bytes(int64_t N, int Hq, int heads, int D, int B, int64_t prefix)
+size_t attn_workspace_bytes(int64_t N, int Hq, int heads, int D, int B, int64_t tokens, int64_t prefix)
 {
-    const int64_t rows = rows_of_parts(cut_of(N, Hq, heads, B, prefix), heads);
-    return (size_t)(rows * D * 4 + rows * 8);
+    const Cut p = cut_of(N, Hq, heads, D, B, tokens, prefix);
+    return (size_t)((own_parts(p, heads) + prefix_parts(p, heads)) * (D * 4 + 8));
 }
 
 hipError_t launch_attn(const uint16_t *q, int64_t ldq, int64_t N, int Hq, const KvCache &c, const KvBatch &b, float scale, uint16_t *out, int64_t ldo, void *ws,
                        hipStream_t st)
 {
-    const Cut p = cut_of(N, Hq, c.heads, b.B, b.prefix);
-    Args a{q, ldq, out, ldo, (int)N, Hq, Hq / c.heads, c, b, scale * 1.44269504088896340736f, p.target, (int)p.slots, p.prefix_units, p.prefix_parts, nullptr, nullptr};
-    a.part_o = static_cast<float *>(ws);
-    a.part_ml = reinterpret_cast<float2_t *>(a.part_o + rows_of_parts(p, c.heads) * c.D);
+    const Cut p = cut_of(N, Hq, c.heads, c.D, b.B, (int64_t)b.width << c.page_log2, b.prefix);
+    const int64_t own = own_parts(p, c.heads), pre = prefix_parts(p, c.heads);
+    float *const o = static_cast<float *>(ws);
+    float2_t *const ml = reinterpret_cast<float2_t *>(o + (own + pre) * c.D);
+    const AttnArgs a{q, ldq, out, ldo, (int)N, Hq, Hq / c.heads, c, b, scale * 1.44269504088896340736f, p.target, p.min_units, p.own_rows, p.prefix_rows, p.slots, p.prefix_units,
+                     p.prefix_parts, o, o + own * c.D, ml, ml + own};
     if (c.D <= 64) return c.bits8 ? run<64, true>(a, p, st) : run<64, false>(a, p, st);
     if (c.D <= 128) return c.bits8 ? run<128, true>(a, p, st) : run<128, false>(a, p, st);
     return c.bits8 ? run<256, true>(a, p, st) : run<256, false>(a, p, st);

@@ -1,0 +1,336 @@
+// Attention on tiles of 128 rows: prompts, and many sequences' rows against a shared prefix.  (Formulas: attn_common.h.)
+//
+// Bound by the matrix instructions and, next to them, by the exponentials: 4 D flops and one exponential a (row, token) pair.  The four waves of a workgroup have 32 rows
+// each and share tiles of 64 tokens in LDS, the next tile on its way in registers.  Products: scores^T [tokens x rows] = K Q^T and out^T [D x rows] += V^T P^T, 32 x 32 x 16
+// each; the tokens are dealt to the rows of a score tile so that a lane ends up with the weights that the second product takes from it.  Values lie in LDS as rows of tokens and are turned by the
+// transposing LDS reads.  8-bit caches become bf16 on their way into LDS, once for all four waves.
+#include "attn_common.h"
+
+namespace tj {
+
+namespace {
+
+typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+typedef short short4_t __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ float16_t mfma(u32x4 a, u32x4 b, float16_t c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+
+constexpr int kVector = 2, kMatrix = 8, kLdsReads = 0x100;     // kinds of instructions whose order is laid down below
+
+__device__ __forceinline__ float max32(float v)             // over the two lanes that hold a row
+{
+    const auto b = __builtin_amdgcn_permlane32_swap(f2u(v), f2u(v), false, false);
+    return fmaxf(u2f(b[0]), u2f(b[1]));
+}
+__device__ __forceinline__ float sum32(float v)
+{
+    const auto b = __builtin_amdgcn_permlane32_swap(f2u(v), f2u(v), false, false);
+    return u2f(b[0]) + u2f(b[1]);
+}
+
+// Rows of a tile lie in LDS one after the other, their 16-byte chunks exchanged by the token: chunk c of token t is at c ^ bank(t).  The lanes that read at once (eight
+// tokens' same chunk of keys, eight tokens' 64 bytes of values) then meet all banks alike.
+__device__ __forceinline__ int bank(int t) { return (t & 3) | (t >> 1 & 4); }
+
+template <int DP> struct Shape {
+    static constexpr int TOK = DP > 128 ? 32 : 64;           // tokens of a tile
+    static constexpr int BYTES = 2 * DP;                     // of a token
+    static constexpr int CHUNKS = DP / 8;                    // of 16 bytes
+    static constexpr int PER = kThreads / CHUNKS;            // tokens that the workgroup moves at once
+    static constexpr int MOVES = TOK / PER;
+    static constexpr int GROUPS = TOK / 16;                  // runs of 16 tokens, each in one page
+};
+
+// a tile on its way: what a thread moves of keys and values
+template <int DP, bool BITS8> struct Moved {
+    u32x4 k[Shape<DP>::MOVES], v[Shape<DP>::MOVES];          // 8 bits: codes in the first two words, the exponent in the third
+};
+
+template <int DP, bool BITS8, bool PREFIX>
+__global__ __launch_bounds__(kThreads, 2) void attn_wide_kernel(AttnArgs a)
+{
+    using S = Shape<DP>;
+    constexpr int ROWS = kWideRows, TT = S::TOK / 32, DT = DP / 32;
+    __shared__ int64_t lds[kWaves];
+    __shared__ int odd[2][kWaves];                            // whether a wave has put a value that is not finite and that not every row sees
+    __shared__ __align__(16) char keys[2][S::TOK * S::BYTES];
+    __shared__ __align__(16) char values[2][S::TOK * S::BYTES];
+    const int head = blockIdx.x % a.c.heads, item = blockIdx.x / a.c.heads;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    const int row = lane & 31, h = lane >> 5;
+    Work w;
+    if (!work_of<PREFIX>(a, item, lds, w)) return;
+    const int rows = w.count * a.G, r0 = w.tile * ROWS + wave * 32;
+    const int end = min(w.end, sees_of<PREFIX>(a, w, w.tile * ROWS + ROWS - 1));
+    const int r = r0 + row;
+    const bool valid = r < rows;
+    const int limit = min(sees_of<PREFIX>(a, w, r), end);
+    u32x4 q[DP / 16];
+    const uint16_t *const qp = a.q + (int64_t)(w.first + (valid ? r / a.G : 0)) * a.ldq + (int64_t)(head * a.G + (valid ? r % a.G : 0)) * a.c.D;
+#pragma unroll
+    for (int c = 0; c < DP / 16; ++c) {
+        const int d = 16 * c + 8 * h;
+        q[c] = u32x4{0, 0, 0, 0};
+        if (valid && d < a.c.D) q[c] = *reinterpret_cast<const bf16x8_at2 *>(qp + d);
+    }
+    const int least = min(sees_of<PREFIX>(a, w, w.tile * ROWS), end);         // that a row of the workgroup sees
+    // the least and the most that a row of the wave sees
+    const int low = min(sees_of<PREFIX>(a, w, r0), end), high = min(sees_of<PREFIX>(a, w, r0 + 31), end);
+
+    float m = -INFINITY, l = 0.0f;
+    float16_t o[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+
+    // ---- tiles on their way ----
+    // A wave's loads of a move are of one run of 16 tokens, in one page: its start is in scalar registers, a lane's place in the run is always the same.
+    const int mt = threadIdx.x / S::CHUNKS, mc = threadIdx.x % S::CHUNKS;      // the thread's token (of PER) and chunk
+    const bool there = 8 * mc < a.c.D;                                         // else zeros, whatever was loaded
+    const uint32_t in_run = (mt & 15) * a.c.D + (there ? 8 * mc : 0), e_in_run = (mt & 15) * a.c.groups + (there ? mc / 16 : 0);
+    int pages = -1, held = 64 / S::GROUPS;                                     // page numbers of the next tiles, lane GROUPS i + g: run g of the i-th
+    Moved<DP, BITS8> x;
+    uint32_t ok_next = 0;
+    const auto fetch = [&](int t0) {
+        if (held == 64 / S::GROUPS) {
+            const int i = (t0 + 16 * lane) >> a.c.page_log2;
+            pages = i < w.table_len ? w.table[i] : -1;
+            pages = pages < a.c.pages ? pages : -1;
+            held = 0;
+        }
+        ok_next = 0;
+#pragma unroll
+        for (int g = 0; g < S::GROUPS; ++g) ok_next |= (uint32_t)(__builtin_amdgcn_readlane(pages, S::GROUPS * held + g) >= 0) << g;
+#pragma unroll
+        for (int i = 0; i < S::MOVES; ++i) {
+            const int run = uniform((i * S::PER + mt) >> 4);
+            const int page = __builtin_amdgcn_readlane(pages, S::GROUPS * held + run);
+            const int64_t token = (((int64_t)(page < 0 ? 0 : page) * a.c.heads + head) << a.c.page_log2) + ((t0 + 16 * run) & ((1 << a.c.page_log2) - 1));
+            if constexpr (BITS8) {
+                const u32x2 k = *reinterpret_cast<const u32x2 *>(shared_row(static_cast<const char *>(a.c.k) + token * a.c.D) + in_run);
+                const u32x2 v = *reinterpret_cast<const u32x2 *>(shared_row(static_cast<const char *>(a.c.v) + token * a.c.D) + in_run);
+                x.k[i] = u32x4{k[0], k[1], shared_row(a.c.k_exps + token * a.c.groups)[e_in_run], 0};
+                x.v[i] = u32x4{v[0], v[1], shared_row(a.c.v_exps + token * a.c.groups)[e_in_run], 0};
+            } else {
+                x.k[i] = *reinterpret_cast<const u32x4 *>(shared_row(static_cast<const uint16_t *>(a.c.k) + token * a.c.D) + in_run);
+                x.v[i] = *reinterpret_cast<const u32x4 *>(shared_row(static_cast<const uint16_t *>(a.c.v) + token * a.c.D) + in_run);
+            }
+        }
+        ++held;
+    };
+    const auto put = [&](int t0, int buffer) {
+        bool fine = true;
+        const bool cut = t0 + S::TOK > end || ok_next != (1u << S::GROUPS) - 1;
+#pragma unroll
+        for (int i = 0; i < S::MOVES; ++i) {
+            const int t = i * S::PER + mt;
+            u32x4 k = x.k[i], v = x.v[i];
+            if constexpr (BITS8) {
+                const float ke = power_of(k[2], 0), ve = power_of(v[2], 0);
+                k = u32x4{bf16_of_codes(k[0], false, ke), bf16_of_codes(k[0], true, ke), bf16_of_codes(k[1], false, ke), bf16_of_codes(k[1], true, ke)};
+                v = u32x4{bf16_of_codes(v[0], false, ve), bf16_of_codes(v[0], true, ve), bf16_of_codes(v[1], false, ve), bf16_of_codes(v[1], true, ve)};
+            }
+            if (a.c.D != DP && !there) k = v = u32x4{0, 0, 0, 0};
+            // tokens that no row of the workgroup sees may hold anything
+            if (cut && (t0 + t >= end || !(ok_next >> (t >> 4) & 1))) v = u32x4{0, 0, 0, 0};
+            const int at = t * S::BYTES + 16 * (mc ^ bank(t));
+            *reinterpret_cast<u32x4 *>(keys[buffer] + at) = k;
+            *reinterpret_cast<u32x4 *>(values[buffer] + at) = v;
+            if (t0 + S::TOK > least) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) fine &= bf16_pair_finite(v[j]);
+            }
+        }
+        const int any = !__all(fine);
+        if (lane == 0) odd[buffer][wave] = any;
+    };
+
+    // ---- the lane's places in a tile ----
+    // keys: row i of a score tile is token swap(i) (bits 2 and 3 exchanged), of which bank() is i & 7; chunk 2c + h
+    const int kt = (row & 0x13) | (row & 4) << 1 | (row & 8) >> 1;
+    int kat[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) kat[c] = kt * S::BYTES + 16 * ((2 * c + h) ^ (row & 7));
+    // values: 16 lanes turn 4 tokens x 16 elements; tokens 8h + 4i + (lane / 4 mod 4), elements 16 (lane / 16 mod 2) + 4 (lane mod 4) of 32
+    const int vt = 8 * h + (lane >> 2 & 3), vc = 2 * (lane >> 4 & 1) + (lane >> 1 & 1), vb = (lane >> 2 & 3) | h << 2;
+    int vat[2];
+#pragma unroll
+    for (int d = 0; d < 2; ++d) vat[d] = vt * S::BYTES + 16 * ((4 * d + vc) ^ vb) + 8 * (lane & 1);
+
+    if (w.begin < end) {
+        fetch(w.begin);
+        put(w.begin, 0);
+    }
+    int buffer = 0;
+    for (int t0 = w.begin; t0 < end; t0 += S::TOK, buffer ^= 1) {
+        __syncthreads();
+        const uint32_t ok = ok_next;
+        const bool more = t0 + S::TOK < end;
+        if (more) fetch(t0 + S::TOK);
+        if (t0 < high) {
+            const char *const kb = keys[buffer], *const vb = values[buffer];
+            float16_t sc[TT];
+#pragma unroll
+            for (int t = 0; t < TT; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sc[t][i] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < TT * (DP / 16); ++i) {
+                const int t = i % TT, c = i / TT;
+                sc[t] = mfma(*reinterpret_cast<const u32x4 *>(kb + kat[c & 3] + (c >> 2) * 128 + t * 32 * S::BYTES), q[c], sc[t]);
+            }
+            // four fragments on their way in front of the products
+            __builtin_amdgcn_sched_group_barrier(kLdsReads, 4, 0);
+#pragma unroll
+            for (int i = 0; i < TT * (DP / 16) - 4; ++i) {
+                __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kLdsReads, 1, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(kMatrix, 4, 0);
+            const bool whole = t0 + S::TOK <= low && ok == (1u << S::GROUPS) - 1;
+            if (!whole) {
+                const int sees = limit - t0 - 8 * h;
+#pragma unroll
+                for (int t = 0; t < TT; ++t)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int run = 2 * t + (i >> 3);
+                        if (16 * run + (i & 7) >= (ok >> run & 1 ? sees : 0)) sc[t][i] = -INFINITY;
+                    }
+            }
+            float tops[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                tops[j] = sc[0][j];
+#pragma unroll
+                for (int i = 1; i < 4 * TT; ++i) tops[j] = fmaxf(tops[j], sc[i / 4][4 * (i & 3) + j]);
+            }
+            float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+            top = max32(top) * a.scale2;
+            if (__any(top > m)) {
+                const float to = fmaxf(m, top), by = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - to);
+                l *= by;
+#pragma unroll
+                for (int d = 0; d < DT; ++d) o[d] *= by;
+                m = to;
+            }
+            const float mm = m == -INFINITY ? 0.0f : m;
+            // weights of the lane's eight tokens of run g
+            const auto weights = [&](int g) {
+                float e[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(sc[g / 2][8 * (g & 1) + i], a.scale2, -mm));
+                l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+                return u32x4{bf16_pair(e[0], e[1]), bf16_pair(e[2], e[3]), bf16_pair(e[4], e[5]), bf16_pair(e[6], e[7])};
+            };
+            const auto turned = [&](int g, int d) {
+                u32x4 f;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    typedef __attribute__((address_space(3))) short4_t *lds4;
+                    const u32x2 part = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (lds4)(vb + vat[d & 1] + (d >> 1) * 128 + (16 * g + 4 * i) * S::BYTES)));
+                    f[2 * i] = part[0], f[2 * i + 1] = part[1];
+                }
+                return f;
+            };
+            if (whole || !(odd[buffer][0] | odd[buffer][1] | odd[buffer][2] | odd[buffer][3])) {
+                // the next run's weights and values while the products take this one's
+                u32x4 p = weights(0), f[DT];
+#pragma unroll
+                for (int d = 0; d < DT; ++d) f[d] = turned(0, d);
+#pragma unroll
+                for (int g = 0; g < S::GROUPS; ++g) {
+                    u32x4 next[DT], pn;
+                    if (g + 1 < S::GROUPS) {
+#pragma unroll
+                        for (int d = 0; d < DT; ++d) next[d] = turned(g + 1, d);
+                        pn = weights(g + 1);
+                    }
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) o[d] = mfma(f[d], p, o[d]);
+                    if (g + 1 < S::GROUPS) {
+                        __builtin_amdgcn_sched_group_barrier(kLdsReads, 2 * DT, 0);
+#pragma unroll
+                        for (int d = 0; d < DT; ++d) {
+                            __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
+                            __builtin_amdgcn_sched_group_barrier(kVector, 28 / DT, 0);
+                        }
+                        p = pn;
+#pragma unroll
+                        for (int d = 0; d < DT; ++d) f[d] = next[d];
+                    }
+                }
+            } else {
+                // values that are not finite reach the rows that see them and no others: a product of each row's own
+                u32x4 p[S::GROUPS];
+#pragma unroll
+                for (int g = 0; g < S::GROUPS; ++g) p[g] = weights(g);
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+#pragma unroll 1
+                    for (int j = 0; j < 32; ++j) {
+                        const int sees = __shfl(limit, j, 64) - t0 - 8 * h;
+                        float16_t own;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) own[i] = 0.0f;
+#pragma unroll
+                        for (int g = 0; g < S::GROUPS; ++g) own = mfma(first_tokens(turned(g, d), sees - 16 * g), p[g], own);
+                        if (row == j) o[d] += own;
+                    }
+                }
+            }
+        }
+        if (more) put(t0 + S::TOK, buffer ^ 1);
+    }
+
+    float sum = sum32(l);
+    if (sum != sum) m = INFINITY;                             // no part that has seen a NaN counts as empty, or is outweighed
+    if (!valid) return;
+    if (w.parts == 1) {
+        const float by = over(sum);
+        uint16_t *const p = a.out + (int64_t)(w.first + r / a.G) * a.ldo + (int64_t)(head * a.G + r % a.G) * a.c.D;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int at = 32 * d + 8 * j + 4 * h;
+                typedef uint32_t bf16x4_at2 __attribute__((ext_vector_type(2), aligned(2)));
+                if (at < a.c.D)
+                    *reinterpret_cast<bf16x4_at2 *>(p + at) = bf16x4_at2{bf16_pair(o[d][4 * j] * by, o[d][4 * j + 1] * by), bf16_pair(o[d][4 * j + 2] * by, o[d][4 * j + 3] * by)};
+            }
+    } else {
+        const int64_t slot = (w.slot * a.c.heads + head) * ROWS + wave * 32 + row;
+        float *const p = (PREFIX ? a.prefix_o : a.own_o) + slot * a.c.D;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int at = 32 * d + 8 * j + 4 * h;
+                if (at < a.c.D) *reinterpret_cast<float4_t *>(p + at) = float4_t{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]};
+            }
+        if (h == 0) (PREFIX ? a.prefix_ml : a.own_ml)[slot] = float2_t{m, sum};
+    }
+}
+
+template <int DP, bool BITS8> void run(const AttnArgs &a, bool prefix, int64_t items, hipStream_t st)
+{
+    const unsigned grid = (unsigned)(items * a.c.heads);
+    if (prefix) attn_wide_kernel<DP, BITS8, true><<<grid, kThreads, 0, st>>>(a);
+    else attn_wide_kernel<DP, BITS8, false><<<grid, kThreads, 0, st>>>(a);
+}
+
+}  // namespace
+
+hipError_t launch_attn_wide(const AttnArgs &a, bool prefix, int64_t items, hipStream_t st)
+{
+    if (a.c.D <= 64) a.c.bits8 ? run<64, true>(a, prefix, items, st) : run<64, false>(a, prefix, items, st);
+    else a.c.bits8 ? run<128, true>(a, prefix, items, st) : run<128, false>(a, prefix, items, st);
+    return hipGetLastError();
+}
+
+}  // namespace tj

@@ -37,7 +37,8 @@ hipError_t launch_kv_append(const RowSrc &q, int Hq, const RowSrc &k, const RowS
                             const RowDst &qo, hipStream_t st);
 hipError_t launch_kv_load(const KvCache &c, const KvBatch &b, int64_t N, const RowDst &k, const RowDst &v, hipStream_t st);
 
-size_t attn_workspace_bytes(int64_t N, int Hq, int heads, int D, int B, int64_t prefix);
+// tokens: the most that a sequence can have of its own
+size_t attn_workspace_bytes(int64_t N, int Hq, int heads, int D, int B, int64_t tokens, int64_t prefix);
 hipError_t launch_attn(const uint16_t *q, int64_t ldq, int64_t N, int Hq, const KvCache &c, const KvBatch &b, float scale, uint16_t *out, int64_t ldo,
                        void *ws, hipStream_t st);
 
