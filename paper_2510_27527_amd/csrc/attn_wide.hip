@@ -31,9 +31,15 @@ __device__ __forceinline__ float sum32(float v)
     return u2f(b[0]) + u2f(b[1]);
 }
 
-// Rows of a tile lie in LDS one after the other, their 16-byte chunks exchanged by the token: chunk c of token t is at c ^ bank(t).  The lanes that read at once (eight
-// tokens' same chunk of keys, eight tokens' 64 bytes of values) then meet all banks alike.
-__device__ __forceinline__ int bank(int t) { return (t & 3) | (t >> 1 & 4); }
+// Rows of a tile lie in LDS one after the other, their 16-byte chunks exchanged by the token: chunk c of token t is at c ^ bank(t).  The lanes that read at once then meet all
+// banks alike, whether 128 or 256 bytes are read in a step: 8 or 16 tokens' same chunk of keys (tokens that differ in bits 0, 1, 3 and 2), or 32 or 64 bytes of each of
+// four tokens' values (bits 0 and 1).
+template <int DP> __device__ __forceinline__ int bank(int t)
+{
+    return DP > 64 ? (t & 1) * 10 ^ (t & 2) * 2 ^ (t >> 3 & 1) ^ (t & 4) * 2 : (t & 1) * 2 ^ (t & 2) * 2 ^ (t >> 3 & 1) ^ (t >> 1 & 2);
+}
+// byte of chunk c of token t
+template <int DP> __device__ __forceinline__ int place(int t, int c) { return t * 2 * DP + 16 * (c ^ bank<DP>(t)); }
 
 template <int DP> struct Shape {
     static constexpr int TOK = DP > 128 ? 32 : 64;           // tokens of a tile
@@ -137,7 +143,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_wide_kernel(AttnArgs a)
             if (a.c.D != DP && !there) k = v = u32x4{0, 0, 0, 0};
             // tokens that no row of the workgroup sees may hold anything
             if (cut && (t0 + t >= end || !(ok_next >> (t >> 4) & 1))) v = u32x4{0, 0, 0, 0};
-            const int at = t * S::BYTES + 16 * (mc ^ bank(t));
+            const int at = place<DP>(t, mc);
             *reinterpret_cast<u32x4 *>(keys[buffer] + at) = k;
             *reinterpret_cast<u32x4 *>(values[buffer] + at) = v;
             if (t0 + S::TOK > least) {
@@ -150,16 +156,17 @@ __global__ __launch_bounds__(kThreads, 2) void attn_wide_kernel(AttnArgs a)
     };
 
     // ---- the lane's places in a tile ----
-    // keys: row i of a score tile is token swap(i) (bits 2 and 3 exchanged), of which bank() is i & 7; chunk 2c + h
+    // keys: row i of a score tile is the token that has bits 2 and 3 exchanged; chunk 2c + h
     const int kt = (row & 0x13) | (row & 4) << 1 | (row & 8) >> 1;
-    int kat[4];
+    int kat[DP / 16];
 #pragma unroll
-    for (int c = 0; c < 4; ++c) kat[c] = kt * S::BYTES + 16 * ((2 * c + h) ^ (row & 7));
+    for (int c = 0; c < DP / 16; ++c) kat[c] = place<DP>(kt, 2 * c + h);
     // values: 16 lanes turn 4 tokens x 16 elements; tokens 8h + 4i + (lane / 4 mod 4), elements 16 (lane / 16 mod 2) + 4 (lane mod 4) of 32
-    const int vt = 8 * h + (lane >> 2 & 3), vc = 2 * (lane >> 4 & 1) + (lane >> 1 & 1), vb = (lane >> 2 & 3) | h << 2;
-    int vat[2];
+    int vat[2][DT];
 #pragma unroll
-    for (int d = 0; d < 2; ++d) vat[d] = vt * S::BYTES + 16 * ((4 * d + vc) ^ vb) + 8 * (lane & 1);
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) vat[i][d] = place<DP>(8 * h + 4 * i + (lane >> 2 & 3), 4 * d + 2 * (lane >> 4 & 1) + (lane >> 1 & 1)) + 8 * (lane & 1);
 
     if (w.begin < end) {
         fetch(w.begin);
@@ -181,7 +188,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_wide_kernel(AttnArgs a)
 #pragma unroll
             for (int i = 0; i < TT * (DP / 16); ++i) {
                 const int t = i % TT, c = i / TT;
-                sc[t] = mfma(*reinterpret_cast<const u32x4 *>(kb + kat[c & 3] + (c >> 2) * 128 + t * 32 * S::BYTES), q[c], sc[t]);
+                sc[t] = mfma(*reinterpret_cast<const u32x4 *>(kb + kat[c] + t * 32 * S::BYTES), q[c], sc[t]);
             }
             // four fragments on their way in front of the products
             __builtin_amdgcn_sched_group_barrier(kLdsReads, 4, 0);
@@ -233,7 +240,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_wide_kernel(AttnArgs a)
                 for (int i = 0; i < 2; ++i) {
                     typedef __attribute__((address_space(3))) short4_t *lds4;
                     const u32x2 part = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (lds4)(vb + vat[d & 1] + (d >> 1) * 128 + (16 * g + 4 * i) * S::BYTES)));
+                        (lds4)(vb + vat[i][d] + 16 * g * S::BYTES)));
                     f[2 * i] = part[0], f[2 * i + 1] = part[1];
                 }
                 return f;
