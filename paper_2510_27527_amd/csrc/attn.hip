@@ -155,7 +155,7 @@ template <int DP> __device__ __forceinline__ u32x4 weigh(const float4_t (&sc)[2]
     }
     float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
     top = max16_32(top);
-    if (__any(top > s.m)) {
+    if (__any(top > s.m + kSlack)) {
         const float m = fmaxf(s.m, top);
         const float by = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(s.m - m);
         s.l *= by;

@@ -18,6 +18,10 @@ constexpr int kThreads = 256;
 constexpr int kWaves = 4;
 constexpr int kUnit = 64;                 // tokens in which the parts' lengths are counted
 
+// The maximum that a row's weights are taken from is moved when scores exceed it by more than this (of log2): weights are up to 2^8 then, which loses nothing, and what was summed
+// is rarely scaled.
+constexpr float kSlack = 8.0f;
+
 struct AttnArgs {
     const uint16_t *q;
     int64_t ldq;

@@ -4,6 +4,8 @@
 // each and share tiles of 64 tokens in LDS, the next tile on its way in registers.  Products: scores^T [tokens x rows] = K Q^T and out^T [D x rows] += V^T P^T, 32 x 32 x 16
 // each; the tokens are dealt to the rows of a score tile so that a lane ends up with the weights that the second product takes from it.  Values lie in LDS as rows of tokens and are turned by the
 // transposing LDS reads.  8-bit caches become bf16 on their way into LDS, once for all four waves.
+#include <type_traits>
+
 #include "attn_common.h"
 
 namespace tj {
@@ -55,15 +57,16 @@ template <int DP, bool BITS8> struct Moved {
     u32x4 k[Shape<DP>::MOVES], v[Shape<DP>::MOVES];          // 8 bits: codes in the first two words, the exponent in the third
 };
 
-template <int DP, bool BITS8, bool PREFIX>
+// EXACT: heads of DP elements, else of fewer
+template <int DP, bool EXACT, bool BITS8, bool PREFIX>
 __global__ __launch_bounds__(kThreads, 2) void attn_wide_kernel(AttnArgs a)
 {
     using S = Shape<DP>;
     constexpr int ROWS = kWideRows, TT = S::TOK / 32, DT = DP / 32;
     __shared__ int64_t lds[kWaves];
-    __shared__ int odd[2][kWaves];                            // whether a wave has put a value that is not finite and that not every row sees
-    __shared__ __align__(16) char keys[2][S::TOK * S::BYTES];
-    __shared__ __align__(16) char values[2][S::TOK * S::BYTES];
+    __shared__ int odd[2][kWaves];                            // of a tile that not every row sees: whether a wave has put a value that is not finite
+    __shared__ __align__(16) char keys[2 * S::TOK * S::BYTES];
+    __shared__ __align__(16) char values[2 * S::TOK * S::BYTES];
     const int head = blockIdx.x % a.c.heads, item = blockIdx.x / a.c.heads;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const int row = lane & 31, h = lane >> 5;
@@ -80,7 +83,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_wide_kernel(AttnArgs a)
     for (int c = 0; c < DP / 16; ++c) {
         const int d = 16 * c + 8 * h;
         q[c] = u32x4{0, 0, 0, 0};
-        if (valid && d < a.c.D) q[c] = *reinterpret_cast<const bf16x8_at2 *>(qp + d);
+        if (valid && (EXACT || d < a.c.D)) q[c] = *reinterpret_cast<const bf16x8_at2 *>(qp + d);
     }
     const int least = min(sees_of<PREFIX>(a, w, w.tile * ROWS), end);         // that a row of the workgroup sees
     // the least and the most that a row of the wave sees
@@ -128,31 +131,41 @@ __global__ __launch_bounds__(kThreads, 2) void attn_wide_kernel(AttnArgs a)
         }
         ++held;
     };
+    // whether some row does not see some token of the tile
+    const auto edge = [&](int t0, uint32_t ok) { return t0 + S::TOK > least || ok != (1u << S::GROUPS) - 1; };
     const auto put = [&](int t0, int buffer) {
-        bool fine = true;
-        const bool cut = t0 + S::TOK > end || ok_next != (1u << S::GROUPS) - 1;
+        if constexpr (BITS8) {
 #pragma unroll
-        for (int i = 0; i < S::MOVES; ++i) {
-            const int t = i * S::PER + mt;
-            u32x4 k = x.k[i], v = x.v[i];
-            if constexpr (BITS8) {
+            for (int i = 0; i < S::MOVES; ++i) {
+                const u32x4 k = x.k[i], v = x.v[i];
                 const float ke = power_of(k[2], 0), ve = power_of(v[2], 0);
-                k = u32x4{bf16_of_codes(k[0], false, ke), bf16_of_codes(k[0], true, ke), bf16_of_codes(k[1], false, ke), bf16_of_codes(k[1], true, ke)};
-                v = u32x4{bf16_of_codes(v[0], false, ve), bf16_of_codes(v[0], true, ve), bf16_of_codes(v[1], false, ve), bf16_of_codes(v[1], true, ve)};
-            }
-            if (a.c.D != DP && !there) k = v = u32x4{0, 0, 0, 0};
-            // tokens that no row of the workgroup sees may hold anything
-            if (cut && (t0 + t >= end || !(ok_next >> (t >> 4) & 1))) v = u32x4{0, 0, 0, 0};
-            const int at = place<DP>(t, mc);
-            *reinterpret_cast<u32x4 *>(keys[buffer] + at) = k;
-            *reinterpret_cast<u32x4 *>(values[buffer] + at) = v;
-            if (t0 + S::TOK > least) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) fine &= bf16_pair_finite(v[j]);
+                x.k[i] = u32x4{bf16_of_codes(k[0], false, ke), bf16_of_codes(k[0], true, ke), bf16_of_codes(k[1], false, ke), bf16_of_codes(k[1], true, ke)};
+                x.v[i] = u32x4{bf16_of_codes(v[0], false, ve), bf16_of_codes(v[0], true, ve), bf16_of_codes(v[1], false, ve), bf16_of_codes(v[1], true, ve)};
             }
         }
-        const int any = !__all(fine);
-        if (lane == 0) odd[buffer][wave] = any;
+        if (!EXACT && !there) {
+#pragma unroll
+            for (int i = 0; i < S::MOVES; ++i) x.k[i] = x.v[i] = u32x4{0, 0, 0, 0};
+        }
+        if (edge(t0, ok_next)) {
+            bool fine = true;
+#pragma unroll
+            for (int i = 0; i < S::MOVES; ++i) {
+                const int t = i * S::PER + mt;
+                // tokens that no row of the workgroup sees may hold anything
+                if (t0 + t >= end || !(ok_next >> (t >> 4) & 1)) x.v[i] = u32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) fine &= bf16_pair_finite(x.v[i][j]);
+            }
+            const int any = !__all(fine);
+            if (lane == 0) odd[buffer][wave] = any;
+        }
+#pragma unroll
+        for (int i = 0; i < S::MOVES; ++i) {
+            const int at = buffer * S::TOK * S::BYTES + place<DP>(i * S::PER + mt, mc);
+            *reinterpret_cast<u32x4 *>(keys + at) = x.k[i];
+            *reinterpret_cast<u32x4 *>(values + at) = x.v[i];
+        }
     };
 
     // ---- the lane's places in a tile ----
@@ -168,132 +181,141 @@ __global__ __launch_bounds__(kThreads, 2) void attn_wide_kernel(AttnArgs a)
 #pragma unroll
         for (int d = 0; d < DT; ++d) vat[i][d] = place<DP>(8 * h + 4 * i + (lane >> 2 & 3), 4 * d + 2 * (lane >> 4 & 1) + (lane >> 1 & 1)) + 8 * (lane & 1);
 
+    // One tile.  ODD: it has values that are not finite: they reach the rows that see them and no others, by a product of each row's own.
+    const auto take = [&](int t0, int buffer, uint32_t ok, auto is_odd) {
+        constexpr bool ODD = decltype(is_odd)::value;
+        const int in = buffer * S::TOK * S::BYTES;
+        float16_t sc[TT];
+#pragma unroll
+        for (int i = 0; i < TT * (DP / 16); ++i) {
+            const int t = i % TT, c = i / TT;
+            const u32x4 k = *reinterpret_cast<const u32x4 *>(keys + (kat[c] + in) + t * 32 * S::BYTES);
+            if (c == 0) sc[t] = mfma(k, q[c], float16_t{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0});
+            else sc[t] = mfma(k, q[c], sc[t]);
+        }
+        // four fragments on their way in front of the products
+        __builtin_amdgcn_sched_group_barrier(kLdsReads, 4, 0);
+#pragma unroll
+        for (int i = 0; i < TT * (DP / 16) - 4; ++i) {
+            __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(kLdsReads, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(kMatrix, 4, 0);
+        const bool whole = t0 + S::TOK <= low && ok == (1u << S::GROUPS) - 1;
+        if (!whole) {
+            const int sees = limit - t0 - 8 * h;
+#pragma unroll
+            for (int t = 0; t < TT; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int run = 2 * t + (i >> 3);
+                    if (16 * run + (i & 7) >= (ok >> run & 1 ? sees : 0)) sc[t][i] = -INFINITY;
+                }
+        }
+        float tops[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            tops[j] = sc[0][j];
+#pragma unroll
+            for (int i = 1; i < 4 * TT; ++i) tops[j] = fmaxf(tops[j], sc[i / 4][4 * (i & 3) + j]);
+        }
+        float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+        top = max32(top) * a.scale2;
+        if (__any(top > m + kSlack)) {
+            const float to = fmaxf(m, top), by = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - to);
+            l *= by;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d] *= by;
+            m = to;
+        }
+        const float mm = m == -INFINITY ? 0.0f : m;
+        // weights of the lane's eight tokens of run g
+        const auto weights = [&](int g) {
+            float e[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(sc[g / 2][8 * (g & 1) + i], a.scale2, -mm));
+            l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+            return u32x4{bf16_pair(e[0], e[1]), bf16_pair(e[2], e[3]), bf16_pair(e[4], e[5]), bf16_pair(e[6], e[7])};
+        };
+        const auto turned = [&](int g, int d) {
+            u32x4 f;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                typedef __attribute__((address_space(3))) short4_t *lds4;
+                const u32x2 part = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (lds4)(values + (vat[i][d] + in) + 16 * g * S::BYTES)));
+                f[2 * i] = part[0], f[2 * i + 1] = part[1];
+            }
+            return f;
+        };
+        if constexpr (!ODD) {
+            // the next run's weights and values while the products take this one's
+            u32x4 p = weights(0), f[DT];
+#pragma unroll
+            for (int d = 0; d < DT; ++d) f[d] = turned(0, d);
+#pragma unroll
+            for (int g = 0; g < S::GROUPS; ++g) {
+                u32x4 next[DT], pn;
+                if (g + 1 < S::GROUPS) {
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) next[d] = turned(g + 1, d);
+                    pn = weights(g + 1);
+                }
+#pragma unroll
+                for (int d = 0; d < DT; ++d) o[d] = mfma(f[d], p, o[d]);
+                if (g + 1 < S::GROUPS) {
+                    __builtin_amdgcn_sched_group_barrier(kLdsReads, 2 * DT, 0);
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) {
+                        __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
+                        __builtin_amdgcn_sched_group_barrier(kVector, 28 / DT, 0);
+                    }
+                    p = pn;
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) f[d] = next[d];
+                }
+            }
+        } else {
+            // values that are not finite reach the rows that see them and no others: a product of each row's own
+            u32x4 p[S::GROUPS];
+#pragma unroll
+            for (int g = 0; g < S::GROUPS; ++g) p[g] = weights(g);
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+#pragma unroll 1
+                for (int j = 0; j < 32; ++j) {
+                    const int sees = __shfl(limit, j, 64) - t0 - 8 * h;
+                    float16_t own;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) own[i] = 0.0f;
+#pragma unroll
+                    for (int g = 0; g < S::GROUPS; ++g) own = mfma(first_tokens(turned(g, d), sees - 16 * g), p[g], own);
+                    if (row == j) o[d] += own;
+                }
+            }
+        }
+    };
+
     if (w.begin < end) {
         fetch(w.begin);
         put(w.begin, 0);
     }
-    int buffer = 0;
-    for (int t0 = w.begin; t0 < end; t0 += S::TOK, buffer ^= 1) {
-        __syncthreads();
-        const uint32_t ok = ok_next;
-        const bool more = t0 + S::TOK < end;
-        if (more) fetch(t0 + S::TOK);
-        if (t0 < high) {
-            const char *const kb = keys[buffer], *const vb = values[buffer];
-            float16_t sc[TT];
-#pragma unroll
-            for (int t = 0; t < TT; ++t)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) sc[t][i] = 0.0f;
-#pragma unroll
-            for (int i = 0; i < TT * (DP / 16); ++i) {
-                const int t = i % TT, c = i / TT;
-                sc[t] = mfma(*reinterpret_cast<const u32x4 *>(kb + kat[c] + t * 32 * S::BYTES), q[c], sc[t]);
-            }
-            // four fragments on their way in front of the products
-            __builtin_amdgcn_sched_group_barrier(kLdsReads, 4, 0);
-#pragma unroll
-            for (int i = 0; i < TT * (DP / 16) - 4; ++i) {
-                __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(kLdsReads, 1, 0);
-            }
-            __builtin_amdgcn_sched_group_barrier(kMatrix, 4, 0);
-            const bool whole = t0 + S::TOK <= low && ok == (1u << S::GROUPS) - 1;
-            if (!whole) {
-                const int sees = limit - t0 - 8 * h;
-#pragma unroll
-                for (int t = 0; t < TT; ++t)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int run = 2 * t + (i >> 3);
-                        if (16 * run + (i & 7) >= (ok >> run & 1 ? sees : 0)) sc[t][i] = -INFINITY;
-                    }
-            }
-            float tops[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                tops[j] = sc[0][j];
-#pragma unroll
-                for (int i = 1; i < 4 * TT; ++i) tops[j] = fmaxf(tops[j], sc[i / 4][4 * (i & 3) + j]);
-            }
-            float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-            top = max32(top) * a.scale2;
-            if (__any(top > m)) {
-                const float to = fmaxf(m, top), by = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - to);
-                l *= by;
-#pragma unroll
-                for (int d = 0; d < DT; ++d) o[d] *= by;
-                m = to;
-            }
-            const float mm = m == -INFINITY ? 0.0f : m;
-            // weights of the lane's eight tokens of run g
-            const auto weights = [&](int g) {
-                float e[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(sc[g / 2][8 * (g & 1) + i], a.scale2, -mm));
-                l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
-                return u32x4{bf16_pair(e[0], e[1]), bf16_pair(e[2], e[3]), bf16_pair(e[4], e[5]), bf16_pair(e[6], e[7])};
-            };
-            const auto turned = [&](int g, int d) {
-                u32x4 f;
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    typedef __attribute__((address_space(3))) short4_t *lds4;
-                    const u32x2 part = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (lds4)(vb + vat[i][d] + 16 * g * S::BYTES)));
-                    f[2 * i] = part[0], f[2 * i + 1] = part[1];
-                }
-                return f;
-            };
-            if (whole || !(odd[buffer][0] | odd[buffer][1] | odd[buffer][2] | odd[buffer][3])) {
-                // the next run's weights and values while the products take this one's
-                u32x4 p = weights(0), f[DT];
-#pragma unroll
-                for (int d = 0; d < DT; ++d) f[d] = turned(0, d);
-#pragma unroll
-                for (int g = 0; g < S::GROUPS; ++g) {
-                    u32x4 next[DT], pn;
-                    if (g + 1 < S::GROUPS) {
-#pragma unroll
-                        for (int d = 0; d < DT; ++d) next[d] = turned(g + 1, d);
-                        pn = weights(g + 1);
-                    }
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) o[d] = mfma(f[d], p, o[d]);
-                    if (g + 1 < S::GROUPS) {
-                        __builtin_amdgcn_sched_group_barrier(kLdsReads, 2 * DT, 0);
-#pragma unroll
-                        for (int d = 0; d < DT; ++d) {
-                            __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
-                            __builtin_amdgcn_sched_group_barrier(kVector, 28 / DT, 0);
-                        }
-                        p = pn;
-#pragma unroll
-                        for (int d = 0; d < DT; ++d) f[d] = next[d];
-                    }
-                }
-            } else {
-                // values that are not finite reach the rows that see them and no others: a product of each row's own
-                u32x4 p[S::GROUPS];
-#pragma unroll
-                for (int g = 0; g < S::GROUPS; ++g) p[g] = weights(g);
-#pragma unroll
-                for (int d = 0; d < DT; ++d) {
-#pragma unroll 1
-                    for (int j = 0; j < 32; ++j) {
-                        const int sees = __shfl(limit, j, 64) - t0 - 8 * h;
-                        float16_t own;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) own[i] = 0.0f;
-#pragma unroll
-                        for (int g = 0; g < S::GROUPS; ++g) own = mfma(first_tokens(turned(g, d), sees - 16 * g), p[g], own);
-                        if (row == j) o[d] += own;
-                    }
-                }
-            }
+    int buffer = 0, t0 = w.begin;
+    const auto walk = [&](auto is_odd) {
+        for (; t0 < end; t0 += S::TOK, buffer ^= 1) {
+            __syncthreads();
+            const uint32_t ok = ok_next;
+            if constexpr (!decltype(is_odd)::value)
+                if (edge(t0, ok) && (odd[buffer][0] | odd[buffer][1] | odd[buffer][2] | odd[buffer][3])) break;
+            const bool more = t0 + S::TOK < end;
+            if (more) fetch(t0 + S::TOK);
+            if (t0 < high) take(t0, buffer, ok, is_odd);
+            if (more) put(t0 + S::TOK, buffer ^ 1);
         }
-        if (more) put(t0 + S::TOK, buffer ^ 1);
-    }
+    };
+    // From the first tile with values that are not finite and that not every row sees, a second loop: the first one's registers stay where they are.
+    walk(std::false_type());
+    walk(std::true_type());
 
     float sum = sum32(l);
     if (sum != sum) m = INFINITY;                             // no part that has seen a NaN counts as empty, or is outweighed
@@ -307,7 +329,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_wide_kernel(AttnArgs a)
             for (int j = 0; j < 4; ++j) {
                 const int at = 32 * d + 8 * j + 4 * h;
                 typedef uint32_t bf16x4_at2 __attribute__((ext_vector_type(2), aligned(2)));
-                if (at < a.c.D)
+                if (EXACT || at < a.c.D)
                     *reinterpret_cast<bf16x4_at2 *>(p + at) = bf16x4_at2{bf16_pair(o[d][4 * j] * by, o[d][4 * j + 1] * by), bf16_pair(o[d][4 * j + 2] * by, o[d][4 * j + 3] * by)};
             }
     } else {
@@ -318,25 +340,30 @@ __global__ __launch_bounds__(kThreads, 2) void attn_wide_kernel(AttnArgs a)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int at = 32 * d + 8 * j + 4 * h;
-                if (at < a.c.D) *reinterpret_cast<float4_t *>(p + at) = float4_t{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]};
+                if (EXACT || at < a.c.D) *reinterpret_cast<float4_t *>(p + at) = float4_t{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]};
             }
         if (h == 0) (PREFIX ? a.prefix_ml : a.own_ml)[slot] = float2_t{m, sum};
     }
 }
 
-template <int DP, bool BITS8> void run(const AttnArgs &a, bool prefix, int64_t items, hipStream_t st)
+template <int DP, bool EXACT, bool BITS8> void run(const AttnArgs &a, bool prefix, int64_t items, hipStream_t st)
 {
     const unsigned grid = (unsigned)(items * a.c.heads);
-    if (prefix) attn_wide_kernel<DP, BITS8, true><<<grid, kThreads, 0, st>>>(a);
-    else attn_wide_kernel<DP, BITS8, false><<<grid, kThreads, 0, st>>>(a);
+    if (prefix) attn_wide_kernel<DP, EXACT, BITS8, true><<<grid, kThreads, 0, st>>>(a);
+    else attn_wide_kernel<DP, EXACT, BITS8, false><<<grid, kThreads, 0, st>>>(a);
+}
+template <int DP> void run(const AttnArgs &a, bool prefix, int64_t items, hipStream_t st)
+{
+    if (a.c.D == DP) a.c.bits8 ? run<DP, true, true>(a, prefix, items, st) : run<DP, true, false>(a, prefix, items, st);
+    else a.c.bits8 ? run<DP, false, true>(a, prefix, items, st) : run<DP, false, false>(a, prefix, items, st);
 }
 
 }  // namespace
 
 hipError_t launch_attn_wide(const AttnArgs &a, bool prefix, int64_t items, hipStream_t st)
 {
-    if (a.c.D <= 64) a.c.bits8 ? run<64, true>(a, prefix, items, st) : run<64, false>(a, prefix, items, st);
-    else a.c.bits8 ? run<128, true>(a, prefix, items, st) : run<128, false>(a, prefix, items, st);
+    if (a.c.D <= 64) run<64>(a, prefix, items, st);
+    else run<128>(a, prefix, items, st);
     return hipGetLastError();
 }
 
