@@ -226,14 +226,13 @@ template <int DP, bool BITS8, bool PREFIX>
 __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attn_kernel(AttnArgs a)
 {
     constexpr int DV = DP / 16, LD = DP + 4;
-    __shared__ int64_t lds[kWaves];
     __shared__ __align__(16) float part[kWaves][kTile][LD];
     __shared__ float2_t part_ml[kWaves][kTile];
     const int head = blockIdx.x % a.c.heads, item = blockIdx.x / a.c.heads;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const int row = lane & 15, g = lane >> 4;
     Work w;
-    if (!work_of<PREFIX>(a, item, lds, w)) return;
+    if (!work_of<PREFIX>(a, item, w)) return;
     const int first = w.first, r = w.tile * kTile + row, rows = w.count * a.G;
     int high = sees_of<PREFIX>(a, w, w.tile * kTile + kTile - 1);
     const int begin = w.begin, end = min(w.end, high);
@@ -340,7 +339,6 @@ template <int DP>
 __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs a)
 {
     constexpr int L = DP / 4, GROUPS = kThreads / L;          // lanes of a part; parts at once
-    __shared__ int64_t lds[kWaves];
     __shared__ float4_t sums[GROUPS][L];
     __shared__ float2_t mls[GROUPS];
     const int head = blockIdx.x % a.Hq, n = blockIdx.x / a.Hq;
@@ -351,7 +349,7 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs a)
     if (n < first || n >= first + count) return;
     Place p;
     int part_units;
-    find(a, -1, b, p, part_units, lds);
+    find(a, -1, b, p, part_units);
     if (p.parts == 1 && !a.b.prefix) return;                  // written already
     if (p.base + (int64_t)tiles_of(count, a.G, a.own_rows) * p.parts > a.slots) return;      // starts that name rows twice
     const int kv = head / a.G, in_seq = (n - first) * a.G + head % a.G, in_all = n * a.G + head % a.G;
@@ -401,8 +399,10 @@ struct Cut {
     int64_t slots, items, prefix_items;        // of a key head
 };
 
-constexpr int kGroups = 2048;             // workgroups that a batch's own tokens are spread over where tiles have 16 rows
-constexpr int kWideGroups = 512;          // and more: two a CU
+// Workgroups that a batch's own tokens are spread over: where there are few tiles, all at once, two a CU; where there are many, whose lengths differ, four times as many, so that
+// none is left behind with much.  us, 512 / 1024 / 2048 workgroups: one sequence of 200000 tokens in 8 bits 77 / 85 / 98, 64 of 1024 to 8192 tokens 248 / 237 / 226.
+constexpr int kGroups = 512, kManyGroups = 2048;
+constexpr int kManyTiles = 256;
 
 int rows_of_tile(int64_t rows, int D) { return rows < 64 || D > 128 ? kTile : kWideRows; }
 
@@ -414,7 +414,7 @@ Cut cut_of(int64_t N, int Hq, int heads, int D, int B, int64_t tokens, int64_t p
     p.min_units = p.own_rows == kTile ? 2 : 4;
     const int64_t tiles = N * G / p.own_rows + B, units = (tokens + kUnit - 1) / kUnit;
     // Enough tiles of several rows: nothing is cut.  Else the own tokens are cut, also where there are many sequences: their lengths differ.
-    const int64_t groups = p.own_rows == kTile ? kGroups : kWideGroups;
+    const int64_t groups = p.own_rows == kTile && tiles * heads > kManyTiles ? kManyGroups : kGroups;
     const bool cut = (N <= 2 * B || tiles * heads < groups) && units > p.min_units;
     p.target = cut ? (int)((groups + heads - 1) / heads) : 0;
     const int64_t most = cut ? (units + p.min_units - 1) / p.min_units : 1;                // parts of a tile
@@ -424,8 +424,8 @@ Cut cut_of(int64_t N, int Hq, int heads, int D, int B, int64_t tokens, int64_t p
     p.prefix_items = 0;
     if (prefix > 0) {
         p.prefix_rows = rows_of_tile(N * G, D);
-        const int64_t tiles = (N * G + p.prefix_rows - 1) / p.prefix_rows, wanted = p.prefix_rows == kTile ? kGroups / 2 : kWideGroups;
-        const int64_t units = (prefix + kUnit - 1) / kUnit, want = (wanted + tiles * heads - 1) / (tiles * heads);
+        const int64_t tiles = (N * G + p.prefix_rows - 1) / p.prefix_rows;
+        const int64_t units = (prefix + kUnit - 1) / kUnit, want = (kGroups + tiles * heads - 1) / (tiles * heads);
         int64_t part = (units + want - 1) / want;
         const int least = p.prefix_rows == kTile ? 2 : 4;
         part = part < least ? least : part;

@@ -49,19 +49,28 @@ struct Place {
 __device__ __forceinline__ int units(int tokens) { return (tokens + kUnit - 1) / kUnit; }
 __device__ __forceinline__ int tiles_of(int rows, int G, int of) { return (rows * G + of - 1) / of; }
 
-__device__ __forceinline__ int64_t block_sum_scan(int64_t v, int64_t *lds, int64_t &before)      // sum over the workgroup; before: over the threads in front
+// v of another lane by a DPP control, 0 where there is none or the row is masked.  Counts are doubles here: exact, and two words a move.
+template <int CTRL, int ROWS> __device__ __forceinline__ double lane_in_front(double v)
 {
-    int64_t incl = v;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int64_t t = __shfl_up((long long)incl, o, 64);
-        if ((int)(threadIdx.x & 63) >= o) incl += t;
-    }
+    const uint64_t u = (uint64_t)__double_as_longlong(v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, ROWS, 0xF, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, ROWS, 0xF, false);
+    return __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
+}
+// Sum over the workgroup; before: over the threads in front.  No barrier follows the last read of lds: the next call takes another array.
+__device__ __forceinline__ double block_sum_scan(double v, double *lds, double &before)
+{
+    double incl = v;
+    incl += lane_in_front<0x111, 0xF>(incl);                   // from 1, 2, 4 and 8 lanes in front, within rows of 16
+    incl += lane_in_front<0x112, 0xF>(incl);
+    incl += lane_in_front<0x114, 0xF>(incl);
+    incl += lane_in_front<0x118, 0xF>(incl);
+    incl += lane_in_front<0x142, 0xA>(incl);                   // the row in front's last lane, into rows 1 and 3
+    incl += lane_in_front<0x143, 0xC>(incl);                   // lane 31, into rows 2 and 3
     const int w = threadIdx.x >> 6;
-    __syncthreads();
     if ((threadIdx.x & 63) == 63) lds[w] = incl;
     __syncthreads();
-    int64_t total = 0;
+    double total = 0.0;
     before = incl - v;
 #pragma unroll
     for (int i = 0; i < kWaves; ++i) {
@@ -72,42 +81,56 @@ __device__ __forceinline__ int64_t block_sum_scan(int64_t v, int64_t *lds, int64
 }
 
 // Units of a part of the own tokens: all tiles' units over the parts wanted.  Then where slot `slot` lies (slot >= 0), or where sequence `seq` starts.
-// Every thread of the workgroup calls it; false: there is no such slot.
-__device__ inline bool find(const AttnArgs &a, int slot, int seq, Place &p, int &part_units, int64_t *lds)
+// Every thread of the workgroup calls it, once; false: there is no such slot.
+__device__ inline bool find(const AttnArgs &a, int slot, int seq, Place &p, int &part_units)
 {
     __shared__ Place found;
+    __shared__ double lds[2][kWaves];
     const int per = (a.b.B + kThreads - 1) / kThreads, b0 = threadIdx.x * per, b1 = min(b0 + per, a.b.B);
     if (threadIdx.x == 0) found.b = -1;
+    // tiles and units of a sequence; those of the thread's first are kept
+    const auto size_of = [&](int b, int &tiles, int &length) {
+        int first, count;
+        rows_of(a.b, b, a.N, first, count);
+        tiles = tiles_of(count, a.G, a.own_rows);
+        length = units(tokens_of(a.b, a.c, b));
+    };
+    int tiles0 = 0, length0 = 0;
+    if (b0 < b1) size_of(b0, tiles0, length0);
+    const auto sized = [&](int b, int &tiles, int &length) {
+        if (b == b0) tiles = tiles0, length = length0;
+        else size_of(b, tiles, length);
+    };
     part_units = 1 << 25;                                      // more than any sequence has
+    double at;
     if (a.target > 0) {
-        int64_t sum = 0;
+        double sum = 0.0;
         for (int b = b0; b < b1; ++b) {
-            int first, count;
-            rows_of(a.b, b, a.N, first, count);
-            sum += (int64_t)tiles_of(count, a.G, a.own_rows) * units(tokens_of(a.b, a.c, b));
+            int tiles, length;
+            sized(b, tiles, length);
+            sum += (double)tiles * (double)length;
         }
-        int64_t before;
-        const int64_t total = block_sum_scan(sum, lds, before), wanted = (total + a.target - 1) / a.target;
-        part_units = wanted < a.min_units ? a.min_units : wanted < part_units ? (int)wanted : part_units;
+        const double wanted = ceil(block_sum_scan(sum, lds[0], at) / (double)a.target);
+        part_units = wanted < (double)a.min_units ? a.min_units : wanted < (double)part_units ? (int)wanted : part_units;
     }
-    int64_t sum = 0, at;
+    double sum = 0.0;
     for (int b = b0; b < b1; ++b) {
-        int first, count;
-        rows_of(a.b, b, a.N, first, count);
-        sum += (int64_t)tiles_of(count, a.G, a.own_rows) * max(1, (units(tokens_of(a.b, a.c, b)) + part_units - 1) / part_units);
+        int tiles, length;
+        sized(b, tiles, length);
+        sum += (double)tiles * (double)max(1, (length + part_units - 1) / part_units);
     }
-    block_sum_scan(sum, lds, at);
+    block_sum_scan(sum, lds[1], at);
     for (int b = b0; b < b1; ++b) {
-        int first, count;
-        rows_of(a.b, b, a.N, first, count);
-        const int parts = max(1, (units(tokens_of(a.b, a.c, b)) + part_units - 1) / part_units);
-        const int64_t n = (int64_t)tiles_of(count, a.G, a.own_rows) * parts;
-        if (slot >= 0 ? slot >= at && slot < at + n : b == seq) {
-            const int in = slot >= 0 ? (int)(slot - at) : 0;
-            found = Place{b, in / parts, in % parts, parts, at};
+        int tiles, length;
+        sized(b, tiles, length);
+        const int parts = max(1, (length + part_units - 1) / part_units);
+        const double next = at + (double)tiles * (double)parts;
+        if (slot >= 0 ? (double)slot >= at && (double)slot < next : b == seq) {
+            const int in = slot >= 0 ? (int)((double)slot - at) : 0;
+            found = Place{b, in / parts, in % parts, parts, (int64_t)at};
             break;
         }
-        at += n;
+        at = next;
     }
     __syncthreads();
     p = found;
@@ -124,7 +147,7 @@ struct Work {
 };
 
 // Tile and part number `item` of a key head; false: there is none.  PREFIX: of all rows against the prefix; else of a sequence's against its own.  Every thread of the workgroup calls it.
-template <bool PREFIX> __device__ __forceinline__ bool work_of(const AttnArgs &a, int item, int64_t *lds, Work &w)
+template <bool PREFIX> __device__ __forceinline__ bool work_of(const AttnArgs &a, int item, Work &w)
 {
     if constexpr (PREFIX) {
         w.first = 0, w.count = a.N;
@@ -140,7 +163,7 @@ template <bool PREFIX> __device__ __forceinline__ bool work_of(const AttnArgs &a
     } else {
         Place p;
         int part_units;
-        if (!find(a, item, -1, p, part_units, lds)) return false;
+        if (!find(a, item, -1, p, part_units)) return false;
         rows_of(a.b, p.b, a.N, w.first, w.count);
         // the tiles that see most come first
         w.tile = tiles_of(w.count, a.G, a.own_rows) - 1 - p.tile;

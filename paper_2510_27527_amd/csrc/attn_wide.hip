@@ -20,8 +20,6 @@ __device__ __forceinline__ float16_t mfma(u32x4 a, u32x4 b, float16_t c)
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
 }
 
-constexpr int kVector = 2, kMatrix = 8, kLdsReads = 0x100;     // kinds of instructions whose order is laid down below
-
 __device__ __forceinline__ float max32(float v)             // over the two lanes that hold a row
 {
     const auto b = __builtin_amdgcn_permlane32_swap(f2u(v), f2u(v), false, false);
@@ -63,7 +61,6 @@ __global__ __launch_bounds__(kThreads, 2) void attn_wide_kernel(AttnArgs a)
 {
     using S = Shape<DP>;
     constexpr int ROWS = kWideRows, TT = S::TOK / 32, DT = DP / 32;
-    __shared__ int64_t lds[kWaves];
     __shared__ int odd[2][kWaves];                            // of a tile that not every row sees: whether a wave has put a value that is not finite
     __shared__ __align__(16) char keys[2 * S::TOK * S::BYTES];
     __shared__ __align__(16) char values[2 * S::TOK * S::BYTES];
@@ -71,7 +68,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_wide_kernel(AttnArgs a)
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const int row = lane & 31, h = lane >> 5;
     Work w;
-    if (!work_of<PREFIX>(a, item, lds, w)) return;
+    if (!work_of<PREFIX>(a, item, w)) return;
     const int rows = w.count * a.G, r0 = w.tile * ROWS + wave * 32;
     const int end = min(w.end, sees_of<PREFIX>(a, w, w.tile * ROWS + ROWS - 1));
     const int r = r0 + row;
@@ -193,14 +190,6 @@ __global__ __launch_bounds__(kThreads, 2) void attn_wide_kernel(AttnArgs a)
             if (c == 0) sc[t] = mfma(k, q[c], float16_t{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0});
             else sc[t] = mfma(k, q[c], sc[t]);
         }
-        // four fragments on their way in front of the products
-        __builtin_amdgcn_sched_group_barrier(kLdsReads, 4, 0);
-#pragma unroll
-        for (int i = 0; i < TT * (DP / 16) - 4; ++i) {
-            __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(kLdsReads, 1, 0);
-        }
-        __builtin_amdgcn_sched_group_barrier(kMatrix, 4, 0);
         const bool whole = t0 + S::TOK <= low && ok == (1u << S::GROUPS) - 1;
         if (!whole) {
             const int sees = limit - t0 - 8 * h;
@@ -264,12 +253,6 @@ __global__ __launch_bounds__(kThreads, 2) void attn_wide_kernel(AttnArgs a)
 #pragma unroll
                 for (int d = 0; d < DT; ++d) o[d] = mfma(f[d], p, o[d]);
                 if (g + 1 < S::GROUPS) {
-                    __builtin_amdgcn_sched_group_barrier(kLdsReads, 2 * DT, 0);
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) {
-                        __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
-                        __builtin_amdgcn_sched_group_barrier(kVector, 28 / DT, 0);
-                    }
                     p = pn;
 #pragma unroll
                     for (int d = 0; d < DT; ++d) f[d] = next[d];
@@ -296,21 +279,25 @@ __global__ __launch_bounds__(kThreads, 2) void attn_wide_kernel(AttnArgs a)
         }
     };
 
-    if (w.begin < end) {
-        fetch(w.begin);
-        put(w.begin, 0);
-    }
+    // The tile after the next is on its way from the moment that the next one is in LDS.
     int buffer = 0, t0 = w.begin;
+    uint32_t ok = 0;
+    const auto put_next = [&](int t, int to) {
+        put(t, to);
+        ok = ok_next;
+        if (t + S::TOK < end) fetch(t + S::TOK);
+    };
+    if (t0 < end) {
+        fetch(t0);
+        put_next(t0, 0);
+    }
     const auto walk = [&](auto is_odd) {
         for (; t0 < end; t0 += S::TOK, buffer ^= 1) {
             __syncthreads();
-            const uint32_t ok = ok_next;
             if constexpr (!decltype(is_odd)::value)
                 if (edge(t0, ok) && (odd[buffer][0] | odd[buffer][1] | odd[buffer][2] | odd[buffer][3])) break;
-            const bool more = t0 + S::TOK < end;
-            if (more) fetch(t0 + S::TOK);
             if (t0 < high) take(t0, buffer, ok, is_odd);
-            if (more) put(t0 + S::TOK, buffer ^ 1);
+            if (t0 + S::TOK < end) put_next(t0 + S::TOK, buffer ^ 1);
         }
     };
     // From the first tile with values that are not finite and that not every row sees, a second loop: the first one's registers stay where they are.
