@@ -347,22 +347,22 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs a)
     int first, count;
     rows_of(a.b, b, a.N, first, count);
     if (n < first || n >= first + count) return;
-    Place p;
-    int part_units;
-    find(a, -1, b, p, part_units);
-    if (p.parts == 1 && !a.b.prefix) return;                  // written already
-    if (p.base + (int64_t)tiles_of(count, a.G, a.own_rows) * p.parts > a.slots) return;      // starts that name rows twice
+    const int64_t base = a.lie[2 * b], parts64 = a.lie[2 * b + 1];
+    if (parts64 == 1 && !a.b.prefix) return;                  // written already
+    // starts that name rows twice can leave sequences without parts: what the workspace says of them then is no place in it
+    if (base < 0 || parts64 < 1 || parts64 > a.slots || base > a.slots - (int64_t)tiles_of(count, a.G, a.own_rows) * parts64) return;
+    const int parts = (int)parts64;
     const int kv = head / a.G, in_seq = (n - first) * a.G + head % a.G, in_all = n * a.G + head % a.G;
-    const int total = p.parts + a.prefix_parts;
+    const int total = parts + a.prefix_parts;
     const int lane = threadIdx.x % L, group = threadIdx.x / L;
     // the row's place among the parts of its tile: own parts, parts of the prefix
-    const int64_t own = ((p.base + (int64_t)(in_seq / a.own_rows) * p.parts) * a.c.heads + kv) * a.own_rows + in_seq % a.own_rows;
+    const int64_t own = ((base + (int64_t)(in_seq / a.own_rows) * parts) * a.c.heads + kv) * a.own_rows + in_seq % a.own_rows;
     const int64_t pre = a.prefix_parts ? ((int64_t)(in_all / a.prefix_rows) * a.prefix_parts * a.c.heads + kv) * a.prefix_rows + in_all % a.prefix_rows : 0;
     float m = -INFINITY, l = 0.0f;
     float4_t o = {0, 0, 0, 0};
     for (int i = group; i < total; i += GROUPS) {
-        const bool mine = i < p.parts;
-        const int64_t slot = mine ? own + (int64_t)i * a.c.heads * a.own_rows : pre + (int64_t)(i - p.parts) * a.c.heads * a.prefix_rows;
+        const bool mine = i < parts;
+        const int64_t slot = mine ? own + (int64_t)i * a.c.heads * a.own_rows : pre + (int64_t)(i - parts) * a.c.heads * a.prefix_rows;
         const float2_t ml = (mine ? a.own_ml : a.prefix_ml)[slot];
         const float4_t v = 4 * lane < a.c.D ? *reinterpret_cast<const float4_t *>((mine ? a.own_o : a.prefix_o) + slot * a.c.D + 4 * lane) : float4_t{0, 0, 0, 0};
         const float top = fmaxf(m, ml.x);
@@ -464,7 +464,7 @@ template <int DP, bool BITS8> hipError_t run(const AttnArgs &a, const Cut &p, hi
 size_t attn_workspace_bytes(int64_t N, int Hq, int heads, int D, int B, int64_t tokens, int64_t prefix)
 {
     const Cut p = cut_of(N, Hq, heads, D, B, tokens, prefix);
-    return (size_t)((own_parts(p, heads) + prefix_parts(p, heads)) * (D * 4 + 8));
+    return (size_t)((own_parts(p, heads) + prefix_parts(p, heads)) * (D * 4 + 8) + (p.slots > 0 ? (int64_t)B * 16 : 0));
 }
 
 hipError_t launch_attn(const uint16_t *q, int64_t ldq, int64_t N, int Hq, const KvCache &c, const KvBatch &b, float scale, uint16_t *out, int64_t ldo, void *ws,
@@ -475,7 +475,7 @@ hipError_t launch_attn(const uint16_t *q, int64_t ldq, int64_t N, int Hq, const 
     float *const o = static_cast<float *>(ws);
     float2_t *const ml = reinterpret_cast<float2_t *>(o + (own + pre) * c.D);
     const AttnArgs a{q, ldq, out, ldo, (int)N, Hq, Hq / c.heads, c, b, scale * 1.44269504088896340736f, p.target, p.min_units, p.own_rows, p.prefix_rows, p.slots, p.prefix_units,
-                     p.prefix_parts, o, o + own * c.D, ml, ml + own};
+                     p.prefix_parts, o, o + own * c.D, ml, ml + own, reinterpret_cast<int64_t *>(ml + own + pre)};
     if (c.D <= 64) return c.bits8 ? run<64, true>(a, p, st) : run<64, false>(a, p, st);
     if (c.D <= 128) return c.bits8 ? run<128, true>(a, p, st) : run<128, false>(a, p, st);
     return c.bits8 ? run<256, true>(a, p, st) : run<256, false>(a, p, st);

@@ -38,6 +38,7 @@ struct AttnArgs {
     int prefix_units, prefix_parts;       // units of a part of the prefix, and how many there are
     float *own_o, *prefix_o;              // [slot][key head][rows of a tile][D]
     float2_t *own_ml, *prefix_ml;         // [slot][key head][rows of a tile]: maximum (of log2), sum
+    int64_t *lie;                         // [B][2]: first slot of a sequence, parts of its tiles
 };
 
 // What a workgroup has to know of the batch: how many units a part has, and where a part lies.
@@ -80,9 +81,9 @@ __device__ __forceinline__ double block_sum_scan(double v, double *lds, double &
     return total;
 }
 
-// Units of a part of the own tokens: all tiles' units over the parts wanted.  Then where slot `slot` lies (slot >= 0), or where sequence `seq` starts.
+// Units of a part of the own tokens: all tiles' units over the parts wanted.  Then where slot `slot` lies.
 // Every thread of the workgroup calls it, once; false: there is no such slot.
-__device__ inline bool find(const AttnArgs &a, int slot, int seq, Place &p, int &part_units)
+__device__ inline bool find(const AttnArgs &a, int slot, Place &p, int &part_units)
 {
     __shared__ Place found;
     __shared__ double lds[2][kWaves];
@@ -125,8 +126,8 @@ __device__ inline bool find(const AttnArgs &a, int slot, int seq, Place &p, int 
         sized(b, tiles, length);
         const int parts = max(1, (length + part_units - 1) / part_units);
         const double next = at + (double)tiles * (double)parts;
-        if (slot >= 0 ? (double)slot >= at && (double)slot < next : b == seq) {
-            const int in = slot >= 0 ? (int)((double)slot - at) : 0;
+        if ((double)slot >= at && (double)slot < next) {
+            const int in = (int)((double)slot - at);
             found = Place{b, in / parts, in % parts, parts, (int64_t)at};
             break;
         }
@@ -163,12 +164,13 @@ template <bool PREFIX> __device__ __forceinline__ bool work_of(const AttnArgs &a
     } else {
         Place p;
         int part_units;
-        if (!find(a, item, -1, p, part_units)) return false;
+        if (!find(a, item, p, part_units)) return false;
         rows_of(a.b, p.b, a.N, w.first, w.count);
         // the tiles that see most come first
         w.tile = tiles_of(w.count, a.G, a.own_rows) - 1 - p.tile;
         w.slot = p.base + (int64_t)w.tile * p.parts + p.part;
         w.parts = a.b.prefix ? 2 : p.parts;
+        if (a.slots > 0 && blockIdx.x % a.c.heads == 0 && p.tile == 0 && p.part == 0 && threadIdx.x == 0) a.lie[2 * p.b] = p.base, a.lie[2 * p.b + 1] = p.parts;
         w.len = tokens_of(a.b, a.c, p.b);
         w.begin = p.part * part_units * kUnit;
         w.end = p.part == p.parts - 1 ? w.len : min(w.len, w.begin + part_units * kUnit);
