@@ -4,8 +4,8 @@
 //   top_p and min_p let it be;  W = sum of the kept w;  the token is the first whose sum of w with those before it exceeds u W.
 //
 // Nothing is sorted.  The order is cut into bins 1/32 of a unit of x / T wide (a function of x that never falls as x grows, whatever it is rounded to), and a bin's weight and number of tokens say which bin a
-// border lies in: one kernel makes the bins of slices of a row, a second joins them, and takes from the row the tokens of the few bins that matter.  Inside a bin a place is found by further
-// cuts, of the 64-bit number (x, index) that the order goes by.
+// border lies in: one kernel makes the bins of slices of a row, a second joins them and takes from the row the tokens of the few bins that matter, a third finds the places inside these
+// bins by further cuts, of the 64-bit number (x, index) that the order goes by.
 //
 // Weights are fixed-point numbers, 2^43 for the largest: their sums do not depend on the order of the additions, which LDS atomics leave open.
 #include "rowwise.h"
@@ -32,11 +32,10 @@ struct Slice {
 
 struct Weight {
     double top, step;         // largest logit, log2 e / T
-    // round(2^43 * 2^(-(top - x) step)); the Taylor series of 2^-f about f = 1/2 to degree 11 is off by 2^-46
+    // round(2^43 * 2^(-(top - x) step)).  The Taylor series of 2^-f about f = 1/2 to degree 11 is off by 2^-47 of it: the largest weight comes out as 2^43.
     __device__ __forceinline__ uint64_t operator()(float x) const
     {
-        const double y = (top - (double)x) * step;
-        if (!(y < 45.0)) return 0;
+        const double y = fmin((top - (double)x) * step, 46.0);                  // 46 and more, and no number (of -infinity): 0
         const double n = floor(y), z = (0.5 - (y - n)) * 0.69314718055994530942;
         double p = 1.0 / 39916800;
         p = fma(p, z, 1.0 / 3628800);
@@ -50,14 +49,13 @@ struct Weight {
         p = fma(p, z, 0.5);
         p = fma(p, z, 1.0);
         p = fma(p, z, 1.0);
-        // times 2^(43 - n) / sqrt 2, and rounded to an integer in the low bits of a number from 2^52 on; the largest weight is 2^43 itself
-        if (y == 0.0) return (uint64_t)kOne;
+        // times 2^(43 - n) / sqrt 2, and rounded to an integer in the low bits of a number from 2^52 on
         const double scale = __longlong_as_double((long long)(1023 + 43 - (int)n) << 52) * 0.70710678118654752440;
         return (uint64_t)__double_as_longlong(fma(p, scale, 4503599627370496.0)) & 0xFFFFFFFFFFFFFull;
     }
 };
 
-// bin number of a logit, counted from the row's own zero upwards
+// bin number of a logit, counted from the row's own zero upwards; NaN and -infinity are in the lowest
 __device__ __forceinline__ float bin_of(float x, float per_unit)
 {
     return floorf(fminf(fmaxf(x * per_unit, -0x1p30f), 0x1p30f));
@@ -71,6 +69,7 @@ __device__ __forceinline__ float bins_per_unit(float T) { return fminf(32.0f / T
 
 __device__ __forceinline__ float temperature_of(const SampleArgs &a, int64_t n) { return a.temperature ? a.temperature[n] : 1.0f; }
 __device__ __forceinline__ bool is_greedy(float T) { return !(T > 0.0f); }
+__device__ __forceinline__ double share_of(float u) { return u > 0.0f ? (double)fminf(u, 0x1.fffffep-1f) : 0.0; }
 
 // A logit as the order sees it: NaN as -infinity, -0 as 0; where the largest is +infinity, 0 for it and -infinity for everything else.
 __device__ __forceinline__ float seen(float x, bool infinite)
@@ -103,20 +102,35 @@ __device__ __forceinline__ void larger(float &x, int &at, float y, int where)
     if (y > x || (y == x && where < at)) x = y, at = where;
 }
 
-// ws of a row: slices, then their bins' weights, then their bins' numbers of tokens
-__host__ __device__ __forceinline__ size_t row_bytes(int slices) { return (size_t)slices * (sizeof(Slice) + kBins * 12); }
-struct RowSpace {
-    uint64_t *sums;
-    uint32_t *counts;
-    Slice *slices;
+// What the second kernel says of a row: its bins joined, which of them hold a border, and their tokens.
+struct RowBins {
+    double ends[kBins];        // weight of the row's tokens up to and with each bin
+    uint32_t count_ends[kBins];
+    uint32_t keys[kList], index[kList];
+    uint32_t listed;           // tokens in the list; more than kList: some were left out
+    int by_k, by_p, by_m;
+    int k0, p0, p1, m0, m1, u0, u1;       // first and last bin in which the border can lie
 };
-__device__ __forceinline__ RowSpace row_space(char *ws, int64_t row, int slices)
-{
-    char *const p = ws + row * row_bytes(slices);
-    return RowSpace{reinterpret_cast<uint64_t *>(p), reinterpret_cast<uint32_t *>(p + (size_t)slices * kBins * 8), reinterpret_cast<Slice *>(p + (size_t)slices * kBins * 12)};
-}
 
-template <bool F32> __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs a, char *ws, int slices, int slice_len)
+// ws: what is said of each row, then of each row its slices, their bins' weights and numbers of tokens
+struct Space {
+    RowBins *rows;
+    uint64_t *sums;            // [N][slices][kBins]
+    uint32_t *counts;
+    Slice *slices;             // [N][slices]
+};
+Space space_of(void *ws, int64_t N, int slices)
+{
+    Space s;
+    s.rows = static_cast<RowBins *>(ws);
+    s.sums = reinterpret_cast<uint64_t *>(s.rows + N);
+    s.counts = reinterpret_cast<uint32_t *>(s.sums + N * slices * kBins);
+    s.slices = reinterpret_cast<Slice *>(s.counts + N * slices * kBins);
+    return s;
+}
+size_t space_bytes(int64_t N, int slices) { return (size_t)N * (sizeof(RowBins) + (size_t)slices * (kBins * 12 + sizeof(Slice))); }
+
+template <bool F32> __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs a, Space ws, int slices, int slice_len)
 {
     __shared__ uint64_t sums[kBins];
     __shared__ uint32_t counts[kBins];
@@ -124,7 +138,6 @@ template <bool F32> __global__ __launch_bounds__(kThreads) void sample_bins_kern
     __shared__ int where[kWaves];
     const int64_t row = blockIdx.x / slices;
     const int slice = blockIdx.x % slices, begin = slice * slice_len, end = min((int)a.V, begin + slice_len);
-    const RowSpace out = row_space(ws, row, slices);
     float top = -INFINITY;
     int at = 0x7FFFFFFF;
     for (int i = begin + 8 * threadIdx.x; i < end; i += 8 * kThreads) {
@@ -141,7 +154,10 @@ template <bool F32> __global__ __launch_bounds__(kThreads) void sample_bins_kern
     __syncthreads();
     top = tops[0], at = where[0];
     for (int w = 1; w < kWaves; ++w) larger(top, at, tops[w], where[w]);
-    if (threadIdx.x == 0) out.slices[slice] = Slice{top, at};
+    if (threadIdx.x == 0) {
+        ws.slices[blockIdx.x] = Slice{top, at};
+        if (slice == 0) ws.rows[row].listed = 0;
+    }
     const float T = temperature_of(a, row);
     if (is_greedy(T) || top == -INFINITY) return;
     const bool infinite = top == INFINITY, count = a.top_k != nullptr;
@@ -151,19 +167,27 @@ template <bool F32> __global__ __launch_bounds__(kThreads) void sample_bins_kern
     for (int i = begin + 8 * threadIdx.x; i < end; i += 8 * kThreads) {
         float v[8];
         logits8<F32>(a, row, i, end, v);
+        if (infinite) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = seen(v[j], true);
+        }
+        uint64_t w[8];
+        int b[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float x = seen(v[j], infinite);
-            if (x == -INFINITY) continue;
-            const int b = bin_below(anchor, x, per_unit);
-            if (b >= kBins - 1) continue;
-            atomicAdd(reinterpret_cast<unsigned long long *>(&sums[b]), (unsigned long long)weight(x));
-            if (count) atomicAdd(&counts[b], 1u);
+            w[j] = weight(v[j]);
+            b[j] = bin_below(anchor, v[j], per_unit);
         }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (b[j] < kBins - 1) {
+                atomicAdd(reinterpret_cast<unsigned long long *>(&sums[b[j]]), (unsigned long long)w[j]);
+                if (count) atomicAdd(&counts[b[j]], 1u);
+            }
     }
     __syncthreads();
-    out.sums[slice * kBins + threadIdx.x] = sums[threadIdx.x];
-    if (count) out.counts[slice * kBins + threadIdx.x] = counts[threadIdx.x];
+    ws.sums[(int64_t)blockIdx.x * kBins + threadIdx.x] = sums[threadIdx.x];
+    if (count) ws.counts[(int64_t)blockIdx.x * kBins + threadIdx.x] = counts[threadIdx.x];
 }
 
 // (weight, number of tokens) up to and with each thread's; all threads of the workgroup call it
@@ -195,20 +219,50 @@ struct Row {
 };
 
 struct Shared {
-    double ends[kBins];        // weight of the row's tokens up to and with each bin
+    double ends[kBins];        // of RowBins
     uint32_t count_ends[kBins];
+    uint32_t keys[kList], index[kList];
     uint64_t sums[kCuts];
     uint32_t counts[kCuts];
-    uint32_t keys[kList], index[kList];
     double lw[kWaves];
     uint32_t lc[kWaves];
     uint64_t low, high;
     uint64_t few[kFew], few_weight[kFew];
     double found[2];
-    int bins[8];
+    int cut, bin;
     uint32_t n;
     int token;
 };
+
+// The row's largest logit, its temperature and what follows from them; false: the token is `token`, without a draw.
+__device__ __forceinline__ bool row_of(const SampleArgs &a, const Space &ws, int64_t row, int slices, Row &r, float (&tops)[kMaxSlices], int64_t &token)
+{
+    float top = -INFINITY;
+    int at = 0x7FFFFFFF;
+    Slice s[kMaxSlices];
+#pragma unroll
+    for (int i = 0; i < kMaxSlices; ++i) s[i] = i < slices ? ws.slices[row * slices + i] : Slice{-INFINITY, 0x7FFFFFFF};
+    const float T = temperature_of(a, row);
+#pragma unroll
+    for (int i = 0; i < kMaxSlices; ++i) {
+        larger(top, at, s[i].top, s[i].index);
+        tops[i] = s[i].top;
+    }
+    token = top == -INFINITY ? -1 : at;
+    if (top == -INFINITY || is_greedy(T)) return false;
+    r.infinite = top == INFINITY;
+    if (r.infinite) {
+        top = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kMaxSlices; ++i) tops[i] = tops[i] == INFINITY ? 0.0f : -INFINITY;
+    }
+    r.weight = Weight{(double)top, 1.44269504088896340736 / (double)T};
+    r.per_unit = bins_per_unit(T);
+    r.anchor = bin_of(top, r.per_unit);
+    r.row = row;
+    r.listed = -1;
+    return true;
+}
 
 // ascending with the order: larger logits have smaller numbers
 __device__ __forceinline__ uint32_t key_of(float x)
@@ -268,7 +322,7 @@ template <bool F32, bool RANK> __device__ void locate(const SampleArgs &a, const
     for (;;) {
         s.sums[threadIdx.x] = 0;
         s.counts[threadIdx.x] = 0;
-        if (threadIdx.x == 0) s.bins[7] = -1;
+        if (threadIdx.x == 0) s.cut = -1;
         __syncthreads();
         each<F32>(a, r, s, bin, [&](uint64_t k, float x) {
             const uint64_t c = (k - low) >> shift;
@@ -286,10 +340,10 @@ template <bool F32, bool RANK> __device__ void locate(const SampleArgs &a, const
         c += rank;
         // the cut in which the sum passes the target; the last one that weighs anything where none does
         const bool passes = RANK ? (double)c > target : w > target, passed = RANK ? (double)(c - here) > target : w - own > target;
-        if (here && passes && !passed) atomicMax(&s.bins[7], kCuts + (kCuts - (int)threadIdx.x));
-        else if (RANK ? here > 0 : own > 0.0) atomicMax(&s.bins[7], (int)threadIdx.x);
+        if (here && passes && !passed) atomicMax(&s.cut, kCuts + (kCuts - (int)threadIdx.x));
+        else if (RANK ? here > 0 : own > 0.0) atomicMax(&s.cut, (int)threadIdx.x);
         __syncthreads();
-        const int cut = s.bins[7] >= kCuts ? 2 * kCuts - s.bins[7] : s.bins[7];
+        const int cut = s.cut >= kCuts ? 2 * kCuts - s.cut : s.cut;
         if ((int)threadIdx.x == cut) s.found[0] = w - own, s.n = c - here;
         __syncthreads();
         before = s.found[0];
@@ -328,76 +382,73 @@ template <bool F32, bool RANK> __device__ void locate(const SampleArgs &a, const
     __syncthreads();
 }
 
-template <bool F32> __global__ __launch_bounds__(kThreads) void sample_choose_kernel(SampleArgs a, char *ws, int slices)
+// Joins the bins of a row's slices, says which of them hold the borders, and lists the slice's tokens in them.
+template <bool F32> __global__ __launch_bounds__(kThreads) void sample_list_kernel(SampleArgs a, Space ws, int slices, int slice_len)
 {
-    __shared__ Shared s;
-    const int64_t row = blockIdx.x;
-    const int t = threadIdx.x;
-    const RowSpace in = row_space(ws, row, slices);
-    float top = -INFINITY;
-    int at = 0x7FFFFFFF;
-    for (int i = 0; i < slices; ++i) larger(top, at, in.slices[i].top, in.slices[i].index);
-    const float T = temperature_of(a, row);
-    if (top == -INFINITY || is_greedy(T)) {
-        if (t == 0) a.tokens[row] = top == -INFINITY ? -1 : at;
-        return;
-    }
+    __shared__ double ends[kBins];
+    __shared__ uint32_t count_ends[kBins];
+    __shared__ uint32_t keys[kList], index[kList];
+    __shared__ double lw[kWaves], factors[kMaxSlices];
+    __shared__ uint32_t lc[kWaves], n, base;
+    __shared__ int bins[8];
+    const int64_t row = blockIdx.x / slices;
+    const int slice = blockIdx.x % slices, t = threadIdx.x;
     Row r;
-    r.infinite = top == INFINITY;
-    if (r.infinite) top = 0.0f;
-    r.weight = Weight{(double)top, 1.44269504088896340736 / (double)T};
-    r.per_unit = bins_per_unit(T);
-    r.anchor = bin_of(top, r.per_unit);
-    r.row = row;
-    r.listed = 0;
-    // The slices' bins, moved to where they lie below the row's largest and scaled by their own.
+    float tops[kMaxSlices];
+    int64_t token;
+    if (!row_of(a, ws, row, slices, r, tops, token)) return;
+    const int k = a.top_k ? a.top_k[row] : 0;
+    float p = a.top_p ? a.top_p[row] : 1.0f, m = a.min_p ? a.min_p[row] : 0.0f;
+    const double u = share_of(a.u[row]);
+    if (t < kMaxSlices) {
+        float top = tops[0];
+#pragma unroll
+        for (int i = 1; i < kMaxSlices; ++i) top = t == i ? tops[i] : top;
+        factors[t] = exp2(-(r.weight.top - (double)top) * r.weight.step);
+    }
+    if (t < 8) bins[t] = -1;
+    if (t == 0) n = 0;
+    // The slices' bins, moved to where they lie below the row's largest logit and scaled by their own.
+    uint64_t sums[kMaxSlices];
+    uint32_t counts[kMaxSlices];
+#pragma unroll
+    for (int i = 0; i < kMaxSlices; ++i) {
+        const float off = tops[i] == -INFINITY ? (float)kBins : r.anchor - bin_of(tops[i], r.per_unit);
+        const int b = t - (int)fminf(off, (float)kBins);
+        const bool some = b >= 0 && t < kBins - 1;
+        const int64_t at = (row * slices + i) * kBins + b;
+        sums[i] = some ? ws.sums[at] : 0;
+        counts[i] = some && a.top_k ? ws.counts[at] : 0;
+    }
+    __syncthreads();
     double w = 0.0;
     uint32_t c = 0;
-    for (int i = 0; i < slices; ++i) {
-        float st = in.slices[i].top;
-        if (st == -INFINITY || (r.infinite && st != INFINITY)) continue;
-        if (r.infinite) st = 0.0f;
-        const float off = r.anchor - bin_of(st, r.per_unit);
-        if (!(off < (float)(kBins - 1))) continue;
-        const int b = t - (int)off;
-        if (b < 0 || t >= kBins - 1) continue;
-        w += (double)in.sums[i * kBins + b] * exp2(-(r.weight.top - (double)st) * r.weight.step);
-        if (a.top_k) c += in.counts[i * kBins + b];
+#pragma unroll
+    for (int i = 0; i < kMaxSlices; ++i) {
+        if (sums[i]) w += (double)sums[i] * factors[i];
+        c += counts[i];
     }
     const double own = w;
     const uint32_t own_count = c;
-    scan(w, c, s.lw, s.lc);
-    s.ends[t] = w;
-    s.count_ends[t] = c;
-    if (t < 8) s.bins[t] = -1;
-    if (t == 0) s.n = 0;
+    scan(w, c, lw, lc);
+    ends[t] = w;
+    count_ends[t] = c;
     __syncthreads();
-    const double total = s.ends[kBins - 1];
-    const uint32_t tokens = s.count_ends[kBins - 1];
-    const double begin = t ? s.ends[t - 1] : 0.0;
+    const double total = ends[kBins - 1], begin = t ? ends[t - 1] : 0.0;
+    const uint32_t tokens = count_ends[kBins - 1];
     // bins[i]: the bin that a sum falls in, the last one with weight where it is beyond all
     const auto bin_at = [&](int i, double sum) {
-        if (own > 0.0 && begin <= sum && (sum < w || w >= total)) atomicMax(&s.bins[i], t);
+        if (own > 0.0 && begin <= sum && (sum < w || w >= total)) bins[i] = t;
     };
-    const int k = a.top_k ? a.top_k[row] : 0;
-    const bool by_k = k >= 1 && (uint32_t)k < tokens;
-    float p = a.top_p ? a.top_p[row] : 1.0f;
-    const bool by_p = p < 1.0f;
-    if (by_p && !(p > 0.0f)) p = 0.0f;
-    float m = a.min_p ? a.min_p[row] : 0.0f;
-    const bool by_m = m > 0.0f;
-    if (m > 1.0f) m = 1.0f;
-    float uf = a.u[row];
-    uf = uf > 0.0f ? fminf(uf, 0x1.fffffep-1f) : 0.0f;
-    const double u = (double)uf;
-    // 0: the bin of the k-th token
-    if (by_k && own_count && c - own_count < (uint32_t)k && (uint32_t)k <= c) s.bins[0] = t;
+    const bool by_k = k >= 1 && (uint32_t)k < tokens, by_p = p < 1.0f, by_m = m > 0.0f;
+    p = p > 0.0f ? p : 0.0f;
+    m = fminf(m, 1.0f);
+    if (by_k && own_count && c - own_count < (uint32_t)k && (uint32_t)k <= c) bins[0] = t;
     __syncthreads();
-    const int kbin = s.bins[0];
-    const double least_k = by_k ? (kbin ? s.ends[kbin - 1] : 0.0) : total, most_k = by_k ? s.ends[kbin] : total;
-    // 1, 2: the first and the last bin in which the border of top_p can lie
+    const int k0 = bins[0];
+    const double least_k = by_k ? (k0 ? ends[k0 - 1] : 0.0) : total, most_k = by_k ? ends[k0] : total;
     if (by_p) bin_at(1, (double)p * least_k), bin_at(2, (double)p * most_k);
-    // 3, 4: of min_p, whose border is at log2(1 / m) / step below the largest; one bin more on either side, for the roundings
+    // the border of min_p is at log2(1 / m) / step below the largest logit; one bin more on either side, for the roundings
     int m0 = kBins - 2, m1 = kBins - 2;
     if (by_m) {
         const float edge = (float)(r.weight.top + log2((double)m) / r.weight.step);
@@ -405,71 +456,129 @@ template <bool F32> __global__ __launch_bounds__(kThreads) void sample_choose_ke
         m0 = max(0, min(e - 1, kBins - 2)), m1 = max(0, min(e + 1, kBins - 2));
     }
     __syncthreads();
-    const int p0 = s.bins[1], p1 = s.bins[2];
+    const int p0 = bins[1], p1 = bins[2];
     double least = least_k, most = most_k;
-    if (by_p) least = fmin(least, p0 ? s.ends[p0 - 1] : 0.0), most = fmin(most, s.ends[p1]);
-    if (by_m) least = fmin(least, m0 ? s.ends[m0 - 1] : 0.0), most = fmin(most, s.ends[m1]);
+    if (by_p) least = fmin(least, p0 ? ends[p0 - 1] : 0.0), most = fmin(most, ends[p1]);
+    if (by_m) least = fmin(least, m0 ? ends[m0 - 1] : 0.0), most = fmin(most, ends[m1]);
     least = fmax(least, kOne), most = fmax(most, kOne);
-    bin_at(5, u * least * (1.0 - 0x1p-40));
-    bin_at(6, u * most * (1.0 + 0x1p-40));
+    bin_at(3, u * least * (1.0 - 0x1p-40));
+    bin_at(4, u * most * (1.0 + 0x1p-40));
     __syncthreads();
-    const int u0 = s.bins[5], u1 = s.bins[6];
-    const auto wanted = [&](int b) {
-        return (b >= u0 && b <= u1) || (by_k && b == kbin) || (by_p && b >= p0 && b <= p1) || (by_m && b >= m0 && b <= m1);
-    };
-    // those bins' tokens, out of the row; as many as there are where they fit
-    for (int i = 8 * t; i < (int)a.V; i += 8 * kThreads) {
-        float v[8];
-        logits8<F32>(a, row, i, (int)a.V, v);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float x = seen(v[j], r.infinite);
-            if (x == -INFINITY || !wanted(bin_below(r.anchor, x, r.per_unit))) continue;
-            const uint32_t to = atomicAdd(&s.n, 1u);
-            if (to < kList) s.keys[to] = key_of(x), s.index[to] = (uint32_t)(i + j);
+    const int u0 = bins[3], u1 = bins[4];
+    RowBins &out = ws.rows[row];
+    if (slice == 0) {
+        out.ends[t] = w;
+        out.count_ends[t] = c;
+        if (t == 0) {
+            out.by_k = by_k, out.by_p = by_p, out.by_m = by_m;
+            out.k0 = k0, out.p0 = p0, out.p1 = p1, out.m0 = m0, out.m1 = m1, out.u0 = u0, out.u1 = u1;
         }
     }
+    // lengths of the runs of bins, less one; without a border a run that no bin is in
+    const uint32_t uk = u1 - u0, pk = p1 - p0, mk = m1 - m0;
+    const int ks = by_k ? k0 : kBins, ps = by_p ? p0 : kBins, ms = by_m ? m0 : kBins;
+    const int begin_at = slice * slice_len, end = min((int)a.V, begin_at + slice_len);
+    for (int i0 = begin_at; i0 < end; i0 += 8 * kThreads) {
+        const int i = i0 + 8 * t;
+        float v[8];
+        uint32_t mine = 0;
+        if (i < end) {
+            logits8<F32>(a, row, i, end, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                v[j] = seen(v[j], r.infinite);
+                const int b = bin_below(r.anchor, v[j], r.per_unit);
+                const bool wanted = (uint32_t)(b - u0) <= uk || b == ks || (uint32_t)(b - ps) <= pk || (uint32_t)(b - ms) <= mk;
+                mine |= (uint32_t)(wanted && v[j] != -INFINITY) << j;
+            }
+        }
+        if (!__any(mine)) continue;
+        // places in the list: the lanes' numbers of tokens summed over the wave, one addition for all
+        uint32_t at = __popc(mine);
+        for (int o = 1; o < 64; o <<= 1) {
+            const uint32_t x = __shfl_up(at, o, 64);
+            if ((t & 63) >= o) at += x;
+        }
+        uint32_t from = 0;
+        if ((t & 63) == 63) from = atomicAdd(&n, at);
+        at += __shfl(from, 63, 64) - __popc(mine);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (mine >> j & 1) {
+                if (at < kList) keys[at] = key_of(v[j]), index[at] = (uint32_t)(i + j);
+                ++at;
+            }
+    }
     __syncthreads();
-    r.listed = s.n <= kList ? (int)s.n : -1;
+    const uint32_t many = n;
+    if (many == 0) return;
+    if (t == 0) base = atomicAdd(&out.listed, many);
     __syncthreads();
+    const uint32_t to = base;
+    for (uint32_t i = t; i < min(many, (uint32_t)kList); i += kThreads)
+        if (to + i < kList) out.keys[to + i] = keys[i], out.index[to + i] = index[i];
+}
+
+// The draw, from the joined bins and the listed tokens.
+template <bool F32> __global__ __launch_bounds__(kThreads) void sample_choose_kernel(SampleArgs a, Space ws, int slices)
+{
+    __shared__ Shared s;
+    const int64_t row = blockIdx.x;
+    const int t = threadIdx.x;
+    Row r;
+    float tops[kMaxSlices];
+    int64_t token;
+    if (!row_of(a, ws, row, slices, r, tops, token)) {
+        if (t == 0) a.tokens[row] = token;
+        return;
+    }
+    const RowBins &in = ws.rows[row];
+    const int k = a.top_k ? a.top_k[row] : 0;
+    const float p = a.top_p ? fmaxf(a.top_p[row], 0.0f) : 1.0f, m = a.min_p ? fminf(a.min_p[row], 1.0f) : 0.0f;
+    const double u = share_of(a.u[row]);
+    const uint32_t listed = in.listed;
+    s.ends[t] = in.ends[t];
+    s.count_ends[t] = in.count_ends[t];
+    for (uint32_t i = t; i < min(listed, (uint32_t)kList); i += kThreads) s.keys[i] = in.keys[i], s.index[i] = in.index[i];
+    if (listed <= kList) r.listed = (int)listed;
+    __syncthreads();
+    const double total = s.ends[kBins - 1];
+    // the bin in which a sum falls, from `first` to `last`
+    const auto bin_of_sum = [&](double sum, int first, int last) {
+        if (t == 0) s.bin = last;
+        __syncthreads();
+        if (t >= first && t < last && sum < s.ends[t]) atomicMin(&s.bin, t);
+        __syncthreads();
+        return s.bin;
+    };
     // what the filters leave, as a sum of weights
     double kept = total;
-    if (by_k) {
-        locate<F32, true>(a, r, s, kbin, (double)(k - 1));
+    if (in.by_k) {
+        locate<F32, true>(a, r, s, in.k0, (double)(k - 1));
         kept = s.found[1];
     }
-    if (by_p) {
+    if (in.by_p) {
         const double target = (double)p * kept;
-        __syncthreads();
-        if (t == 0) s.bins[1] = -1;
-        __syncthreads();
-        bin_at(1, target);
-        __syncthreads();
-        locate<F32, false>(a, r, s, min(max(s.bins[1], p0), p1), target);
+        locate<F32, false>(a, r, s, bin_of_sum(target, in.p0, in.p1), target);
         kept = fmin(kept, s.found[0] == target ? s.found[0] : s.found[1]);
     }
-    if (by_m) {
+    if (in.by_m) {
         // the tokens of the bins around the border that are heavy enough, after all those in front of them
         uint64_t sum = 0;
-        for (int b = m0; b <= m1; ++b)
+        for (int b = in.m0; b <= in.m1; ++b)
             each<F32>(a, r, s, b, [&](uint64_t, float x) {
                 if (exp2(-(r.weight.top - (double)x) * r.weight.step) >= (double)m) sum += r.weight(x);
             });
         double all = (double)sum;
         uint32_t none = 0;
         scan(all, none, s.lw, s.lc);
-        if (t == kThreads - 1) s.found[0] = all + (m0 ? s.ends[m0 - 1] : 0.0);
+        if (t == kThreads - 1) s.found[0] = all + (in.m0 ? s.ends[in.m0 - 1] : 0.0);
         __syncthreads();
         kept = fmin(kept, s.found[0]);
     }
     kept = fmax(kept, kOne);                                 // the first token stays
     const double target = u * kept;
-    __syncthreads();
-    if (t == 0) s.bins[5] = -1;
-    __syncthreads();
-    bin_at(5, target);
-    __syncthreads();
-    locate<F32, false>(a, r, s, min(max(s.bins[5], u0), u1), target);
+    locate<F32, false>(a, r, s, bin_of_sum(target, in.u0, in.u1), target);
     if (t == 0) a.tokens[row] = s.token;
 }
 
@@ -482,22 +591,24 @@ int slices_of(int64_t N, int64_t V)
     return (int)(s < 1 ? 1 : s > kMaxSlices ? kMaxSlices : s);
 }
 
-template <bool F32> hipError_t run(const SampleArgs &a, char *ws, hipStream_t st)
+template <bool F32> hipError_t run(const SampleArgs &a, void *ws, hipStream_t st)
 {
     const int slices = slices_of(a.N, a.V);
     const int len = (int)(((a.V + slices - 1) / slices + 7) / 8 * 8);
-    sample_bins_kernel<F32><<<(unsigned)(a.N * slices), kThreads, 0, st>>>(a, ws, slices, len);
-    sample_choose_kernel<F32><<<(unsigned)a.N, kThreads, 0, st>>>(a, ws, slices);
+    const Space space = space_of(ws, a.N, slices);
+    sample_bins_kernel<F32><<<(unsigned)(a.N * slices), kThreads, 0, st>>>(a, space, slices, len);
+    sample_list_kernel<F32><<<(unsigned)(a.N * slices), kThreads, 0, st>>>(a, space, slices, len);
+    sample_choose_kernel<F32><<<(unsigned)a.N, kThreads, 0, st>>>(a, space, slices);
     return hipGetLastError();
 }
 
 }  // namespace
 
-size_t sample_workspace_bytes(int64_t N, int64_t V) { return (size_t)N * row_bytes(slices_of(N, V)); }
+size_t sample_workspace_bytes(int64_t N, int64_t V) { return space_bytes(N, slices_of(N, V)); }
 
 hipError_t launch_sample(const SampleArgs &a, void *ws, hipStream_t st)
 {
-    return a.f32 ? run<true>(a, static_cast<char *>(ws), st) : run<false>(a, static_cast<char *>(ws), st);
+    return a.f32 ? run<true>(a, ws, st) : run<false>(a, ws, st);
 }
 
 }  // namespace tj
