@@ -22,6 +22,7 @@ constexpr int kCuts = 1024;                   // cuts of a bin
 constexpr int kFew = 64;                      // tokens among which a wave finds the place
 constexpr int kList = 4096;                   // tokens that are taken out of a row; where there are more, they stay in it
 constexpr int kMaxSlices = 8;
+constexpr int kKept = 2;                      // runs of eight logits that a thread keeps between its two walks over them
 constexpr double kOne = 8796093022208.0;      // 2^43
 
 // what a slice leaves
@@ -140,7 +141,19 @@ template <bool F32> __global__ __launch_bounds__(kThreads) void sample_bins_kern
     const int slice = blockIdx.x % slices, begin = slice * slice_len, end = min((int)a.V, begin + slice_len);
     float top = -INFINITY;
     int at = 0x7FFFFFFF;
-    for (int i = begin + 8 * threadIdx.x; i < end; i += 8 * kThreads) {
+    float kept[kKept][8];                         // a thread's first logits, for the second walk
+#pragma unroll
+    for (int c = 0; c < kKept; ++c) {
+        const int i = begin + 8 * (threadIdx.x + c * kThreads);
+        if (i < end) logits8<F32>(a, row, i, end, kept[c]);
+        else
+#pragma unroll
+            for (int j = 0; j < 8; ++j) kept[c][j] = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (kept[c][j] > top) top = kept[c][j], at = i + j;
+    }
+    for (int i = begin + 8 * (threadIdx.x + kKept * kThreads); i < end; i += 8 * kThreads) {
         float v[8];
         logits8<F32>(a, row, i, end, v);
 #pragma unroll
@@ -164,9 +177,7 @@ template <bool F32> __global__ __launch_bounds__(kThreads) void sample_bins_kern
     if (infinite) top = 0.0f;
     const Weight weight{(double)top, 1.44269504088896340736 / (double)T};
     const float per_unit = bins_per_unit(T), anchor = bin_of(top, per_unit);
-    for (int i = begin + 8 * threadIdx.x; i < end; i += 8 * kThreads) {
-        float v[8];
-        logits8<F32>(a, row, i, end, v);
+    const auto add = [&](float (&v)[8]) {
         if (infinite) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = seen(v[j], true);
@@ -184,6 +195,14 @@ template <bool F32> __global__ __launch_bounds__(kThreads) void sample_bins_kern
                 atomicAdd(reinterpret_cast<unsigned long long *>(&sums[b[j]]), (unsigned long long)w[j]);
                 if (count) atomicAdd(&counts[b[j]], 1u);
             }
+    };
+#pragma unroll
+    for (int c = 0; c < kKept; ++c)
+        if (begin + 8 * c * kThreads < end) add(kept[c]);
+    for (int i = begin + 8 * (threadIdx.x + kKept * kThreads); i < end; i += 8 * kThreads) {
+        float v[8];
+        logits8<F32>(a, row, i, end, v);
+        add(v);
     }
     __syncthreads();
     ws.sums[(int64_t)blockIdx.x * kBins + threadIdx.x] = sums[threadIdx.x];
@@ -222,11 +241,11 @@ struct Shared {
     double ends[kBins];        // of RowBins
     uint32_t count_ends[kBins];
     uint32_t keys[kList], index[kList];
+    uint64_t weights[kList];
     uint64_t sums[kCuts];
     uint32_t counts[kCuts];
     double lw[kWaves];
     uint32_t lc[kWaves];
-    uint64_t low, high;
     uint64_t few[kFew], few_weight[kFew];
     double found[2];
     int cut, bin;
@@ -272,13 +291,13 @@ __device__ __forceinline__ uint32_t key_of(float x)
 }
 __device__ __forceinline__ float logit_of(uint32_t k) { return u2f(k & 0x80000000u ? k : ~k & 0x7FFFFFFFu); }
 
-// do(place in the order as a number, logit) for every token of bin `bin`
+// what(place in the order as a number, logit, weight) for every token of bin `bin`
 template <bool F32, typename Do> __device__ __forceinline__ void each(const SampleArgs &a, const Row &r, Shared &s, int bin, Do &&what)
 {
     if (r.listed >= 0) {
         for (int i = threadIdx.x; i < r.listed; i += kThreads) {
             const float x = logit_of(s.keys[i]);
-            if (bin_below(r.anchor, x, r.per_unit) == bin) what((uint64_t)s.keys[i] << 32 | s.index[i], x);
+            if (bin_below(r.anchor, x, r.per_unit) == bin) what((uint64_t)s.keys[i] << 32 | s.index[i], x, s.weights[i]);
         }
     } else {
         for (int i = 8 * threadIdx.x; i < (int)a.V; i += 8 * kThreads) {
@@ -286,7 +305,7 @@ template <bool F32, typename Do> __device__ __forceinline__ void each(const Samp
             logits8<F32>(a, r.row, i, (int)a.V, v);
             for (int j = 0; j < 8; ++j) {
                 const float x = seen(v[j], r.infinite);
-                if (x != -INFINITY && bin_below(r.anchor, x, r.per_unit) == bin) what((uint64_t)key_of(x) << 32 | (uint32_t)(i + j), x);
+                if (x != -INFINITY && bin_below(r.anchor, x, r.per_unit) == bin) what((uint64_t)key_of(x) << 32 | (uint32_t)(i + j), x, r.weight(x));
             }
         }
     }
@@ -298,36 +317,27 @@ template <bool F32, bool RANK> __device__ void locate(const SampleArgs &a, const
 {
     double before = bin ? s.ends[bin - 1] : 0.0;
     uint32_t rank = bin ? s.count_ends[bin - 1] : 0;
-    __syncthreads();
-    if (threadIdx.x == 0) s.low = ~0ull, s.high = 0;
-    __syncthreads();
-    unsigned long long least = ~0ull, most = 0;
-    each<F32>(a, r, s, bin, [&](uint64_t k, float) {
-        least = k < least ? k : least;
-        most = k > most ? k : most;
-    });
-    for (int o = 1; o < 64; o <<= 1) {
-        const unsigned long long x = __shfl_xor(least, o, 64), y = __shfl_xor(most, o, 64);
-        least = x < least ? x : least;
-        most = y > most ? y : most;
+    // The numbers that the bin's tokens can have, from its edges (a little wider, for the product's rounding); everything where the bin's number was limited, or has no edges.
+    uint64_t low = 0, high = ~0ull;
+    {
+        const double f = (double)r.anchor - bin, per = (double)r.per_unit, up = (f + 1.0) / per, down = f / per;
+        if (fabs(f) < 0x1p29 && fabs(up) < 0x1p126 && fabs(down) < 0x1p126) {
+            low = (uint64_t)key_of((float)(up + fabs(up) * 0x1p-20 + 0x1p-126)) << 32;
+            high = (uint64_t)key_of((float)(down - fabs(down) * 0x1p-20 - 0x1p-126)) << 32 | 0xFFFFFFFFu;
+        }
     }
-    if ((threadIdx.x & 63) == 0 && least <= most) {
-        atomicMin(reinterpret_cast<unsigned long long *>(&s.low), least);
-        atomicMax(reinterpret_cast<unsigned long long *>(&s.high), most);
-    }
-    __syncthreads();
-    uint64_t low = s.low;
-    const uint64_t span = s.high - low;
+    const uint64_t span = high - low;
     int shift = span >> 10 ? 54 - __clzll((long long)span) : 0;           // span >> shift < 1024
+    __syncthreads();
     for (;;) {
         s.sums[threadIdx.x] = 0;
         s.counts[threadIdx.x] = 0;
         if (threadIdx.x == 0) s.cut = -1;
         __syncthreads();
-        each<F32>(a, r, s, bin, [&](uint64_t k, float x) {
+        each<F32>(a, r, s, bin, [&](uint64_t k, float, uint64_t weight) {
             const uint64_t c = (k - low) >> shift;
             if (k < low || c >= kCuts) return;
-            atomicAdd(reinterpret_cast<unsigned long long *>(&s.sums[c]), (unsigned long long)r.weight(x));
+            atomicAdd(reinterpret_cast<unsigned long long *>(&s.sums[c]), (unsigned long long)weight);
             atomicAdd(&s.counts[c], 1u);
         });
         __syncthreads();
@@ -356,11 +366,11 @@ template <bool F32, bool RANK> __device__ void locate(const SampleArgs &a, const
     }
     if (threadIdx.x == 0) s.n = 0;
     __syncthreads();
-    each<F32>(a, r, s, bin, [&](uint64_t k, float x) {
+    each<F32>(a, r, s, bin, [&](uint64_t k, float, uint64_t weight) {
         if (k < low || (k - low) >> shift) return;
         const uint32_t i = atomicAdd(&s.n, 1u);
         s.few[i] = k;
-        s.few_weight[i] = r.weight(x);
+        s.few_weight[i] = weight;
     });
     __syncthreads();
     if (threadIdx.x < 64) {
@@ -393,6 +403,9 @@ template <bool F32> __global__ __launch_bounds__(kThreads) void sample_list_kern
     __shared__ int bins[8];
     const int64_t row = blockIdx.x / slices;
     const int slice = blockIdx.x % slices, t = threadIdx.x;
+    const int begin_at = slice * slice_len, end = min((int)a.V, begin_at + slice_len);
+    float ahead[8];                               // the thread's first logits, on their way while the bins are joined
+    if (begin_at + 8 * t < end) logits8<F32>(a, row, begin_at + 8 * t, end, ahead);
     Row r;
     float tops[kMaxSlices];
     int64_t token;
@@ -477,13 +490,17 @@ template <bool F32> __global__ __launch_bounds__(kThreads) void sample_list_kern
     // lengths of the runs of bins, less one; without a border a run that no bin is in
     const uint32_t uk = u1 - u0, pk = p1 - p0, mk = m1 - m0;
     const int ks = by_k ? k0 : kBins, ps = by_p ? p0 : kBins, ms = by_m ? m0 : kBins;
-    const int begin_at = slice * slice_len, end = min((int)a.V, begin_at + slice_len);
     for (int i0 = begin_at; i0 < end; i0 += 8 * kThreads) {
         const int i = i0 + 8 * t;
         float v[8];
         uint32_t mine = 0;
         if (i < end) {
-            logits8<F32>(a, row, i, end, v);
+            if (i0 == begin_at) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = ahead[j];
+            } else {
+                logits8<F32>(a, row, i, end, v);
+            }
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 v[j] = seen(v[j], r.infinite);
@@ -539,7 +556,10 @@ template <bool F32> __global__ __launch_bounds__(kThreads) void sample_choose_ke
     const uint32_t listed = in.listed;
     s.ends[t] = in.ends[t];
     s.count_ends[t] = in.count_ends[t];
-    for (uint32_t i = t; i < min(listed, (uint32_t)kList); i += kThreads) s.keys[i] = in.keys[i], s.index[i] = in.index[i];
+    for (uint32_t i = t; i < min(listed, (uint32_t)kList); i += kThreads) {
+        const uint32_t key = in.keys[i];
+        s.keys[i] = key, s.index[i] = in.index[i], s.weights[i] = r.weight(logit_of(key));
+    }
     if (listed <= kList) r.listed = (int)listed;
     __syncthreads();
     const double total = s.ends[kBins - 1];
@@ -566,8 +586,8 @@ template <bool F32> __global__ __launch_bounds__(kThreads) void sample_choose_ke
         // the tokens of the bins around the border that are heavy enough, after all those in front of them
         uint64_t sum = 0;
         for (int b = in.m0; b <= in.m1; ++b)
-            each<F32>(a, r, s, b, [&](uint64_t, float x) {
-                if (exp2(-(r.weight.top - (double)x) * r.weight.step) >= (double)m) sum += r.weight(x);
+            each<F32>(a, r, s, b, [&](uint64_t, float x, uint64_t weight) {
+                if (exp2(-(r.weight.top - (double)x) * r.weight.step) >= (double)m) sum += weight;
             });
         double all = (double)sum;
         uint32_t none = 0;
