@@ -31,22 +31,23 @@ __device__ __forceinline__ float2_t cos_sin(int pos, float freq)
     return float2_t{q == 1 || q == 2 ? -a : a, q >= 2 ? -b : b};
 }
 
-// up to eight consecutive elements; those from n on are zeros
-template <typename T> __device__ __forceinline__ void get8(const T *p, int n, float (&v)[8])
+// Up to eight consecutive elements as they lie in memory; those from n on are zeros.
+template <typename T> using RawOf = Raw<sizeof(T) == 2 ? kBf16 : kF32>;
+template <typename T> __device__ __forceinline__ RawOf<T> raw8(const T *p, int n)
 {
+    RawOf<T> r = zero8<sizeof(T) == 2 ? kBf16 : kF32>();
     if (n >= 8) {
-        if constexpr (sizeof(T) == 2) widen(Raw<kBf16>{*reinterpret_cast<const bf16x8_at2 *>(p)}, v);
-        else widen(Raw<kF32>{*reinterpret_cast<const f32x4_at4 *>(p), *reinterpret_cast<const f32x4_at4 *>(p + 4)}, v);
-        return;
+        if constexpr (sizeof(T) == 2) r.q = *reinterpret_cast<const bf16x8_at2 *>(p);
+        else r.lo = *reinterpret_cast<const f32x4_at4 *>(p), r.hi = *reinterpret_cast<const f32x4_at4 *>(p + 4);
+        return r;
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        v[i] = 0.0f;
+    for (int i = 0; i < 7; ++i)
         if (i < n) {
-            if constexpr (sizeof(T) == 2) v[i] = u2f((uint32_t)p[i] << 16);
-            else v[i] = p[i];
+            if constexpr (sizeof(T) == 2) r.q[i / 2] |= (uint32_t)p[i] << (16 * (i & 1));
+            else (i < 4 ? r.lo : r.hi)[i & 3] = p[i];
         }
-    }
+    return r;
 }
 template <typename T> __device__ __forceinline__ void put8(T *p, int n, const float (&v)[8])
 {
@@ -74,47 +75,58 @@ template <typename T> __device__ __forceinline__ void put8(T *p, int n, const fl
 // units of a head: runs of eight pairs, then runs of eight elements that are not turned
 __host__ __device__ __forceinline__ int units_of(int D, int half) { return (half + 7) / 8 + (D - 2 * half + 7) / 8; }
 
-// Unit u of a head.  cs: the token's cosines and sines.  All of a unit is read before any of it is written: src may be dst.
-template <typename S, typename T>
-__device__ __forceinline__ void turn_unit(const S *src, T *dst, int D, int half, int pairs, int u, const float2_t *cs)
+// Unit u of a head: two runs of up to eight elements, the second one of turned units alone.
+template <typename S> struct Unit { RawOf<S> x, y; };
+template <typename S> __device__ __forceinline__ Unit<S> read_unit(const S *src, int D, int half, int pairs, int u)
 {
-    const int turned = (half + 7) >> 3;
-    if (u >= turned) {
-        const int at = 2 * half + 8 * (u - turned);
-        float v[8];
-        get8(src + at, D - at, v);
-        put8(dst + at, D - at, v);
+    const int runs = (half + 7) >> 3, j = 8 * u, n = half - j;
+    Unit<S> r;
+    r.y = zero8<sizeof(S) == 2 ? kBf16 : kF32>();
+    if (u >= runs) {
+        const int at = 2 * half + 8 * (u - runs);
+        r.x = raw8(src + at, D - at);
+    } else if (pairs) {
+        r.x = raw8(src + 2 * j, 2 * n);
+        r.y = raw8(src + 2 * j + 8, 2 * n - 8);
+    } else {
+        r.x = raw8(src + j, n);
+        r.y = raw8(src + half + j, n);
+    }
+    return r;
+}
+// The unit turned, in its place.  cs: the token's cosines and sines.  All of a unit has been read before any of it is written: src may be dst.
+template <typename S, typename T>
+__device__ __forceinline__ void write_unit(const Unit<S> &r, T *dst, int D, int half, int pairs, int u, const float2_t *cs)
+{
+    const int runs = (half + 7) >> 3, j = 8 * u, n = half - j;
+    float x[8], y[8];
+    widen(r.x, x);
+    if (u >= runs) {
+        const int at = 2 * half + 8 * (u - runs);
+        put8(dst + at, D - at, x);
         return;
     }
-    const int j = 8 * u, n = min(8, half - j);
-    float a[8], b[8];
+    widen(r.y, y);
     if (pairs) {
-        float x[8], y[8];
-        get8(src + 2 * j, 2 * n, x);
-        get8(src + 2 * j + 8, 2 * n - 8, y);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            a[i] = x[2 * i], b[i] = x[2 * i + 1];
-            a[4 + i] = y[2 * i], b[4 + i] = y[2 * i + 1];
+            const float2_t s = cs[min(j + i, half - 1)], t = cs[min(j + 4 + i, half - 1)];
+            const float a = x[2 * i], b = x[2 * i + 1], c = y[2 * i], d = y[2 * i + 1];
+            x[2 * i] = fmaf(a, s.x, -(b * s.y)), x[2 * i + 1] = fmaf(b, s.x, a * s.y);
+            y[2 * i] = fmaf(c, t.x, -(d * t.y)), y[2 * i + 1] = fmaf(d, t.x, c * t.y);
         }
-    } else {
-        get8(src + j, n, a);
-        get8(src + half + j, n, b);
-    }
-    float c[8], d[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float2_t t = cs[i < n ? j + i : 0];
-        c[i] = fmaf(a[i], t.x, -(b[i] * t.y));
-        d[i] = fmaf(b[i], t.x, a[i] * t.y);
-    }
-    if (pairs) {
-        const float x[8] = {c[0], d[0], c[1], d[1], c[2], d[2], c[3], d[3]}, y[8] = {c[4], d[4], c[5], d[5], c[6], d[6], c[7], d[7]};
         put8(dst + 2 * j, 2 * n, x);
         put8(dst + 2 * j + 8, 2 * n - 8, y);
     } else {
-        put8(dst + j, n, c);
-        put8(dst + half + j, n, d);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float2_t t = cs[min(j + i, half - 1)];
+            const float a = x[i], b = y[i];
+            x[i] = fmaf(a, t.x, -(b * t.y));
+            y[i] = fmaf(b, t.x, a * t.y);
+        }
+        put8(dst + j, n, x);
+        put8(dst + half + j, n, y);
     }
 }
 
@@ -142,7 +154,8 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(const S *x, int64_t ldx,
     for (int i = threadIdx.x; i < count * row_units; i += kThreads) {
         const int t = i / row_units, w = i - t * row_units, h = w / units;
         const int64_t n = n0 + t;
-        turn_unit(x + n * ldx + (int64_t)h * D, y + n * ldy + (int64_t)h * D, D, r.half, r.pairs, w - h * units, cs + t * r.half);
+        const int u = w - h * units;
+        write_unit(read_unit(x + n * ldx + (int64_t)h * D, D, r.half, r.pairs, u), y + n * ldy + (int64_t)h * D, D, r.half, r.pairs, u, cs + t * r.half);
     }
 }
 
@@ -166,6 +179,8 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(const S *q, int64_t
     __shared__ int seen[kMaxTokens];            // whether the row has a place in a sequence
     __shared__ int position[kMaxTokens];
     const int n0 = blockIdx.x * tokens, count = min(tokens, N - n0);
+    const int units = units_of(c.D, r.half), plain = c.D >> 3;
+    const int uq = Hq * units, uk = c.heads * units, row = uq + uk + c.heads * plain;
     if ((int)threadIdx.x < count) {
         int seq;
         const int place = place_of(b, c, n0 + threadIdx.x, N, seq);
@@ -182,8 +197,6 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(const S *q, int64_t
         }
         __syncthreads();
     }
-    const int units = units_of(c.D, r.half), plain = c.D >> 3;
-    const int uq = Hq * units, uk = c.heads * units, row = uq + uk + c.heads * plain;
     const int64_t head_stride = (int64_t)c.D << c.page_log2;
     uint16_t *const ck = static_cast<uint16_t *>(c.k), *const cv = static_cast<uint16_t *>(c.v);
     for (int i = threadIdx.x; i < count * row; i += kThreads) {
@@ -192,20 +205,20 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(const S *q, int64_t
         const int64_t n = n0 + t;
         if (!seen[t]) continue;
         if (w < uq) {
-            const int h = w / units;
-            turn_unit(q + n * ldq + (int64_t)h * c.D, qo + n * ldqo + (int64_t)h * c.D, c.D, r.half, r.pairs, w - h * units, cs + t * r.half);
+            const int h = w / units, u = w - h * units;
+            write_unit(read_unit(q + n * ldq + (int64_t)h * c.D, c.D, r.half, r.pairs, u), qo + n * ldqo + (int64_t)h * c.D, c.D, r.half, r.pairs, u, cs + t * r.half);
             continue;
         }
         if (base[t] < 0) continue;
         w -= uq;
         if (w < uk) {
-            const int h = w / units;
-            turn_unit(k + n * ldk + (int64_t)h * c.D, ck + base[t] + h * head_stride, c.D, r.half, r.pairs, w - h * units, cs + t * r.half);
+            const int h = w / units, u = w - h * units;
+            write_unit(read_unit(k + n * ldk + (int64_t)h * c.D, c.D, r.half, r.pairs, u), ck + base[t] + h * head_stride, c.D, r.half, r.pairs, u, cs + t * r.half);
         } else {
             w -= uk;
             const int h = w / plain, at = 8 * (w - h * plain);
             float e[8];
-            get8(v + n * ldv + (int64_t)h * c.D + at, 8, e);
+            widen(raw8(v + n * ldv + (int64_t)h * c.D + at, 8), e);
             put8(cv + base[t] + h * head_stride + at, 8, e);
         }
     }
@@ -220,39 +233,57 @@ __global__ __launch_bounds__(kThreads) void kv_append8_kernel(const S *q, int64_
     __shared__ float2_t cs[kMaxHeadDim / 2];
     __shared__ __align__(16) float turned[kSliceElems];
     const int n = blockIdx.x;
-    int seq;
-    const int place = place_of(b, c, n, N, seq);
-    if (place < 0) return;
-    const int page = page_of(b, c, seq, place);
-    for (int j = threadIdx.x; j < r.half; j += kThreads) cs[j] = turn_of(r, place + b.prefix, j, 0);
-    __syncthreads();
     const int units = units_of(c.D, r.half);
     const int h0 = blockIdx.y * slice, heads = min(slice, c.heads - h0);
     // the query heads in as many parts as there are slices of key heads
     const int q0 = (int)((int64_t)Hq * blockIdx.y / gridDim.y), q1 = (int)((int64_t)Hq * (blockIdx.y + 1) / gridDim.y);
-    for (int i = threadIdx.x; i < (q1 - q0) * units; i += kThreads) {
-        const int h = q0 + i / units;
-        turn_unit(q + n * ldq + (int64_t)h * c.D, qo + n * ldqo + (int64_t)h * c.D, c.D, r.half, r.pairs, i - (h - q0) * units, cs);
+    const int uq = (q1 - q0) * units, uk = heads * units, group_lanes = c.groups * kGroupLanes;
+    const S *const qn = q + n * ldq + (int64_t)q0 * c.D, *const kn = k + n * ldk + (int64_t)h0 * c.D, *const vn = v + n * ldv + (int64_t)h0 * c.D;
+    const auto read = [&](const S *row, int i) {
+        const int h = i / units;
+        return read_unit(row + (int64_t)h * c.D, c.D, r.half, r.pairs, i - h * units);
+    };
+    const auto read_value = [&](int i) {
+        const int h = i / group_lanes, at = 8 * (i - h * group_lanes);
+        return raw8(vn + (int64_t)h * c.D + at, c.D - at);
+    };
+    // the thread's first unit of each is on its way while the place is looked up
+    const int t = threadIdx.x;
+    Unit<S> qu, ku;
+    RawOf<S> vu;
+    if (t < uk) ku = read(kn, t);
+    if (t < heads * group_lanes) vu = read_value(t);
+    if (t < uq) qu = read(qn, t);
+    int seq;
+    const int place = place_of(b, c, n, N, seq);
+    if (place < 0) return;
+    const int page = page_of(b, c, seq, place);
+    for (int j = t; j < r.half; j += kThreads) cs[j] = turn_of(r, place + b.prefix, j, 0);
+    __syncthreads();
+    if (page >= 0)
+        for (int i = t; i < uk; i += kThreads) {
+            const int h = i / units;
+            if (i >= kThreads) ku = read(kn, i);
+            write_unit(ku, turned + h * c.D, c.D, r.half, r.pairs, i - h * units, cs);
+        }
+    for (int i = t; i < uq; i += kThreads) {
+        const int h = i / units;
+        if (i >= kThreads) qu = read(qn, i);
+        write_unit(qu, qo + n * ldqo + (int64_t)(q0 + h) * c.D, c.D, r.half, r.pairs, i - h * units, cs);
     }
     if (page < 0) return;
-    for (int i = threadIdx.x; i < heads * units; i += kThreads) {
-        const int h = i / units;
-        turn_unit(k + n * ldk + (int64_t)(h0 + h) * c.D, turned + h * c.D, c.D, r.half, r.pairs, i - h * units, cs);
-    }
     __syncthreads();
-    const int group_lanes = c.groups * kGroupLanes;                     // of a head
     const int slot = place & ((1 << c.page_log2) - 1);
-    // Every lane of 16 that share a group comes by together: the count is a multiple of 16.
-    for (int i = threadIdx.x; i < 2 * heads * group_lanes; i += kThreads) {
-        const int value = i >= heads * group_lanes;
-        const int w = i - value * heads * group_lanes, h = w / group_lanes, at = 8 * (w - h * group_lanes);
+    // Every lane of 16 that share a group come by together: the count is a multiple of 16.
+    for (int i = t; i < heads * group_lanes; i += kThreads) {
+        const int h = i / group_lanes, at = 8 * (i - h * group_lanes);
+        const int64_t row = (((int64_t)page * c.heads + h0 + h) << c.page_log2) + slot;
         float e[8] = {};
-        if (at < c.D) {
-            if (value) get8(v + n * ldv + (int64_t)(h0 + h) * c.D + at, 8, e);
-            else get8(turned + h * c.D + at, 8, e);
-        }
-        const CkptOut o{static_cast<uint8_t *>(value ? c.v : c.k), value ? c.v_exps : c.k_exps, c.groups};
-        ckpt_store8<false>(o, (((int64_t)page * c.heads + h0 + h) << c.page_log2) + slot, at, c.D, e);
+        if (at < c.D) widen(raw8(turned + h * c.D + at, 8), e);
+        ckpt_store8<false>(CkptOut{static_cast<uint8_t *>(c.k), c.k_exps, c.groups}, row, at, c.D, e);
+        if (i >= kThreads) vu = read_value(i);
+        widen(vu, e);
+        ckpt_store8<false>(CkptOut{static_cast<uint8_t *>(c.v), c.v_exps, c.groups}, row, at, c.D, e);
     }
 }
 
