@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass
 from typing import Optional
 
@@ -57,18 +58,8 @@ class CCkpt8(C.Structure):
     _fields_ = [("codes", C.c_void_p), ("exps", C.c_void_p), ("rows", C.c_int64), ("K", C.c_int64)]
 
 
-class CRotation(C.Structure):
-    _fields_ = [("freqs", C.c_void_p), ("R", C.c_int64), ("form", C.c_int32), ("scale", C.c_float)]
-
-
-class CKvCache(C.Structure):
-    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_exps", C.c_void_p), ("v_exps", C.c_void_p), ("pages", C.c_int64), ("H", C.c_int64), ("page", C.c_int64),
-                ("D", C.c_int64), ("kind", C.c_int32), ("reserved", C.c_int32)]
-
-
-class CKvBatch(C.Structure):
-    _fields_ = [("table", C.c_void_p), ("lens", C.c_void_p), ("starts", C.c_void_p), ("prefix_table", C.c_void_p), ("B", C.c_int64), ("width", C.c_int64),
-                ("prefix", C.c_int64)]
+# nvfp4_rotation, nvfp4_kvcache and nvfp4_kvbatch as bytes: 0.3 us of the host each, where a ctypes structure takes 1.0 to make.
+_ROTATION, _KVCACHE, _KVBATCH = struct.Struct("Pqif"), struct.Struct("PPPPqqqqii"), struct.Struct("PPPPqqq")
 
 
 class CProductPlan(C.Structure):
@@ -152,17 +143,17 @@ def lib():
         L.nvfp4_ckpt8_load.argtypes = [vp, vp, i32, i64, vp]
         L.nvfp4_gemv.restype = i32
         L.nvfp4_gemv.argtypes = [vp, i64, i64, vp, vp, i32, i64, vp]
-        dbl, rot, kvc, kvb = C.c_double, C.POINTER(CRotation), C.POINTER(CKvCache), C.POINTER(CKvBatch)
+        dbl = C.c_double
         L.nvfp4_rope_frequencies.restype = i32
         L.nvfp4_rope_frequencies.argtypes = [i64, dbl, i32, dbl, dbl, dbl, dbl, vp]
         L.nvfp4_rope.restype = i32
-        L.nvfp4_rope.argtypes = [vp, i32, i64, vp, i64, i64, i64, rot, i32, vp, i32, i64, vp]
+        L.nvfp4_rope.argtypes = [vp, i32, i64, vp, i64, i64, i64, vp, i32, vp, i32, i64, vp]
         L.nvfp4_kv_append.restype = i32
-        L.nvfp4_kv_append.argtypes = [vp, i64, i64, vp, i64, vp, i64, i32, i64, kvc, kvb, rot, vp, i32, i64, vp]
+        L.nvfp4_kv_append.argtypes = [vp, i64, i64, vp, i64, vp, i64, i32, i64, vp, vp, vp, vp, i32, i64, vp]
         L.nvfp4_kv_load.restype = i32
-        L.nvfp4_kv_load.argtypes = [kvc, kvb, i64, vp, i64, vp, i64, i32, vp]
+        L.nvfp4_kv_load.argtypes = [vp, vp, i64, vp, i64, vp, i64, i32, vp]
         L.nvfp4_attn.restype = i32
-        L.nvfp4_attn.argtypes = [vp, i64, i64, i64, kvc, kvb, C.c_float, vp, i64, vp, sz, vp]
+        L.nvfp4_attn.argtypes = [vp, i64, i64, i64, vp, vp, C.c_float, vp, i64, vp, sz, vp]
         L.nvfp4_attn_workspace_bytes.restype = sz
         L.nvfp4_attn_workspace_bytes.argtypes = [i64] * 8
         L.nvfp4_sample.restype = i32
@@ -618,6 +609,7 @@ def alloc_stats(N: int, device="cuda") -> torch.Tensor:
     return torch.empty((N, 2), dtype=torch.float32, device=device)
 
 
+_BF16, _F32, _U8, _I32 = torch.bfloat16, torch.float32, torch.uint8, torch.int32
 _KINDS = {torch.bfloat16: SRC_BF16, torch.float32: SRC_F32}
 
 
@@ -793,10 +785,10 @@ class Rope:
     form: int = ROPE_HALF
     scale: float = 1.0       # of cosine and sine
 
-    def c_struct(self, dev: int) -> CRotation:
+    def packed(self, dev: int) -> bytes:
         f = self.freqs
-        assert f.dtype == torch.float32 and f.dim() == 1 and f.is_contiguous() and f.get_device() == dev, "freqs: float32 [R / 2], on the current device"
-        return CRotation(_ptr(f), 2 * f.numel(), self.form, self.scale)
+        assert f.dtype == _F32 and f.dim() == 1 and f.is_contiguous() and f.get_device() == dev, "freqs: float32 [R / 2], on the current device"
+        return _ROTATION.pack(f.data_ptr() or _ptr(f) or 0, 2 * f.numel(), self.form, self.scale)
 
 
 @dataclass
@@ -807,18 +799,18 @@ class KVCache:
     k_exps: Optional[torch.Tensor] = None
     v_exps: Optional[torch.Tensor] = None
 
-    def c_struct(self, dev: int) -> CKvCache:
+    def packed(self, dev: int) -> bytes:
         k, v, ke, ve = self.k, self.v, self.k_exps, self.v_exps
-        kind = KV_BF16 if k.dtype == torch.bfloat16 else KV_8
-        assert k.dim() == 4 and k.dtype in (torch.bfloat16, torch.uint8) and k.shape == v.shape and k.dtype == v.dtype, "cache: bf16 or uint8 [pages, heads, page, D], keys and values alike"
-        assert k.is_contiguous() and v.is_contiguous() and k.get_device() == v.get_device() == dev, "cache: contiguous, on the current device"
-        pages, heads, page, D = k.shape
-        if kind == KV_8:
-            for e in (ke, ve):
-                assert e is not None and e.dtype == torch.uint8 and tuple(e.shape) == (pages, heads, page, -(-D // CKPT_GROUP)) and e.is_contiguous() and e.get_device() == dev, "exponents of an 8-bit cache, on the current device"
-        else:
+        shape, dtype = k.shape, k.dtype
+        assert len(shape) == 4 and v.shape == shape and v.dtype == dtype and (dtype == _BF16 or dtype == _U8), "cache: bf16 or uint8 [pages, heads, page, D], keys and values alike"
+        assert k.is_contiguous() and v.is_contiguous() and k.get_device() == dev == v.get_device(), "cache: contiguous, on the current device"
+        pages, heads, page, D = shape
+        if dtype == _BF16:
             assert ke is None and ve is None, "exponents: of an 8-bit cache alone"
-        return CKvCache(_ptr(k), _ptr(v), _ptr(ke), _ptr(ve), pages, heads, page, D, kind, 0)
+            return _KVCACHE.pack(k.data_ptr() or _ptr(k) or 0, v.data_ptr() or _ptr(v) or 0, 0, 0, pages, heads, page, D, KV_BF16, 0)
+        for e in (ke, ve):
+            assert e is not None and e.dtype == _U8 and e.shape == (pages, heads, page, -(-D // CKPT_GROUP)) and e.is_contiguous() and e.get_device() == dev, "exponents of an 8-bit cache, on the current device"
+        return _KVCACHE.pack(*(t.data_ptr() or _ptr(t) or 0 for t in (k, v, ke, ve)), pages, heads, page, D, KV_8, 0)
 
 
 def alloc_kv_cache(pages: int, heads: int, page: int, D: int, kind: int = KV_BF16, device="cuda") -> KVCache:
@@ -837,14 +829,32 @@ class KVBatch:
     prefix_table: Optional[torch.Tensor] = None   # pages of the tokens that all sequences share
     prefix: int = 0                               # how many those are
 
-    def c_struct(self, dev: int, page: int) -> CKvBatch:
-        ok = lambda t, *shape: t.dtype == torch.int32 and tuple(t.shape) == shape and t.is_contiguous() and t.get_device() == dev
-        table, lens, starts, prefix = self.table, self.lens, self.starts, self.prefix_table
-        B, width = table.shape
-        assert ok(table, B, width) and ok(lens, B), "table [B, width] and lens [B]: int32, contiguous, on the current device"
-        assert starts is None or ok(starts, B + 1), "starts: int32 [B + 1], on the current device"
-        assert self.prefix <= 0 or (prefix is not None and ok(prefix, prefix.numel()) and prefix.numel() * page >= self.prefix), "prefix_table: int32, pages of the whole prefix, on the current device"
-        return CKvBatch(_ptr(table), _ptr(lens), _ptr(starts), _ptr(prefix), B, width, self.prefix)
+    def packed(self, dev: int, page: int) -> bytes:
+        table, lens, starts, prefix_table, prefix = self.table, self.lens, self.starts, self.prefix_table, self.prefix
+        shape = table.shape
+        assert len(shape) == 2 and table.dtype == _I32 and table.is_contiguous() and table.get_device() == dev, "table: int32 [B, width], contiguous, on the current device"
+        B, width = shape
+        _check_ints(lens, B, "lens", dev)
+        if starts is not None:
+            _check_ints(starts, B + 1, "starts", dev)
+            starts = starts.data_ptr()
+        if prefix > 0:
+            assert prefix_table is not None, "prefix_table: pages of the whole prefix"
+            _check_ints(prefix_table, prefix_table.numel(), "prefix_table", dev)
+            assert prefix_table.numel() * page >= prefix, "prefix_table: pages of the whole prefix"
+            prefix_table = prefix_table.data_ptr()
+        else:
+            prefix_table = 0
+        return _KVBATCH.pack(table.data_ptr() or _ptr(table) or 0, lens.data_ptr() or _ptr(lens) or 0, starts or 0, prefix_table, B, width, prefix)
+
+
+def _check_ints(t: torch.Tensor, n: int, what: str, dev: int):
+    assert t.dtype == _I32 and t.shape == (n,) and t.is_contiguous() and t.get_device() == dev, what + ": int32 [%d], on the current device" % n
+
+
+def _scratch(nbytes: int, like: torch.Tensor) -> Optional[torch.Tensor]:
+    """A workspace in elements of another tensor's type, 1 us of the host's less than one of bytes."""
+    return like.new_empty(-(-nbytes // like.element_size())) if nbytes else None
 
 
 def rope(X: torch.Tensor, pos: torch.Tensor, rotation: Rope, heads: int, out_dtype: int = OUT_BF16, *, inverse: bool = False,
@@ -853,9 +863,9 @@ def rope(X: torch.Tensor, pos: torch.Tensor, rotation: Rope, heads: int, out_dty
     dev = _current_device()
     kind, ldx, N, width = _rows(X, "X", dev)
     assert heads > 0 and width % heads == 0, "X: rows of whole heads"
-    assert pos.dtype == torch.int32 and tuple(pos.shape) == (N,) and pos.is_contiguous() and pos.get_device() == dev, "pos: int32 [N], on the current device"
+    _check_ints(pos, N, "pos", dev)
     Y, ldy = _out_rows(Y, N, width, out_dtype, X, "Y", dev)
-    _check(lib().nvfp4_rope(_ptr(X), kind, ldx, _ptr(pos), N, heads, width // heads, C.byref(rotation.c_struct(dev)), int(inverse), _ptr(Y), out_dtype, ldy,
+    _check(lib().nvfp4_rope(_ptr(X), kind, ldx, _ptr(pos), N, heads, width // heads, rotation.packed(dev), int(inverse), _ptr(Y), out_dtype, ldy,
                             _raw_stream(dev)), "nvfp4_rope")
     return Y
 
@@ -864,32 +874,32 @@ def kv_append(K: torch.Tensor, V: torch.Tensor, cache: KVCache, batch: KVBatch, 
               out_dtype: int = OUT_BF16, Qo: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
     """nvfp4_kv_append: keys (turned at their positions) and values [N, heads * D] of the batch's rows into the cache; Q [N, any heads * D] turned in the same way is returned."""
     dev = _current_device()
-    cc = cache.c_struct(dev)
-    cb = batch.c_struct(dev, cc.page)
+    cc = cache.packed(dev)
+    _, heads, page, D = cache.k.shape
     kind, ldk, N, width = _rows(K, "K", dev)
     vkind, ldv, *shape = _rows(V, "V", dev)
-    assert width == cc.H * cc.D and shape == [N, width] and vkind == kind, "K, V: one type, [N, heads * D] of the cache"
+    assert width == heads * D and shape == [N, width] and vkind == kind, "K, V: one type, [N, heads * D] of the cache"
     ldq = Hq = ldo = 0
     if Q is not None:
         qkind, ldq, rows, qwidth = _rows(Q, "Q", dev)
-        assert rows == N and qwidth % cc.D == 0 and qkind == kind, "Q: the type and rows of K, whole heads"
-        Hq = qwidth // cc.D
+        assert rows == N and qwidth % D == 0 and qkind == kind, "Q: the type and rows of K, whole heads"
+        Hq = qwidth // D
         Qo, ldo = _out_rows(Qo, N, qwidth, out_dtype, Q, "Qo", dev)
     else:
         assert Qo is None, "Qo: the output of Q"
-    _check(lib().nvfp4_kv_append(_ptr(Q), ldq, Hq, _ptr(K), ldk, _ptr(V), ldv, kind, N, C.byref(cc), C.byref(cb),
-                                 C.byref(rotation.c_struct(dev)) if rotation is not None else None, _ptr(Qo), out_dtype, ldo, _raw_stream(dev)), "nvfp4_kv_append")
+    _check(lib().nvfp4_kv_append(_ptr(Q), ldq, Hq, _ptr(K), ldk, _ptr(V), ldv, kind, N, cc, batch.packed(dev, page),
+                                 None if rotation is None else rotation.packed(dev), _ptr(Qo), out_dtype, ldo, _raw_stream(dev)), "nvfp4_kv_append")
     return Qo
 
 
 def kv_load(cache: KVCache, batch: KVBatch, N: int, out_dtype: int = OUT_BF16, *, K: Optional[torch.Tensor] = None, V: Optional[torch.Tensor] = None):
     """nvfp4_kv_load: (K, V) [N, heads * D] of the batch's N rows as the cache holds them."""
     dev = _current_device()
-    cc = cache.c_struct(dev)
-    cb = batch.c_struct(dev, cc.page)
-    K, ldk = _out_rows(K, N, cc.H * cc.D, out_dtype, cache.k, "K", dev)
-    V, ldv = _out_rows(V, N, cc.H * cc.D, out_dtype, cache.k, "V", dev)
-    _check(lib().nvfp4_kv_load(C.byref(cc), C.byref(cb), N, _ptr(K), ldk, _ptr(V), ldv, out_dtype, _raw_stream(dev)), "nvfp4_kv_load")
+    cc = cache.packed(dev)
+    _, heads, page, D = cache.k.shape
+    K, ldk = _out_rows(K, N, heads * D, out_dtype, cache.k, "K", dev)
+    V, ldv = _out_rows(V, N, heads * D, out_dtype, cache.k, "V", dev)
+    _check(lib().nvfp4_kv_load(cc, batch.packed(dev, page), N, _ptr(K), ldk, _ptr(V), ldv, out_dtype, _raw_stream(dev)), "nvfp4_kv_load")
     return K, V
 
 
@@ -902,17 +912,20 @@ def attn(Q: torch.Tensor, cache: KVCache, batch: KVBatch, heads: int, *, scale: 
          ws: Optional[torch.Tensor] = None) -> torch.Tensor:
     """nvfp4_attn: the batch's rows Q [N, heads * D] (bf16) over the cache; scale: 1 / sqrt(D) unless given.  Rows that belong to no sequence are not written."""
     dev = _current_device()
-    cc = cache.c_struct(dev)
-    cb = batch.c_struct(dev, cc.page)
+    cc = cache.packed(dev)
+    _, kv_heads, page, D = cache.k.shape
     kind, ldq, N, width = _rows(Q, "Q", dev)
-    assert kind == SRC_BF16 and width == heads * cc.D, "Q: bf16 [N, heads * D]"
+    assert kind == SRC_BF16 and width == heads * D, "Q: bf16 [N, heads * D]"
+    cb = batch.packed(dev, page)
     Out, ldo = _out_rows(Out, N, width, OUT_BF16, Q, "Out", dev)
+    L = lib()
     if ws is None:
-        ws = alloc_workspace(lib().nvfp4_attn_workspace_bytes(N, heads, cc.H, cc.D, cc.page, cb.B, cb.width, cb.prefix), Q.device)
+        B, table_width = batch.table.shape
+        ws = _scratch(L.nvfp4_attn_workspace_bytes(N, heads, kv_heads, D, page, B, table_width, batch.prefix), Q)
     else:
         assert ws.get_device() == dev, "ws: on the current device"
-    _check(lib().nvfp4_attn(_ptr(Q), ldq, N, heads, C.byref(cc), C.byref(cb), cc.D ** -0.5 if scale is None else scale, _ptr(Out), ldo, _ptr(ws), ws.numel() * ws.element_size(),
-                            _raw_stream(dev)), "nvfp4_attn")
+    _check(L.nvfp4_attn(_ptr(Q), ldq, N, heads, cc, cb, D ** -0.5 if scale is None else scale, _ptr(Out), ldo, _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(),
+                        _raw_stream(dev)), "nvfp4_attn")
     return Out
 
 
@@ -922,15 +935,14 @@ def sample(logits: torch.Tensor, u: torch.Tensor, *, temperature: Optional[torch
     """nvfp4_sample: a token (int64 [N]) per row of logits [N, V] from u (float32 [N], 0 <= u < 1); the other parameters are [N], float32 (top_k: int32)."""
     dev = _current_device()
     kind, ld, N, V = _rows(logits, "logits", dev)
-    for t, what, dtype in ((u, "u", torch.float32), (temperature, "temperature", torch.float32), (top_k, "top_k", torch.int32), (top_p, "top_p", torch.float32),
-                           (min_p, "min_p", torch.float32), (tokens, "tokens", torch.int64)):
-        assert t is None or (t.dtype == dtype and tuple(t.shape) == (N,) and t.is_contiguous() and t.get_device() == dev), what + ": %s [N], on the current device" % dtype
+    for t, what, dtype in ((u, "u", _F32), (temperature, "temperature", _F32), (top_k, "top_k", _I32), (top_p, "top_p", _F32), (min_p, "min_p", _F32), (tokens, "tokens", torch.int64)):
+        assert t is None or (t.dtype == dtype and t.shape == (N,) and t.is_contiguous() and t.get_device() == dev), what + ": %s [N], on the current device" % dtype
     if tokens is None:
         tokens = torch.empty(N, dtype=torch.int64, device=logits.device)
     if ws is None:
-        ws = alloc_workspace(lib().nvfp4_sample_workspace_bytes(N, V), logits.device)
+        ws = _scratch(lib().nvfp4_sample_workspace_bytes(N, V), logits)
     else:
         assert ws.get_device() == dev, "ws: on the current device"
     _check(lib().nvfp4_sample(_ptr(logits), kind, ld, N, V, _ptr(u), _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(tokens), _ptr(ws),
-                              ws.numel() * ws.element_size(), _raw_stream(dev)), "nvfp4_sample")
+                              0 if ws is None else ws.numel() * ws.element_size(), _raw_stream(dev)), "nvfp4_sample")
     return tokens
