@@ -211,18 +211,27 @@ __global__ __launch_bounds__(kThreads, 2) void attn_wide_kernel(AttnArgs a)
         float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
         top = max32(top) * a.scale2;
         if (__any(top > m + kSlack)) {
-            const float to = fmaxf(m, top), by = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - to);
-            l *= by;
+            const float to = fmaxf(m, top), old = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - to);
+            l *= old;
 #pragma unroll
-            for (int d = 0; d < DT; ++d) o[d] *= by;
+            for (int d = 0; d < DT; ++d) o[d] *= old;
             m = to;
         }
-        const float mm = m == -INFINITY ? 0.0f : m;
+        // score * scale - maximum in one operation: the product is not rounded, and the largest one not taken from itself exactly.  Scores that the difference then matters for are
+        // scaled first.
+        float mm = m == -INFINITY ? 0.0f : m, by = a.scale2;
+        if (__any(fabsf(mm) > 0x1p20f)) {
+#pragma unroll
+            for (int t = 0; t < TT; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sc[t][i] = sc[t][i] * a.scale2 - mm;
+            mm = 0.0f, by = 1.0f;
+        }
         // weights of the lane's eight tokens of run g
         const auto weights = [&](int g) {
             float e[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(sc[g / 2][8 * (g & 1) + i], a.scale2, -mm));
+            for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(sc[g / 2][8 * (g & 1) + i], by, -mm));
             l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
             return u32x4{bf16_pair(e[0], e[1]), bf16_pair(e[2], e[3]), bf16_pair(e[4], e[5]), bf16_pair(e[6], e[7])};
         };
