@@ -404,13 +404,13 @@ struct Cut {
 constexpr int kGroups = 512, kManyGroups = 2048;
 constexpr int kManyTiles = 256;
 
-int rows_of_tile(int64_t rows, int D) { return rows < 64 || D > 128 ? kTile : kWideRows; }
+int rows_of_tile(int64_t rows) { return rows < 64 ? kTile : kWideRows; }
 
-Cut cut_of(int64_t N, int Hq, int heads, int D, int B, int64_t tokens, int64_t prefix)
+Cut cut_of(int64_t N, int Hq, int heads, int B, int64_t tokens, int64_t prefix)
 {
     Cut p;
     const int64_t G = Hq / heads;
-    p.own_rows = rows_of_tile((N + B - 1) / B * G, D);
+    p.own_rows = rows_of_tile((N + B - 1) / B * G);
     p.min_units = p.own_rows == kTile ? 2 : 4;
     const int64_t tiles = N * G / p.own_rows + B, units = (tokens + kUnit - 1) / kUnit;
     // Enough tiles of several rows: nothing is cut.  Else the own tokens are cut, also where there are many sequences: their lengths differ.
@@ -423,7 +423,7 @@ Cut cut_of(int64_t N, int Hq, int heads, int D, int B, int64_t tokens, int64_t p
     p.prefix_rows = p.prefix_units = p.prefix_parts = 0;
     p.prefix_items = 0;
     if (prefix > 0) {
-        p.prefix_rows = rows_of_tile(N * G, D);
+        p.prefix_rows = rows_of_tile(N * G);
         const int64_t tiles = (N * G + p.prefix_rows - 1) / p.prefix_rows;
         const int64_t units = (prefix + kUnit - 1) / kUnit, want = (kGroups + tiles * heads - 1) / (tiles * heads);
         int64_t part = (units + want - 1) / want;
@@ -463,14 +463,14 @@ template <int DP, bool BITS8> hipError_t run(const AttnArgs &a, const Cut &p, hi
 
 size_t attn_workspace_bytes(int64_t N, int Hq, int heads, int D, int B, int64_t tokens, int64_t prefix)
 {
-    const Cut p = cut_of(N, Hq, heads, D, B, tokens, prefix);
+    const Cut p = cut_of(N, Hq, heads, B, tokens, prefix);
     return (size_t)((own_parts(p, heads) + prefix_parts(p, heads)) * (D * 4 + 8) + (p.slots > 0 ? (int64_t)B * 16 : 0));
 }
 
 hipError_t launch_attn(const uint16_t *q, int64_t ldq, int64_t N, int Hq, const KvCache &c, const KvBatch &b, float scale, uint16_t *out, int64_t ldo, void *ws,
                        hipStream_t st)
 {
-    const Cut p = cut_of(N, Hq, c.heads, c.D, b.B, (int64_t)b.width << c.page_log2, b.prefix);
+    const Cut p = cut_of(N, Hq, c.heads, b.B, (int64_t)b.width << c.page_log2, b.prefix);
     const int64_t own = own_parts(p, c.heads), pre = prefix_parts(p, c.heads);
     float *const o = static_cast<float *>(ws);
     float2_t *const ml = reinterpret_cast<float2_t *>(o + (own + pre) * c.D);

@@ -57,7 +57,7 @@ template <int DP, bool BITS8> struct Moved {
 
 // EXACT: heads of DP elements, else of fewer
 template <int DP, bool EXACT, bool BITS8, bool PREFIX>
-__global__ __launch_bounds__(kThreads, 2) void attn_wide_kernel(AttnArgs a)
+__global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attn_wide_kernel(AttnArgs a)
 {
     using S = Shape<DP>;
     constexpr int ROWS = kWideRows, TT = S::TOK / 32, DT = DP / 32;
@@ -115,7 +115,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_wide_kernel(AttnArgs a)
         for (int i = 0; i < S::MOVES; ++i) {
             const int run = uniform((i * S::PER + mt) >> 4);
             const int page = __builtin_amdgcn_readlane(pages, S::GROUPS * held + run);
-            const int64_t token = (((int64_t)(page < 0 ? 0 : page) * a.c.heads + head) << a.c.page_log2) + ((t0 + 16 * run) & ((1 << a.c.page_log2) - 1));
+            const int64_t token = (((int64_t)(page < 0 ? 0 : page) * a.c.heads + head) << a.c.page_log2) + ((t0 + 16 * run) & ((1 << a.c.page_log2) - 1)) +
+                                  (i * S::PER & 15);
             if constexpr (BITS8) {
                 const u32x2 k = *reinterpret_cast<const u32x2 *>(shared_row(static_cast<const char *>(a.c.k) + token * a.c.D) + in_run);
                 const u32x2 v = *reinterpret_cast<const u32x2 *>(shared_row(static_cast<const char *>(a.c.v) + token * a.c.D) + in_run);
@@ -359,7 +360,8 @@ template <int DP> void run(const AttnArgs &a, bool prefix, int64_t items, hipStr
 hipError_t launch_attn_wide(const AttnArgs &a, bool prefix, int64_t items, hipStream_t st)
 {
     if (a.c.D <= 64) run<64>(a, prefix, items, st);
-    else run<128>(a, prefix, items, st);
+    else if (a.c.D <= 128) run<128>(a, prefix, items, st);
+    else run<256>(a, prefix, items, st);
     return hipGetLastError();
 }
 

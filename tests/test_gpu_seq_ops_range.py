@@ -23,7 +23,7 @@ def check_attn(bt, q, k, v, o, scale, Hq):
 
 # prompts and pieces of prompts on both kinds of tiles, whole and ragged heads, one answer, a prefix
 @pytest.mark.parametrize("case", [([0], [20], 2, 2, 64, 16, 0), ([5], [9], 8, 1, 128, 16, 0), ([40], [1], 4, 2, 96, 32, 0), ([0], [150], 1, 1, 64, 16, 0), ([70, 0], [90, 64], 2, 1, 128, 32, 0), ([3], [40], 4, 1, 256, 16, 0),
-                                  ([0, 3], [3, 2], 4, 2, 64, 16, 70), ([0], [70], 2, 1, 80, 16, 100)], ids=lambda c: "-".join(str(v) for v in (max(c[0]), max(c[1])) + c[2:]))
+                                  ([0, 3], [3, 2], 4, 2, 64, 16, 70), ([0], [70], 2, 1, 80, 16, 100), ([0, 20], [80, 70], 1, 1, 208, 16, 0)], ids=lambda c: "-".join(str(v) for v in (max(c[0]), max(c[1])) + c[2:]))
 @pytest.mark.parametrize("bits8", [False, True])
 def test_what_is_not_finite_stays_with_the_rows_that_see_it(tj, case, bits8):  # noqa: F811
     """NaN and infinities in keys and values of new tokens: the rows in front of them must not know.  An 8-bit cache holds NaN in their place."""
