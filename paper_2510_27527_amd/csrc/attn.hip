@@ -395,7 +395,7 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs a)
 // ---- how a call is cut -------------------------------------------------------------------------
 
 struct Cut {
-    int target, min_units, own_rows, prefix_rows, prefix_units, prefix_parts;
+    int target, min_units, own_rows, prefix_rows, through, prefix_units, prefix_parts;
     int64_t slots, items, prefix_items;        // of a key head
 };
 
@@ -419,6 +419,9 @@ Cut cut_of(int64_t N, int Hq, int heads, int B, int64_t tokens, int64_t prefix)
     p.target = cut ? (int)((groups + heads - 1) / heads) : 0;
     const int64_t most = cut ? (units + p.min_units - 1) / p.min_units : 1;                // parts of a tile
     p.items = tiles * most < tiles + p.target ? tiles * most : tiles + p.target;           // every tile at least once, and the cuts
+    // Sequences of whole tiles that nobody cuts take the prefix themselves: no partial results, no join.  (Four prompts of up to 1000 tokens after 1000 shared ones: 100 us, 242 with parts.)
+    p.through = prefix > 0 && !cut && N * G >= (int64_t)B * kWideRows;
+    if (p.through) prefix = 0;
     p.slots = cut || prefix ? p.items : 0;
     p.prefix_rows = p.prefix_units = p.prefix_parts = 0;
     p.prefix_items = 0;
@@ -474,7 +477,7 @@ hipError_t launch_attn(const uint16_t *q, int64_t ldq, int64_t N, int Hq, const 
     const int64_t own = own_parts(p, c.heads), pre = prefix_parts(p, c.heads);
     float *const o = static_cast<float *>(ws);
     float2_t *const ml = reinterpret_cast<float2_t *>(o + (own + pre) * c.D);
-    const AttnArgs a{q, ldq, out, ldo, (int)N, Hq, Hq / c.heads, c, b, scale * 1.44269504088896340736f, p.target, p.min_units, p.own_rows, p.prefix_rows, p.slots, p.prefix_units,
+    const AttnArgs a{q, ldq, out, ldo, (int)N, Hq, Hq / c.heads, c, b, scale * 1.44269504088896340736f, p.target, p.min_units, p.own_rows, p.prefix_rows, p.through, p.slots, p.prefix_units,
                      p.prefix_parts, o, o + own * c.D, ml, ml + own, reinterpret_cast<int64_t *>(ml + own + pre)};
     if (c.D <= 64) return c.bits8 ? run<64, true>(a, p, st) : run<64, false>(a, p, st);
     if (c.D <= 128) return c.bits8 ? run<128, true>(a, p, st) : run<128, false>(a, p, st);

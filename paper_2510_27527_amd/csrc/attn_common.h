@@ -34,6 +34,7 @@ struct AttnArgs {
     int target;                           // parts that a key head's own tokens are to be cut into; 0: none are cut
     int min_units;                        // of a part, at least
     int own_rows, prefix_rows;            // rows of a tile of the own tokens, and of the prefix
+    int through;                          // 1: a sequence's tiles take the prefix themselves, in front of their own tokens
     int64_t slots;                        // own parts of a key head, at most
     int prefix_units, prefix_parts;       // units of a part of the prefix, and how many there are
     float *own_o, *prefix_o;              // [slot][key head][rows of a tile][D]
@@ -169,7 +170,7 @@ template <bool PREFIX> __device__ __forceinline__ bool work_of(const AttnArgs &a
         // the tiles that see most come first
         w.tile = tiles_of(w.count, a.G, a.own_rows) - 1 - p.tile;
         w.slot = p.base + (int64_t)w.tile * p.parts + p.part;
-        w.parts = a.b.prefix ? 2 : p.parts;
+        w.parts = a.b.prefix && !a.through ? 2 : p.parts;
         if (a.slots > 0 && blockIdx.x % a.c.heads == 0 && p.tile == 0 && p.part == 0 && threadIdx.x == 0) a.lie[2 * p.b] = p.base, a.lie[2 * p.b + 1] = p.parts;
         w.len = tokens_of(a.b, a.c, p.b);
         w.begin = p.part * part_units * kUnit;

@@ -70,10 +70,8 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attn_wide_kernel(A
     Work w;
     if (!work_of<PREFIX>(a, item, w)) return;
     const int rows = w.count * a.G, r0 = w.tile * ROWS + wave * 32;
-    const int end = min(w.end, sees_of<PREFIX>(a, w, w.tile * ROWS + ROWS - 1));
     const int r = r0 + row;
     const bool valid = r < rows;
-    const int limit = min(sees_of<PREFIX>(a, w, r), end);
     u32x4 q[DP / 16];
     const uint16_t *const qp = a.q + (int64_t)(w.first + (valid ? r / a.G : 0)) * a.ldq + (int64_t)(head * a.G + (valid ? r % a.G : 0)) * a.c.D;
 #pragma unroll
@@ -82,9 +80,24 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attn_wide_kernel(A
         q[c] = u32x4{0, 0, 0, 0};
         if (valid && (EXACT || d < a.c.D)) q[c] = *reinterpret_cast<const bf16x8_at2 *>(qp + d);
     }
-    const int least = min(sees_of<PREFIX>(a, w, w.tile * ROWS), end);         // that a row of the workgroup sees
-    // the least and the most that a row of the wave sees
-    const int low = min(sees_of<PREFIX>(a, w, r0), end), high = min(sees_of<PREFIX>(a, w, r0 + 31), end);
+    // What is walked over: tokens begin .. end of a table; how many of them the lane's row sees, the least that a row of the workgroup sees, the least and the most of a row of the wave.
+    // THROUGH: first the prefix, which every row sees, then the sequence's own tokens.
+    const int *table = w.table;
+    int table_len = w.table_len, begin = w.begin, end, limit, least, low, high;
+    const auto own_tokens = [&]() {
+        end = min(w.end, sees_of<PREFIX>(a, w, w.tile * ROWS + ROWS - 1));
+        limit = min(sees_of<PREFIX>(a, w, r), end);
+        least = min(sees_of<PREFIX>(a, w, w.tile * ROWS), end);
+        low = min(sees_of<PREFIX>(a, w, r0), end), high = min(sees_of<PREFIX>(a, w, r0 + 31), end);
+    };
+    const bool through = !PREFIX && a.through;
+    if (through) {
+        table = a.b.prefix_table;
+        table_len = (a.b.prefix + (1 << a.c.page_log2) - 1) >> a.c.page_log2;
+        begin = 0, end = limit = least = low = high = a.b.prefix;
+    } else {
+        own_tokens();
+    }
 
     float m = -INFINITY, l = 0.0f;
     float16_t o[DT];
@@ -104,7 +117,7 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attn_wide_kernel(A
     const auto fetch = [&](int t0) {
         if (held == 64 / S::GROUPS) {
             const int i = (t0 + 16 * lane) >> a.c.page_log2;
-            pages = i < w.table_len ? w.table[i] : -1;
+            pages = i < table_len ? table[i] : -1;
             pages = pages < a.c.pages ? pages : -1;
             held = 0;
         }
@@ -290,17 +303,13 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attn_wide_kernel(A
     };
 
     // The tile after the next is on its way from the moment that the next one is in LDS.
-    int buffer = 0, t0 = w.begin;
+    int buffer = 0, t0 = begin;
     uint32_t ok = 0;
     const auto put_next = [&](int t, int to) {
         put(t, to);
         ok = ok_next;
         if (t + S::TOK < end) fetch(t + S::TOK);
     };
-    if (t0 < end) {
-        fetch(t0);
-        put_next(t0, 0);
-    }
     const auto walk = [&](auto is_odd) {
         for (; t0 < end; t0 += S::TOK, buffer ^= 1) {
             __syncthreads();
@@ -310,9 +319,22 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attn_wide_kernel(A
             if (t0 + S::TOK < end) put_next(t0 + S::TOK, buffer ^ 1);
         }
     };
-    // From the first tile with values that are not finite and that not every row sees, a second loop: the first one's registers stay where they are.
-    walk(std::false_type());
-    walk(std::true_type());
+    for (int pass = through ? 0 : 1; pass < 2; ++pass) {
+        if (t0 < end) {
+            held = 64 / S::GROUPS;
+            fetch(t0);
+            put_next(t0, buffer);
+        }
+        // From the first tile with values that are not finite and that not every row sees, a second loop: the first one's registers stay where they are.
+        walk(std::false_type());
+        walk(std::true_type());
+        if (pass == 0) {
+            table = w.table, table_len = w.table_len;
+            t0 = w.begin;
+            own_tokens();
+            __syncthreads();                                  // the last tile of the prefix has been read
+        }
+    }
 
     float sum = sum32(l);
     if (sum != sum) m = INFINITY;                             // no part that has seen a NaN counts as empty, or is outweighed
