@@ -155,7 +155,7 @@ template <int DP> __device__ __forceinline__ u32x4 weigh(const float4_t (&sc)[2]
     }
     float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
     top = max16_32(top);
-    if (__any(top > s.m + kSlack)) {
+    if (__any(top > s.m)) {
         const float m = fmaxf(s.m, top);
         const float by = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(s.m - m);
         s.l *= by;
@@ -166,11 +166,11 @@ template <int DP> __device__ __forceinline__ u32x4 weigh(const float4_t (&sc)[2]
     const float m = s.m == -INFINITY ? 0.0f : s.m;
     float w[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        w[i] = __builtin_amdgcn_exp2f(x[i] - m);
-        s.l += w[i];
-    }
-    return u32x4{bf16_pair(w[0], w[1]), bf16_pair(w[2], w[3]), bf16_pair(w[4], w[5]), bf16_pair(w[6], w[7])};
+    for (int i = 0; i < 8; ++i) w[i] = __builtin_amdgcn_exp2f(x[i] - m);
+    const u32x4 p = {bf16_pair(w[0], w[1]), bf16_pair(w[2], w[3]), bf16_pair(w[4], w[5]), bf16_pair(w[6], w[7])};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s.l = add_pair(p[i], s.l);
+    return p;
 }
 
 // element j of the lane's DV for its eight tokens

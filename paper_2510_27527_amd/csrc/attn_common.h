@@ -18,10 +18,6 @@ constexpr int kThreads = 256;
 constexpr int kWaves = 4;
 constexpr int kUnit = 64;                 // tokens in which the parts' lengths are counted
 
-// The maximum that a row's weights are taken from is moved when scores exceed it by more than this (of log2): weights are up to 2^8 then, which loses nothing, and what was summed
-// is rarely scaled.
-constexpr float kSlack = 8.0f;
-
 struct AttnArgs {
     const uint16_t *q;
     int64_t ldq;
@@ -207,6 +203,12 @@ __device__ __forceinline__ uint32_t bf16_of_codes(uint32_t w, bool high, float p
                 : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, power, false));
 }
 __device__ __forceinline__ float power_of(uint32_t bytes, int at) { return u2f(((bytes >> (8 * at)) & 0xFF) << 23); }
+
+// l + the two bf16 of w.  A row's sum is that of its weights as the matrix instructions take them, rounded: where few tokens have most of the weight their roundings cancel.
+__device__ __forceinline__ float add_pair(uint32_t w, float l)
+{
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w), __builtin_bit_cast(bf16x2_t, 0x3F803F80u), l, false);
+}
 
 // what a sum of weights divides by: nothing seen gives zeros, NaN stays
 __device__ __forceinline__ float over(float l) { return l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l; }

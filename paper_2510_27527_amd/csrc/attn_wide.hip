@@ -224,7 +224,9 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attn_wide_kernel(A
         }
         float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
         top = max32(top) * a.scale2;
-        if (__any(top > m + kSlack)) {
+        // moved whenever it is exceeded: a row's largest weight is then 1, which bf16 holds exactly.  (Moved from 2^8 on only: 386 us instead of 398 for four prompts up to 4096 tokens, and
+        // outputs 0.0022 off instead of 0.0018, where rounding the exact ones to bf16 gives 0.0016.)
+        if (__any(top > m)) {
             const float to = fmaxf(m, top), old = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - to);
             l *= old;
 #pragma unroll
@@ -246,8 +248,10 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attn_wide_kernel(A
             float e[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(sc[g / 2][8 * (g & 1) + i], by, -mm));
-            l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
-            return u32x4{bf16_pair(e[0], e[1]), bf16_pair(e[2], e[3]), bf16_pair(e[4], e[5]), bf16_pair(e[6], e[7])};
+            const u32x4 w = {bf16_pair(e[0], e[1]), bf16_pair(e[2], e[3]), bf16_pair(e[4], e[5]), bf16_pair(e[6], e[7])};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) l = add_pair(w[i], l);
+            return w;
         };
         const auto turned = [&](int g, int d) {
             u32x4 f;

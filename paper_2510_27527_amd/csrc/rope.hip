@@ -16,6 +16,14 @@ constexpr int kMaxTokens = 16;               // of a workgroup
 constexpr int kTurnTable = 2048;             // cosines and sines that a workgroup's LDS holds
 constexpr int kSliceElems = 2048;            // elements of the key heads that a workgroup of an 8-bit cache takes: 8 KB of LDS
 
+// i / by for i * by < 2^32, by a product
+struct Quotient {
+    int by;
+    uint32_t magic;
+    __device__ __forceinline__ int operator()(int i) const { return magic ? (int)__umulhi((uint32_t)i, magic) : i; }
+};
+Quotient quotient(int by) { return Quotient{by, by == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + by - 1) / by)}; }
+
 // Cosine and sine of position * freq.  The product of a 31-bit integer and a 24-bit significand has up to 55 bits: in 64 bits it is off by half a unit of
 // the last place at most.  Its turns less the nearest quarter turn leave |x| <= pi / 4 for binary32, where the Taylor series to x^9 and x^10 are off by 2e-9.
 __device__ __forceinline__ float2_t cos_sin(int pos, float freq)
@@ -29,6 +37,43 @@ __device__ __forceinline__ float2_t cos_sin(int pos, float freq)
     const float c = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -1.0f / 3628800, 1.0f / 40320), -1.0f / 720), 1.0f / 24), -0.5f), 1.0f);
     const float a = q & 1 ? s : c, b = q & 1 ? c : s;
     return float2_t{q == 1 || q == 2 ? -a : a, q >= 2 ? -b : b};
+}
+
+// The same in 64 bits, for keys that are rounded to E4M3: an error of 2^-23 moves one in a million of them to a neighbouring code.  The series to x^17 and x^16 are off by 2^-55.
+struct Turn64 {
+    double x, y;
+};
+__device__ __forceinline__ Turn64 cos_sin64(int pos, float freq)
+{
+    const double turns = (double)pos * (double)freq * 0.15915494309189533577;
+    const double quarters = rint(4.0 * turns);
+    const double x = fma(-0.25, quarters, turns) * 6.28318530717958647692, z = x * x;
+    const int q = (int)(long long)quarters & 3;
+    double s = 1.0 / 355687428096000, c = 1.0 / 20922789888000;
+    s = fma(s, z, -1.0 / 1307674368000);
+    s = fma(s, z, 1.0 / 6227020800);
+    s = fma(s, z, -1.0 / 39916800);
+    s = fma(s, z, 1.0 / 362880);
+    s = fma(s, z, -1.0 / 5040);
+    s = fma(s, z, 1.0 / 120);
+    s = fma(s, z, -1.0 / 6);
+    s = fma(s * z, x, x);
+    c = fma(c, z, -1.0 / 87178291200);
+    c = fma(c, z, 1.0 / 479001600);
+    c = fma(c, z, -1.0 / 3628800);
+    c = fma(c, z, 1.0 / 40320);
+    c = fma(c, z, -1.0 / 720);
+    c = fma(c, z, 1.0 / 24);
+    c = fma(c, z, -0.5);
+    c = fma(c, z, 1.0);
+    const double a = q & 1 ? s : c, b = q & 1 ? c : s;
+    return Turn64{q == 1 || q == 2 ? -a : a, q >= 2 ? -b : b};
+}
+// to binary32 for a second rounding to few bits: toward zero, with the last bit set where that left something off, so that the second rounding is that of the number itself
+__device__ __forceinline__ float round_to_odd(double v)
+{
+    const float f = __double2float_rz(v);
+    return (double)f != v && fabsf(f) < INFINITY ? u2f(f2u(f) | 1u) : f;
 }
 
 // Up to eight consecutive elements as they lie in memory; those from n on are zeros.
@@ -94,6 +139,19 @@ template <typename S> __device__ __forceinline__ Unit<S> read_unit(const S *src,
     }
     return r;
 }
+__device__ __forceinline__ void turn_pair(float &a, float &b, float2_t t)
+{
+    const float c = fmaf(a, t.x, -(b * t.y));
+    b = fmaf(b, t.x, a * t.y);
+    a = c;
+}
+__device__ __forceinline__ void turn_pair(float &a, float &b, const Turn64 &t)
+{
+    const double c = fma((double)a, t.x, -((double)b * t.y));
+    b = round_to_odd(fma((double)b, t.x, (double)a * t.y));
+    a = round_to_odd(c);
+}
+
 // The unit turned, in its place.  cs: the token's cosines and sines.  All of a unit has been read before any of it is written: src may be dst.
 template <typename S, typename T>
 __device__ __forceinline__ void write_unit(const Unit<S> &r, T *dst, int D, int half, int pairs, int u, const float2_t *cs)
@@ -110,21 +168,14 @@ __device__ __forceinline__ void write_unit(const Unit<S> &r, T *dst, int D, int 
     if (pairs) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float2_t s = cs[min(j + i, half - 1)], t = cs[min(j + 4 + i, half - 1)];
-            const float a = x[2 * i], b = x[2 * i + 1], c = y[2 * i], d = y[2 * i + 1];
-            x[2 * i] = fmaf(a, s.x, -(b * s.y)), x[2 * i + 1] = fmaf(b, s.x, a * s.y);
-            y[2 * i] = fmaf(c, t.x, -(d * t.y)), y[2 * i + 1] = fmaf(d, t.x, c * t.y);
+            turn_pair(x[2 * i], x[2 * i + 1], cs[min(j + i, half - 1)]);
+            turn_pair(y[2 * i], y[2 * i + 1], cs[min(j + 4 + i, half - 1)]);
         }
         put8(dst + 2 * j, 2 * n, x);
         put8(dst + 2 * j + 8, 2 * n - 8, y);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float2_t t = cs[min(j + i, half - 1)];
-            const float a = x[i], b = y[i];
-            x[i] = fmaf(a, t.x, -(b * t.y));
-            y[i] = fmaf(b, t.x, a * t.y);
-        }
+        for (int i = 0; i < 8; ++i) turn_pair(x[i], y[i], cs[min(j + i, half - 1)]);
         put8(dst + j, n, x);
         put8(dst + half + j, n, y);
     }
@@ -224,62 +275,70 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(const S *q, int64_t
     }
 }
 
-// Keys and values of a token into an 8-bit cache: turned keys go through LDS in binary32, then 16 lanes take the up to 128 elements that share a power of two.
-// blockIdx.y: which heads.
+// Keys and values of a token into an 8-bit cache.  Keys lie in LDS in binary32 and are turned there, a thread a pair; then 16 lanes take the up to 128 elements that share a power of
+// two.  blockIdx.y: which key heads, `slice` of them; the query heads in as many parts.
 template <typename S, typename T>
 __global__ __launch_bounds__(kThreads) void kv_append8_kernel(const S *q, int64_t ldq, int Hq, const S *k, int64_t ldk, const S *v, int64_t ldv, int N, KvCache c, KvBatch b,
-                                                             Rotation r, T *qo, int64_t ldqo, int slice)
+                                                             Rotation r, T *qo, int64_t ldqo, int slice, Quotient units, Quotient half)
 {
     __shared__ float2_t cs[kMaxHeadDim / 2];
-    __shared__ __align__(16) float turned[kSliceElems];
-    const int n = blockIdx.x;
-    const int units = units_of(c.D, r.half);
+    __shared__ Turn64 cs64[kMaxHeadDim / 2];
+    __shared__ __align__(16) float keys[kSliceElems];
+    const int n = blockIdx.x, t = threadIdx.x;
     const int h0 = blockIdx.y * slice, heads = min(slice, c.heads - h0);
-    // the query heads in as many parts as there are slices of key heads
     const int q0 = (int)((int64_t)Hq * blockIdx.y / gridDim.y), q1 = (int)((int64_t)Hq * (blockIdx.y + 1) / gridDim.y);
-    const int uq = (q1 - q0) * units, uk = heads * units, group_lanes = c.groups * kGroupLanes;
+    const int uq = (q1 - q0) * units.by, shift = c.groups == 1 ? 4 : 5;        // 16 or 32 lanes a head where its elements are rounded
     const S *const qn = q + n * ldq + (int64_t)q0 * c.D, *const kn = k + n * ldk + (int64_t)h0 * c.D, *const vn = v + n * ldv + (int64_t)h0 * c.D;
-    const auto read = [&](const S *row, int i) {
-        const int h = i / units;
-        return read_unit(row + (int64_t)h * c.D, c.D, r.half, r.pairs, i - h * units);
+    const auto read_query = [&](int i) {
+        const int h = units(i);
+        return read_unit(qn + (int64_t)h * c.D, c.D, r.half, r.pairs, i - h * units.by);
     };
     const auto read_value = [&](int i) {
-        const int h = i / group_lanes, at = 8 * (i - h * group_lanes);
+        const int h = i >> shift, at = 8 * (i - (h << shift));
         return raw8(vn + (int64_t)h * c.D + at, c.D - at);
     };
-    // the thread's first unit of each is on its way while the place is looked up
-    const int t = threadIdx.x;
-    Unit<S> qu, ku;
+    // what the thread loads first is on its way while the place is looked up
+    Unit<S> qu;
     RawOf<S> vu;
-    if (t < uk) ku = read(kn, t);
-    if (t < heads * group_lanes) vu = read_value(t);
-    if (t < uq) qu = read(qn, t);
+    if (t < heads << shift) vu = read_value(t);
+    if (t < uq) qu = read_query(t);
+    for (int i = t; i < heads * (c.D / 8); i += kThreads) {
+        float e[8];
+        widen(raw8(kn + 8 * i, 8), e);
+        put8(keys + 8 * i, 8, e);
+    }
     int seq;
     const int place = place_of(b, c, n, N, seq);
     if (place < 0) return;
     const int page = page_of(b, c, seq, place);
-    for (int j = t; j < r.half; j += kThreads) cs[j] = turn_of(r, place + b.prefix, j, 0);
+    for (int j = t; j < r.half; j += kThreads) {
+        Turn64 x = cos_sin64(place + b.prefix, r.freqs[j]);
+        x.x *= (double)r.scale, x.y *= (double)r.scale;
+        cs64[j] = x;
+        cs[j] = float2_t{(float)x.x, (float)x.y};
+    }
     __syncthreads();
-    if (page >= 0)
-        for (int i = t; i < uk; i += kThreads) {
-            const int h = i / units;
-            if (i >= kThreads) ku = read(kn, i);
-            write_unit(ku, turned + h * c.D, c.D, r.half, r.pairs, i - h * units, cs);
-        }
+    for (int i = t; i < heads * r.half; i += kThreads) {
+        const int h = half(i), j = i - h * r.half;
+        float *const a = keys + h * c.D + (r.pairs ? 2 * j : j), *const z = a + (r.pairs ? 1 : r.half);
+        float x = *a, y = *z;
+        turn_pair(x, y, cs64[j]);
+        *a = x, *z = y;
+    }
     for (int i = t; i < uq; i += kThreads) {
-        const int h = i / units;
-        if (i >= kThreads) qu = read(qn, i);
-        write_unit(qu, qo + n * ldqo + (int64_t)(q0 + h) * c.D, c.D, r.half, r.pairs, i - h * units, cs);
+        const int h = units(i);
+        if (i >= kThreads) qu = read_query(i);
+        write_unit(qu, qo + n * ldqo + (int64_t)(q0 + h) * c.D, c.D, r.half, r.pairs, i - h * units.by, cs);
     }
     if (page < 0) return;
     __syncthreads();
     const int slot = place & ((1 << c.page_log2) - 1);
     // Every lane of 16 that share a group come by together: the count is a multiple of 16.
-    for (int i = t; i < heads * group_lanes; i += kThreads) {
-        const int h = i / group_lanes, at = 8 * (i - h * group_lanes);
+    for (int i = t; i < heads << shift; i += kThreads) {
+        const int h = i >> shift, at = 8 * (i - (h << shift));
         const int64_t row = (((int64_t)page * c.heads + h0 + h) << c.page_log2) + slot;
         float e[8] = {};
-        if (at < c.D) widen(raw8(turned + h * c.D + at, 8), e);
+        if (at < c.D) widen(raw8(keys + h * c.D + at, 8), e);
         ckpt_store8<false>(CkptOut{static_cast<uint8_t *>(c.k), c.k_exps, c.groups}, row, at, c.D, e);
         if (i >= kThreads) vu = read_value(i);
         widen(vu, e);
@@ -329,9 +388,10 @@ hipError_t run_append(const RowSrc &q, int Hq, const RowSrc &k, const RowSrc &v,
     const S *const qp = static_cast<const S *>(q.p), *const kp = static_cast<const S *>(k.p), *const vp = static_cast<const S *>(v.p);
     T *const op = static_cast<T *>(qo.p);
     if (c.bits8) {
-        const int slice = kSliceElems / c.D;
+        const int fit = kSliceElems / c.D, slice = fit < c.heads ? fit : c.heads;
         const dim3 grid((unsigned)N, (unsigned)((c.heads + slice - 1) / slice));
-        kv_append8_kernel<S, T><<<grid, kThreads, 0, st>>>(qp, q.ld, Hq, kp, k.ld, vp, v.ld, (int)N, c, b, r, op, qo.ld, slice);
+        kv_append8_kernel<S, T><<<grid, kThreads, 0, st>>>(qp, q.ld, Hq, kp, k.ld, vp, v.ld, (int)N, c, b, r, op, qo.ld, slice, quotient(units_of(c.D, r.half)),
+                                                          quotient(r.half > 0 ? r.half : 1));
     } else {
         const int64_t row_units = (int64_t)(Hq + c.heads) * units_of(c.D, r.half) + (int64_t)c.heads * (c.D / 8);
         const int tokens = tokens_of_group(row_units, r.half);
