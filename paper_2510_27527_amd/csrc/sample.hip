@@ -18,9 +18,12 @@ namespace {
 constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / 64;
 constexpr int kBins = 1024;                   // the last one: 31.9 and more below the largest, where weights are 0
-constexpr int kCuts = 1024;                   // cuts of a bin
+constexpr int kChoose = 512;                  // threads that draw from a row's list
+constexpr int kCuts = kChoose;                // cuts of a bin
+constexpr int kCutBits = 9;
 constexpr int kFew = 64;                      // tokens among which a wave finds the place
-constexpr int kList = 4096;                   // tokens that are taken out of a row; where there are more, they stay in it
+constexpr int kList = 8192;                   // tokens that are taken out of a row; where there are more, they stay in it
+constexpr int kSliceList = 4096;              // and out of a slice
 constexpr int kMaxSlices = 8;
 constexpr int kKept = 2;                      // runs of eight logits that a thread keeps between its two walks over them
 constexpr double kOne = 8796093022208.0;      // 2^43
@@ -210,7 +213,7 @@ template <bool F32> __global__ __launch_bounds__(kThreads) void sample_bins_kern
 }
 
 // (weight, number of tokens) up to and with each thread's; all threads of the workgroup call it
-__device__ __forceinline__ void scan(double &w, uint32_t &c, double *lw, uint32_t *lc)
+template <int WAVES> __device__ __forceinline__ void scan(double &w, uint32_t &c, double *lw, uint32_t *lc)
 {
     for (int o = 1; o < 64; o <<= 1) {
         const double x = __shfl_up(w, o, 64);
@@ -223,7 +226,8 @@ __device__ __forceinline__ void scan(double &w, uint32_t &c, double *lw, uint32_
     __syncthreads();
     double x = 0.0;
     uint32_t y = 0;
-    for (int i = 0; i < kWaves; ++i)
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i)
         if (i < wave) x += lw[i], y += lc[i];
     w += x, c += y;
 }
@@ -295,12 +299,12 @@ __device__ __forceinline__ float logit_of(uint32_t k) { return u2f(k & 0x8000000
 template <bool F32, typename Do> __device__ __forceinline__ void each(const SampleArgs &a, const Row &r, Shared &s, int bin, Do &&what)
 {
     if (r.listed >= 0) {
-        for (int i = threadIdx.x; i < r.listed; i += kThreads) {
+        for (int i = threadIdx.x; i < r.listed; i += kChoose) {
             const float x = logit_of(s.keys[i]);
             if (bin_below(r.anchor, x, r.per_unit) == bin) what((uint64_t)s.keys[i] << 32 | s.index[i], x, s.weights[i]);
         }
     } else {
-        for (int i = 8 * threadIdx.x; i < (int)a.V; i += 8 * kThreads) {
+        for (int i = 8 * threadIdx.x; i < (int)a.V; i += 8 * kChoose) {
             float v[8];
             logits8<F32>(a, r.row, i, (int)a.V, v);
             for (int j = 0; j < 8; ++j) {
@@ -327,7 +331,7 @@ template <bool F32, bool RANK> __device__ void locate(const SampleArgs &a, const
         }
     }
     const uint64_t span = high - low;
-    int shift = span >> 10 ? 54 - __clzll((long long)span) : 0;           // span >> shift < 1024
+    int shift = span >> kCutBits ? 64 - kCutBits - __clzll((long long)span) : 0;           // span >> shift < kCuts
     __syncthreads();
     for (;;) {
         s.sums[threadIdx.x] = 0;
@@ -345,7 +349,7 @@ template <bool F32, bool RANK> __device__ void locate(const SampleArgs &a, const
         double w = (double)s.sums[threadIdx.x];
         const double own = w;
         uint32_t c = here;
-        scan(w, c, s.lw, s.lc);
+        scan<kChoose / 64>(w, c, s.lw, s.lc);
         w += before;
         c += rank;
         // the cut in which the sum passes the target; the last one that weighs anything where none does
@@ -362,7 +366,7 @@ template <bool F32, bool RANK> __device__ void locate(const SampleArgs &a, const
         const uint32_t tokens = s.counts[cut];
         __syncthreads();
         if (tokens <= kFew) break;                           // with shift = 0 there is one
-        shift = shift > 10 ? shift - 10 : 0;
+        shift = shift > kCutBits ? shift - kCutBits : 0;
     }
     if (threadIdx.x == 0) s.n = 0;
     __syncthreads();
@@ -397,7 +401,7 @@ template <bool F32> __global__ __launch_bounds__(kThreads) void sample_list_kern
 {
     __shared__ double ends[kBins];
     __shared__ uint32_t count_ends[kBins];
-    __shared__ uint32_t keys[kList], index[kList];
+    __shared__ uint32_t keys[kSliceList], index[kSliceList];
     __shared__ double lw[kWaves], factors[kMaxSlices];
     __shared__ uint32_t lc[kWaves], n, base;
     __shared__ int bins[8];
@@ -443,7 +447,7 @@ template <bool F32> __global__ __launch_bounds__(kThreads) void sample_list_kern
     }
     const double own = w;
     const uint32_t own_count = c;
-    scan(w, c, lw, lc);
+    scan<kWaves>(w, c, lw, lc);
     ends[t] = w;
     count_ends[t] = c;
     __syncthreads();
@@ -522,22 +526,22 @@ template <bool F32> __global__ __launch_bounds__(kThreads) void sample_list_kern
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             if (mine >> j & 1) {
-                if (at < kList) keys[at] = key_of(v[j]), index[at] = (uint32_t)(i + j);
+                if (at < kSliceList) keys[at] = key_of(v[j]), index[at] = (uint32_t)(i + j);
                 ++at;
             }
     }
     __syncthreads();
     const uint32_t many = n;
     if (many == 0) return;
-    if (t == 0) base = atomicAdd(&out.listed, many);
+    if (t == 0) base = atomicAdd(&out.listed, many > kSliceList ? kList + 1u : many);
     __syncthreads();
     const uint32_t to = base;
-    for (uint32_t i = t; i < min(many, (uint32_t)kList); i += kThreads)
+    for (uint32_t i = t; i < min(many, (uint32_t)kSliceList); i += kThreads)
         if (to + i < kList) out.keys[to + i] = keys[i], out.index[to + i] = index[i];
 }
 
 // The draw, from the joined bins and the listed tokens.
-template <bool F32> __global__ __launch_bounds__(kThreads) void sample_choose_kernel(SampleArgs a, Space ws, int slices)
+template <bool F32> __global__ __launch_bounds__(kChoose) void sample_choose_kernel(SampleArgs a, Space ws, int slices)
 {
     __shared__ Shared s;
     const int64_t row = blockIdx.x;
@@ -554,9 +558,8 @@ template <bool F32> __global__ __launch_bounds__(kThreads) void sample_choose_ke
     const float p = a.top_p ? fmaxf(a.top_p[row], 0.0f) : 1.0f, m = a.min_p ? fminf(a.min_p[row], 1.0f) : 0.0f;
     const double u = share_of(a.u[row]);
     const uint32_t listed = in.listed;
-    s.ends[t] = in.ends[t];
-    s.count_ends[t] = in.count_ends[t];
-    for (uint32_t i = t; i < min(listed, (uint32_t)kList); i += kThreads) {
+    for (int i = t; i < kBins; i += kChoose) s.ends[i] = in.ends[i], s.count_ends[i] = in.count_ends[i];
+    for (uint32_t i = t; i < min(listed, (uint32_t)kList); i += kChoose) {
         const uint32_t key = in.keys[i];
         s.keys[i] = key, s.index[i] = in.index[i], s.weights[i] = r.weight(logit_of(key));
     }
@@ -567,7 +570,8 @@ template <bool F32> __global__ __launch_bounds__(kThreads) void sample_choose_ke
     const auto bin_of_sum = [&](double sum, int first, int last) {
         if (t == 0) s.bin = last;
         __syncthreads();
-        if (t >= first && t < last && sum < s.ends[t]) atomicMin(&s.bin, t);
+        for (int i = first + t; i < last; i += kChoose)
+            if (sum < s.ends[i]) atomicMin(&s.bin, i);
         __syncthreads();
         return s.bin;
     };
@@ -591,8 +595,8 @@ template <bool F32> __global__ __launch_bounds__(kThreads) void sample_choose_ke
             });
         double all = (double)sum;
         uint32_t none = 0;
-        scan(all, none, s.lw, s.lc);
-        if (t == kThreads - 1) s.found[0] = all + (in.m0 ? s.ends[in.m0 - 1] : 0.0);
+        scan<kChoose / 64>(all, none, s.lw, s.lc);
+        if (t == kChoose - 1) s.found[0] = all + (in.m0 ? s.ends[in.m0 - 1] : 0.0);
         __syncthreads();
         kept = fmin(kept, s.found[0]);
     }
@@ -618,7 +622,7 @@ template <bool F32> hipError_t run(const SampleArgs &a, void *ws, hipStream_t st
     const Space space = space_of(ws, a.N, slices);
     sample_bins_kernel<F32><<<(unsigned)(a.N * slices), kThreads, 0, st>>>(a, space, slices, len);
     sample_list_kernel<F32><<<(unsigned)(a.N * slices), kThreads, 0, st>>>(a, space, slices, len);
-    sample_choose_kernel<F32><<<(unsigned)a.N, kThreads, 0, st>>>(a, space, slices);
+    sample_choose_kernel<F32><<<(unsigned)a.N, kChoose, 0, st>>>(a, space, slices);
     return hipGetLastError();
 }
 
