@@ -360,17 +360,27 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(AttnArgs a)
     const int64_t pre = a.prefix_parts ? ((int64_t)(in_all / a.prefix_rows) * a.prefix_parts * a.c.heads + kv) * a.prefix_rows + in_all % a.prefix_rows : 0;
     float m = -INFINITY, l = 0.0f;
     float4_t o = {0, 0, 0, 0};
-    for (int i = group; i < total; i += GROUPS) {
-        const bool mine = i < parts;
-        const int64_t slot = mine ? own + (int64_t)i * a.c.heads * a.own_rows : pre + (int64_t)(i - parts) * a.c.heads * a.prefix_rows;
-        const float2_t ml = (mine ? a.own_ml : a.prefix_ml)[slot];
-        const float4_t v = 4 * lane < a.c.D ? *reinterpret_cast<const float4_t *>((mine ? a.own_o : a.prefix_o) + slot * a.c.D + 4 * lane) : float4_t{0, 0, 0, 0};
-        const float top = fmaxf(m, ml.x);
-        if (top == -INFINITY) continue;
-        const float old = __builtin_amdgcn_exp2f(m - top), by = __builtin_amdgcn_exp2f(ml.x - top);
-        l = l * old + ml.y * by;
-        o = ml.x == -INFINITY ? o * old : o * old + v * by;
-        m = top;
+    constexpr int AT_ONCE = 4;                                // parts whose loads a group has on their way together
+    for (int i0 = group; i0 < total; i0 += AT_ONCE * GROUPS) {
+        float2_t ml[AT_ONCE];
+        float4_t v[AT_ONCE];
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) {
+            const int i = i0 + j * GROUPS;
+            const bool mine = i < parts;
+            const int64_t slot = mine ? own + (int64_t)i * a.c.heads * a.own_rows : pre + (int64_t)(i - parts) * a.c.heads * a.prefix_rows;
+            ml[j] = i < total ? (mine ? a.own_ml : a.prefix_ml)[slot] : float2_t{-INFINITY, 0.0f};
+            v[j] = i < total && 4 * lane < a.c.D ? *reinterpret_cast<const float4_t *>((mine ? a.own_o : a.prefix_o) + slot * a.c.D + 4 * lane) : float4_t{0, 0, 0, 0};
+        }
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) {
+            const float top = fmaxf(m, ml[j].x);
+            if (top == -INFINITY) continue;
+            const float old = __builtin_amdgcn_exp2f(m - top), by = __builtin_amdgcn_exp2f(ml[j].x - top);
+            l = l * old + ml[j].y * by;
+            o = ml[j].x == -INFINITY ? o * old : o * old + v[j] * by;
+            m = top;
+        }
     }
     sums[group][lane] = o;
     if (lane == 0) mls[group] = float2_t{m, l};
