@@ -5,7 +5,7 @@
 //
 // Nothing is sorted.  The order is cut into bins 1/32 of a unit of x / T wide (a function of x that never falls as x grows, whatever it is rounded to), and a bin's weight and number of tokens say which bin a
 // border lies in: one kernel makes the bins of slices of a row, a second joins them and takes from the row the tokens of the few bins that matter, a third finds the places inside these
-// bins by further cuts, of the 64-bit number (x, index) that the order goes by.
+// bins by further cuts, of the number (x, index) of 52 bits that the order goes by.
 //
 // Weights are fixed-point numbers, 2^43 for the largest: their sums do not depend on the order of the additions, which LDS atomics leave open.
 #include "rowwise.h"
@@ -21,6 +21,7 @@ constexpr int kBins = 1024;                   // the last one: 31.9 and more bel
 constexpr int kChoose = 512;                  // threads that draw from a row's list
 constexpr int kCuts = kChoose;                // cuts of a bin
 constexpr int kCutBits = 9;
+constexpr int kIndexBits = 20;                // of a token in a row: V is at most 2^20
 constexpr int kFew = 64;                      // tokens among which a wave finds the place
 constexpr int kList = 8192;                   // tokens that are taken out of a row; where there are more, they stay in it
 constexpr int kSliceList = 4096;              // and out of a slice
@@ -293,6 +294,7 @@ __device__ __forceinline__ uint32_t key_of(float x)
     const uint32_t b = f2u(x);
     return b & 0x80000000u ? b : ~(b | 0x80000000u);
 }
+__device__ __forceinline__ uint64_t place_of(uint32_t key, uint32_t index) { return (uint64_t)key << kIndexBits | index; }
 __device__ __forceinline__ float logit_of(uint32_t k) { return u2f(k & 0x80000000u ? k : ~k & 0x7FFFFFFFu); }
 
 // what(place in the order as a number, logit, weight) for every token of bin `bin`
@@ -301,15 +303,20 @@ template <bool F32, typename Do> __device__ __forceinline__ void each(const Samp
     if (r.listed >= 0) {
         for (int i = threadIdx.x; i < r.listed; i += kChoose) {
             const float x = logit_of(s.keys[i]);
-            if (bin_below(r.anchor, x, r.per_unit) == bin) what((uint64_t)s.keys[i] << 32 | s.index[i], x, s.weights[i]);
+            if (bin_below(r.anchor, x, r.per_unit) == bin) what(place_of(s.keys[i], s.index[i]), x, s.weights[i]);
         }
     } else {
+        // many of these logits are equal, and their weight is made once
+        float last = INFINITY;
+        uint64_t weight = 0;
         for (int i = 8 * threadIdx.x; i < (int)a.V; i += 8 * kChoose) {
             float v[8];
             logits8<F32>(a, r.row, i, (int)a.V, v);
             for (int j = 0; j < 8; ++j) {
                 const float x = seen(v[j], r.infinite);
-                if (x != -INFINITY && bin_below(r.anchor, x, r.per_unit) == bin) what((uint64_t)key_of(x) << 32 | (uint32_t)(i + j), x, r.weight(x));
+                if (x == -INFINITY || bin_below(r.anchor, x, r.per_unit) != bin) continue;
+                if (x != last) last = x, weight = r.weight(x);
+                what(place_of(key_of(x), (uint32_t)(i + j)), x, weight);
             }
         }
     }
@@ -322,12 +329,12 @@ template <bool F32, bool RANK> __device__ void locate(const SampleArgs &a, const
     double before = bin ? s.ends[bin - 1] : 0.0;
     uint32_t rank = bin ? s.count_ends[bin - 1] : 0;
     // The numbers that the bin's tokens can have, from its edges (a little wider, for the product's rounding); everything where the bin's number was limited, or has no edges.
-    uint64_t low = 0, high = ~0ull;
+    uint64_t low = 0, high = (1ull << (32 + kIndexBits)) - 1;
     {
         const double f = (double)r.anchor - bin, per = (double)r.per_unit, up = (f + 1.0) / per, down = f / per;
         if (fabs(f) < 0x1p29 && fabs(up) < 0x1p126 && fabs(down) < 0x1p126) {
-            low = (uint64_t)key_of((float)(up + fabs(up) * 0x1p-20 + 0x1p-126)) << 32;
-            high = (uint64_t)key_of((float)(down - fabs(down) * 0x1p-20 - 0x1p-126)) << 32 | 0xFFFFFFFFu;
+            low = place_of(key_of((float)(up + fabs(up) * 0x1p-20 + 0x1p-126)), 0);
+            high = place_of(key_of((float)(down - fabs(down) * 0x1p-20 - 0x1p-126)), (1u << kIndexBits) - 1);
         }
     }
     const uint64_t span = high - low;
@@ -338,12 +345,31 @@ template <bool F32, bool RANK> __device__ void locate(const SampleArgs &a, const
         s.counts[threadIdx.x] = 0;
         if (threadIdx.x == 0) s.cut = -1;
         __syncthreads();
+        // What a thread has for one cut is held back until it meets another: where a row is searched whole most tokens fall into the same one, and additions to it follow each other
+        // (a row of 131072 equal logits 2.9 -> 0.69 ms, with weights of equal logits made once).
+        uint64_t held = 0;
+        uint32_t many = 0;
+        int held_cut = 0;
+        const auto give = [&] {
+            if (!many) return;
+            atomicAdd(reinterpret_cast<unsigned long long *>(&s.sums[held_cut]), (unsigned long long)held);
+            atomicAdd(&s.counts[held_cut], many);
+        };
         each<F32>(a, r, s, bin, [&](uint64_t k, float, uint64_t weight) {
             const uint64_t c = (k - low) >> shift;
             if (k < low || c >= kCuts) return;
-            atomicAdd(reinterpret_cast<unsigned long long *>(&s.sums[c]), (unsigned long long)weight);
-            atomicAdd(&s.counts[c], 1u);
+            if (r.listed >= 0) {
+                atomicAdd(reinterpret_cast<unsigned long long *>(&s.sums[c]), (unsigned long long)weight);
+                atomicAdd(&s.counts[c], 1u);
+                return;
+            }
+            if ((int)c != held_cut) {
+                give();
+                held = 0, many = 0, held_cut = (int)c;
+            }
+            held += weight, ++many;
         });
+        give();
         __syncthreads();
         const uint32_t here = s.counts[threadIdx.x];
         double w = (double)s.sums[threadIdx.x];
@@ -390,7 +416,7 @@ template <bool F32, bool RANK> __device__ void locate(const SampleArgs &a, const
             // the first that passes the target; if none does, the last that weighs anything
             const bool passes = RANK ? (double)(rank + at) == target : e > target && !(b > target && at > 0);
             const bool last = !RANK && e <= target && s.few_weight[i] > 0 && behind == s.few_weight[i];
-            if (passes || last) s.found[0] = b, s.found[1] = e, s.token = (int)(uint32_t)s.few[i];
+            if (passes || last) s.found[0] = b, s.found[1] = e, s.token = (int)(s.few[i] & ((1u << kIndexBits) - 1));
         }
     }
     __syncthreads();

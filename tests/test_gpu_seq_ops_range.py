@@ -342,3 +342,27 @@ def test_captured_steps(tj):  # noqa: F811
             for a, b in zip(kept, step()):
                 assert torch.equal(a, b), turn_no
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("V", [8193, 50021, 1 << 20])
+@pytest.mark.parametrize("values", ["equal", "near", "masked"])
+def test_sample_of_crowded_rows(tj, V, values):  # noqa: F811
+    """More tokens around the borders than the list holds: equal logits, different ones closer together than a bin is wide, and the larger half of a row equal above the others."""
+    N = 4
+    g = torch.Generator().manual_seed(V)
+    if values == "equal":
+        x = torch.full((N, V), -2.5)
+    elif values == "near":
+        x = 1.0 + 0.01 * torch.rand(N, V, generator=g)
+    else:
+        x = torch.where(torch.rand(N, V, generator=g) < 0.5, torch.tensor(3.0), torch.tensor(-1e30))
+    u = torch.tensor([0.0, 0.2513, 0.7031, 1 - 2.0 ** -24])
+    p = torch.tensor([0.9, 0.35, 0.6, 0.77])
+    k = torch.tensor([V // 3, 0, 8192, V // 2 - 5], dtype=torch.int32)
+    for t in (BF, F32):
+        y = x.to(t)
+        for kw in ({}, dict(p=p), dict(k=k, p=p)):
+            print("sample", V, values, t, sorted(kw), flush=True)
+            names = dict(p="top_p", k="top_k")
+            got = tj.sample(y.cuda(), u.cuda(), **{names[n]: a.cuda() for n, a in kw.items()})
+            assert got.tolist() == ref.sample(y, u, **kw), sorted(kw)
