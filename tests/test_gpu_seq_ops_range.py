@@ -366,3 +366,13 @@ def test_sample_of_crowded_rows(tj, V, values):  # noqa: F811
             names = dict(p="top_p", k="top_k")
             got = tj.sample(y.cuda(), u.cuda(), **{names[n]: a.cuda() for n, a in kw.items()})
             assert got.tolist() == ref.sample(y, u, **kw), sorted(kw)
+
+
+@pytest.mark.parametrize("rows", [47, 48, 49, 63, 64])
+@pytest.mark.parametrize("bits8", [False, True])
+@pytest.mark.parametrize("shared", [False, True])
+def test_attention_between_the_kinds_of_tiles(tj, rows, bits8, shared):  # noqa: F811
+    """Rows on either side of where a call takes tiles of 128: new tokens of a sequence after others, and single tokens after a prefix."""
+    case = ([5] * rows, [1] * rows, 2, 2, 128, 16, 333) if shared else ([200, 3], [rows, rows], 2, 2, 64, 32, 0)
+    bt, q, k, v, o, scale = run_attn(tj, case, bits8, 3)
+    check_attn(bt, q, k, v, o, scale, 2)
