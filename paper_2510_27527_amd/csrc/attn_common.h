@@ -166,6 +166,7 @@ template <bool PREFIX> __device__ __forceinline__ bool work_of(const AttnArgs &a
         // the tiles that see most come first
         w.tile = tiles_of(w.count, a.G, a.own_rows) - 1 - p.tile;
         w.slot = p.base + (int64_t)w.tile * p.parts + p.part;
+        if (a.slots > 0 && w.slot >= a.slots) return false;  // starts that name rows twice make more tiles than the workspace has room for
         w.parts = a.b.prefix && !a.through ? 2 : p.parts;
         if (a.slots > 0 && blockIdx.x % a.c.heads == 0 && p.tile == 0 && p.part == 0 && threadIdx.x == 0) a.lie[2 * p.b] = p.base, a.lie[2 * p.b + 1] = p.parts;
         w.len = tokens_of(a.b, a.c, p.b);

@@ -376,3 +376,24 @@ def test_attention_between_the_kinds_of_tiles(tj, rows, bits8, shared):  # noqa:
     case = ([5] * rows, [1] * rows, 2, 2, 128, 16, 333) if shared else ([200, 3], [rows, rows], 2, 2, 64, 32, 0)
     bt, q, k, v, o, scale = run_attn(tj, case, bits8, 3)
     check_attn(bt, q, k, v, o, scale, 2)
+
+
+@pytest.mark.parametrize("N,starts,past,prefix", [(100, [0, 100] * 5 + [0], 40, 200), (40, [0, 40] * 9 + [0], 500, 0), (300, [0, 300, 7] * 6 + [300], 100, 777), (64, [0, 64, 0, 64], 300, 0)])
+@pytest.mark.parametrize("bits8", [False, True])
+def test_starts_that_name_rows_often_stay_in_the_workspace(tj, N, starts, past, prefix, bits8):  # noqa: F811
+    """More tiles than the sizes of the call allow for: nothing behind the workspace or beside the output is written."""
+    Hq, H, D, page = 2, 1, 64, 16
+    B = len(starts) - 1
+    bt = ref.Batch(tj, [past] * B, [1] * B, H, D, page, bits8, prefix, seed=4)
+    normal = draws(9)
+    T = len(bt.tokens())
+    bt.fill(normal(T, H, D), normal(T, H, D))
+    kv = tj.KVBatch(bt.kv.table, bt.kv.lens, torch.tensor(starts, dtype=torch.int32).cuda(), bt.kv.prefix_table, prefix)
+    q = normal(N, Hq * D).to(BF).cuda()
+    need = tj.attn_workspace_bytes(N, Hq, bt.cache, kv)
+    whole = torch.full((need + (1 << 20),), 0xA5, dtype=torch.uint8, device="cuda")
+    out, o = spread(torch.zeros(N, Hq * D, dtype=BF, device="cuda"), 1, 3)
+    print("attn", N, starts, past, prefix, bits8, flush=True)
+    tj.attn(q, bt.cache, kv, Hq, Out=o, ws=whole[:need])
+    torch.cuda.synchronize()
+    assert bool((whole[need:] == 0xA5).all()) and untouched(out, o)
