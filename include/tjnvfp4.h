@@ -399,7 +399,7 @@ int nvfp4_rope_frequencies(int64_t R, double base, int scaling, double factor, d
 /*
  * Y = X with the H heads of D elements of every row turned by pos[n] (device int32 [N], 4-byte aligned); inverse != 0: the transposed rotation (angles negated, the same scale), which
  * takes the gradient of Y to the gradient of X.  X is NVFP4_SRC_BF16 or _F32.  Y may be X itself, with X's type and stride; else it must not overlap X.
- * H * D <= 2^22, D <= 4096, N <= 2^24.  Errors: NULL, SHAPE, ENUM, ALIGN.
+ * H * D <= 2^22, D <= 4096, N < 2^24.  Errors: NULL, SHAPE, ENUM, ALIGN.
  */
 int nvfp4_rope(const void *X, int src_kind, int64_t ldx, const int32_t *pos, int64_t N, int64_t H, int64_t D, const nvfp4_rotation *rotation, int inverse,
                void *Y, int out_dtype, int64_t ldy, void *stream);
@@ -430,7 +430,7 @@ typedef struct nvfp4_kvbatch {
 
 /*
  * Writes keys K [N x H D] (turned at their positions; rotation NULL: as they are) and values V [N x H D] of the batch's rows into the cache.  Q (optional) [N x Hq D]: turned in the same way into Qo.
- * K, V and Q are src_kind; Qo is out_dtype.  Two rows with one place (a page named twice) leave one of the two there, element by element either's.
+ * K, V and Q are src_kind; Qo is out_dtype.  N < 2^24.  Two rows with one place (a page named twice) leave one of the two there, element by element either's.
  * Errors: NULL, SHAPE, ENUM, ALIGN, MISMATCH (starts NULL and N != B).
  */
 int nvfp4_kv_append(const void *Q, int64_t ldq, int64_t Hq, const void *K, int64_t ldk, const void *V, int64_t ldv, int src_kind, int64_t N,
@@ -444,7 +444,8 @@ int nvfp4_kv_load(const nvfp4_kvcache *cache, const nvfp4_kvbatch *batch, int64_
  *   out = sum_t softmax_t(scale q . k_t) v_t        (zeros where it sees nothing)
  * Out [N x Hq D] bf16.  Scores and sums are binary32; the weights of the values are rounded to bf16 for the matrix instructions.  A NaN or infinity in a key or value stays with the
  * rows that see it.  The prefix is read once for all rows of a tile, whatever the number of sequences.
- * Hq a multiple of H, N * Hq <= 2^30; scale finite and above 0.  ws: nvfp4_attn_workspace_bytes of the same sizes (16-byte aligned; from N, B, width and prefix alone, not from lengths, so that
+ * Hq a multiple of H, N < 2^24, N * Hq <= 2^30, and less than 2^24 workgroups: one takes a key head of 16 rows (128 where a sequence, or for the prefix the batch, has 48 and more; a row is a
+ * token and query head), or one token and query head where partial results are joined (a prefix in front of few rows each); SHAPE otherwise.  Out must not overlap Q.  scale finite and above 0.  ws: nvfp4_attn_workspace_bytes of the same sizes (16-byte aligned; from N, B, width and prefix alone, not from lengths, so that
  * one does for all steps of a batch).  Same inputs, same bits.  Errors: NULL, SHAPE, ENUM, ALIGN, MISMATCH, WORKSPACE.
  */
 int nvfp4_attn(const void *Q, int64_t ldq, int64_t N, int64_t Hq, const nvfp4_kvcache *cache, const nvfp4_kvbatch *batch, float scale, void *Out, int64_t ldo,
@@ -461,7 +462,7 @@ size_t nvfp4_attn_workspace_bytes(int64_t N, int64_t Hq, int64_t H, int64_t D, i
  * and of what is left, in this order, the first token whose sum of w with those before it exceeds u times the sum of all.  temperature <= 0 or NaN: the first of the order.
  * NaN logits count as -infinity, which is never drawn; several +infinities share the probability; a row without anything else than -infinity gives -1.
  * temperature, top_k, top_p, min_p: device [N], each optional (1, and no limit).  w and its sums are fixed-point numbers with 2^43 for the largest weight: sums do not depend on
- * their order, and weights under 2^-44 of the largest are 0.  u and the tokens (int64) are device [N].  1 <= V <= 2^20, N <= 2^24.
+ * their order, and weights under 2^-44 of the largest are 0.  u and the tokens (int64) are device [N].  1 <= V <= 2^20, N < 2^22.
  * ws: nvfp4_sample_workspace_bytes(N, V), 16-byte aligned.  Errors: NULL, SHAPE, ENUM, ALIGN, WORKSPACE.
  */
 int nvfp4_sample(const void *logits, int src_kind, int64_t ld, int64_t N, int64_t V, const float *u, const float *temperature, const int32_t *top_k,

@@ -176,7 +176,8 @@ size_t nvfp4_attn_workspace_bytes(int64_t N, int64_t Hq, int64_t H, int64_t D, i
     if (N <= 0 || N > kMaxRows || H < 1 || H > kMaxWidth || Hq < 1 || Hq % H != 0 || Hq > kMaxHeadRows / N || !is_head_dim(D) || !is_page(page) || B <= 0 ||
         check_counts(B, width, prefix, page))
         return 0;
-    return attn_workspace_bytes(N, (int)Hq, (int)H, (int)D, (int)B, width * page, prefix);
+    const int64_t need = attn_workspace_bytes(N, (int)Hq, (int)H, (int)D, (int)B, width * page, prefix);
+    return need > 0 ? (size_t)need : 0;
 }
 
 int nvfp4_attn(const void *Q, int64_t ldq, int64_t N, int64_t Hq, const nvfp4_kvcache *cache, const nvfp4_kvbatch *batch, float scale, void *Out, int64_t ldo,
@@ -198,8 +199,9 @@ int nvfp4_attn(const void *Q, int64_t ldq, int64_t N, int64_t Hq, const nvfp4_kv
     rc = make_dst(Out, NVFP4_OUT_BF16, ldo, N, Hq * c.D, &out);
     if (rc) return rc;
     if (!isfinite(scale) || !(scale > 0.0f)) return NVFP4_ERR_ENUM;
-    const size_t need = nvfp4_attn_workspace_bytes(N, Hq, c.heads, c.D, (int64_t)1 << c.page_log2, b.B, b.width, b.prefix);
-    if (need && (!ws || ws_bytes < need)) return NVFP4_ERR_WORKSPACE;
+    const int64_t need = N == 0 || b.B == 0 ? 0 : attn_workspace_bytes(N, (int)Hq, c.heads, c.D, b.B, (int64_t)b.width << c.page_log2, b.prefix);
+    if (need < 0) return NVFP4_ERR_SHAPE;
+    if (need && (!ws || ws_bytes < (size_t)need)) return NVFP4_ERR_WORKSPACE;
     if (need && !aligned(ws, 16)) return NVFP4_ERR_ALIGN;
     if (N == 0 || b.B == 0) return NVFP4_OK;
     return status(launch_attn(static_cast<const uint16_t *>(Q), q.ld, N, (int)Hq, c, b, scale, static_cast<uint16_t *>(Out), out.ld, ws, static_cast<hipStream_t>(stream)));
@@ -207,7 +209,7 @@ int nvfp4_attn(const void *Q, int64_t ldq, int64_t N, int64_t Hq, const nvfp4_kv
 
 size_t nvfp4_sample_workspace_bytes(int64_t N, int64_t V)
 {
-    if (N <= 0 || N > kMaxRows || V < 1 || V > kMaxVocabulary) return 0;
+    if (N <= 0 || N > kMaxDraws || V < 1 || V > kMaxVocabulary) return 0;
     return sample_workspace_bytes(N, V);
 }
 
@@ -215,7 +217,7 @@ int nvfp4_sample(const void *logits, int src_kind, int64_t ld, int64_t N, int64_
                  const float *top_p, const float *min_p, int64_t *tokens, void *ws, size_t ws_bytes, void *stream)
 {
     if (!u || !tokens) return NVFP4_ERR_NULL;
-    if (N < 0 || N > kMaxRows || V < 1 || V > kMaxVocabulary) return NVFP4_ERR_SHAPE;
+    if (N < 0 || N > kMaxDraws || V < 1 || V > kMaxVocabulary) return NVFP4_ERR_SHAPE;
     int rc = check_sizes(N, V);
     if (rc) return rc;
     RowSrc x;

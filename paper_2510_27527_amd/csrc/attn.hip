@@ -479,10 +479,11 @@ template <int DP, bool BITS8> hipError_t run(const AttnArgs &a, const Cut &p, hi
 
 }  // namespace
 
-size_t attn_workspace_bytes(int64_t N, int Hq, int heads, int D, int B, int64_t tokens, int64_t prefix)
+int64_t attn_workspace_bytes(int64_t N, int Hq, int heads, int D, int B, int64_t tokens, int64_t prefix)
 {
     const Cut p = cut_of(N, Hq, heads, B, tokens, prefix);
-    return (size_t)((own_parts(p, heads) + prefix_parts(p, heads)) * (D * 4 + 8) + (p.slots > 0 ? (int64_t)B * 16 : 0));
+    if (p.items > kMaxGroups / heads || p.prefix_items > kMaxGroups / heads || (p.slots > 0 && N * Hq > kMaxGroups)) return -1;
+    return (own_parts(p, heads) + prefix_parts(p, heads)) * (D * 4 + 8) + (p.slots > 0 ? (int64_t)B * 16 : 0);
 }
 
 hipError_t launch_attn(const uint16_t *q, int64_t ldq, int64_t N, int Hq, const KvCache &c, const KvBatch &b, float scale, uint16_t *out, int64_t ldo, void *ws,

@@ -6,7 +6,9 @@ namespace tj {
 
 constexpr int kMaxHeadDim = 256;
 constexpr int64_t kMaxSequences = 1 << 16;      // of a batch
-constexpr int64_t kMaxRows = 1 << 24;           // tokens of a call
+constexpr int64_t kMaxGroups = (1 << 24) - 1;   // workgroups of 256 threads: a launch has less than 2^32 threads
+constexpr int64_t kMaxRows = kMaxGroups;        // tokens of a call
+constexpr int64_t kMaxDraws = (1 << 22) - 1;    // rows to draw from: their workgroups have 1024 threads
 constexpr int kMinPage = 16, kMaxPage = 1 << 16;
 
 struct Rotation {
@@ -37,8 +39,8 @@ hipError_t launch_kv_append(const RowSrc &q, int Hq, const RowSrc &k, const RowS
                             const RowDst &qo, hipStream_t st);
 hipError_t launch_kv_load(const KvCache &c, const KvBatch &b, int64_t N, const RowDst &k, const RowDst &v, hipStream_t st);
 
-// tokens: the most that a sequence can have of its own
-size_t attn_workspace_bytes(int64_t N, int Hq, int heads, int D, int B, int64_t tokens, int64_t prefix);
+// tokens: the most that a sequence can have of its own; below 0: more workgroups than a launch can have
+int64_t attn_workspace_bytes(int64_t N, int Hq, int heads, int D, int B, int64_t tokens, int64_t prefix);
 hipError_t launch_attn(const uint16_t *q, int64_t ldq, int64_t N, int Hq, const KvCache &c, const KvBatch &b, float scale, uint16_t *out, int64_t ldo,
                        void *ws, hipStream_t st);
 

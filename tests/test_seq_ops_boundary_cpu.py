@@ -195,3 +195,29 @@ def test_binding_refuses(monkeypatch):
                  lambda: B.sample(z(3, 9), torch.zeros(3), tokens=i32(3)), lambda: B.sample(z(3, 9).half(), torch.zeros(3))):
         with pytest.raises(AssertionError):
             call()
+
+
+def test_more_workgroups_than_a_launch_has_are_refused(lib):
+    """A launch has less than 2^32 threads: 2^24 workgroups of 256, 2^22 of 1024."""
+    rope = lambda N: lib.nvfp4_rope(FAKE, 0, 0, FAKE, N, 0, 64, rotation(), 0, FAKE, 0, 0, None)
+    assert rope((1 << 24) - 1) == 0 and rope(1 << 24) == SHAPE
+    none = batch(starts=FAKE)
+    append = lambda N: lib.nvfp4_kv_append(None, 0, 0, FAKE, 128, FAKE, 128, 0, N, cache(), none, None, None, 0, 0, None)
+    load = lambda N: lib.nvfp4_kv_load(cache(), none, N, FAKE, 128, FAKE, 128, 0, None)
+    for f in (append, load):
+        assert f((1 << 24) - 1) == 0 and f(1 << 24) == SHAPE
+    assert lib.nvfp4_sample_workspace_bytes((1 << 22) - 1, 100) > 0 and lib.nvfp4_sample_workspace_bytes(1 << 22, 100) == 0
+    assert lib.nvfp4_sample(FAKE, 0, 100, 1 << 22, 100, FAKE, None, None, None, None, FAKE, FAKE, 1 << 60, None) == SHAPE
+    f = lib.nvfp4_attn_workspace_bytes
+
+    def attn(N, Hq, H, Bn, width, prefix):
+        return lib.nvfp4_attn(FAKE, Hq * 16, N, Hq, cache(H=H, D=16), batch(starts=FAKE, Bn=Bn, width=width, prefix=prefix, prefix_table=FAKE), 0.25, FAKE, Hq * 16, None, 0, None)
+    # rows to join: a token and query head each (64 rows a sequence: 128 would take the prefix themselves).  The size, which is the host's alone, comes first: a call that needs no
+    # workspace would not be refused.
+    assert f(65535, 256, 4, 16, 16, 65535, 1, 4096) > 0
+    assert attn(65535, 256, 4, 65535, 1, 4096) == WORKSPACE
+    assert f(65536, 256, 4, 16, 16, 65536, 1, 4096) == 0
+    assert attn(65536, 256, 4, 65536, 1, 4096) == SHAPE
+    # tiles of key heads: a tile for each sequence at least
+    assert attn(65536, 512, 512, 65536, 1, 0) == SHAPE
+    assert attn(1, 1 << 18, 1 << 18, 65536, 4, 0) == SHAPE
