@@ -147,7 +147,7 @@ def test_append_without_rotation_or_queries(tj):  # noqa: F811
 ATTNS = [([0], [1], 1, 1, 16, 16, 0), ([0, 1, 14, 15, 16, 31, 32, 33], [1] * 8, 4, 2, 64, 16, 0), ([62, 63, 64, 127, 128, 129, 255], [1] * 7, 8, 1, 128, 32, 0), ([300, 5], [1, 1], 16, 16, 80, 64, 0),
          ([700, 90, 0], [1, 1, 1], 6, 2, 96, 128, 0), ([40, 333], [1, 1], 4, 1, 256, 16, 0), ([500], [1], 3, 3, 192, 32, 0), ([0], [70], 2, 1, 64, 16, 0), ([0, 10, 33], [33, 5, 64], 6, 2, 128, 32, 0),
          ([7, 0], [3, 0], 24, 1, 64, 16, 0), ([0, 0, 0], [1, 1, 1], 4, 2, 64, 16, 100), ([20, 3], [1, 1], 8, 2, 128, 16, 513), ([0, 31], [17, 20], 4, 4, 48, 64, 65), ([2, 100], [2, 1], 40, 1, 128, 16, 31)]
-# and enough rows of a sequence, or of all against the prefix, for the kernels with tiles of 128 and 256: whole and ragged tiles, parts, tokens in front of the call's
+# and enough rows of a sequence, or of all against the prefix, for the kernel with tiles of 128: whole and ragged tiles, parts, tokens in front of the call's
 ATTNS += [([0, 30], [64, 50], 4, 2, 64, 16, 0), ([300], [33], 4, 1, 128, 16, 0), ([0, 5], [200, 100], 1, 1, 128, 32, 0), ([0], [300], 2, 2, 64, 64, 0), ([129, 0], [200, 190], 2, 1, 80, 16, 0), ([1500], [100], 1, 1, 112, 128, 0),
           ([0] * 33, [1] * 33, 4, 2, 128, 16, 700), ([3] * 40, [2] * 40, 6, 2, 64, 32, 333), ([0, 7], [130, 150], 3, 1, 128, 16, 100), ([2] * 18, [1] * 18, 12, 1, 96, 16, 1200), ([0, 40], [70, 90], 2, 1, 256, 16, 0), ([300], [70], 3, 1, 192, 32, 60), ([0], [150], 1, 1, 144, 64, 0)]
 
