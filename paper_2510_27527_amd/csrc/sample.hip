@@ -19,7 +19,7 @@ namespace {
 
 constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / 64;
-constexpr int kBins = 1024;                   // the last one: 31.9 and more below the largest, where weights are 0; it holds no border
+constexpr int kBins = 1024;                   // the last one: 31.9 and more below the largest, where weights are 0
 constexpr int kChoose = 512;                  // threads that draw from a row's list
 constexpr int kCuts = kChoose;                // cuts of a bin
 constexpr int kCutBits = 9;
@@ -62,16 +62,15 @@ struct Weight {
     }
 };
 
-// bin number of a logit, counted from the row's own zero upwards
+// Bin number of a logit, counted from the row's own zero upwards.  NaN and -infinity have the lowest, which is also that of logits far below zero: who counts tokens leaves them out by
+// their value.
 __device__ __forceinline__ float bin_of(float x, float per_unit)
 {
     return floorf(fminf(fmaxf(x * per_unit, -0x1p30f), 0x1p30f));
 }
-// bins below the row's largest logit.  What is never drawn, -infinity and NaN, is in the last one by its value, not by its distance: where logits lie so far below zero that their numbers are
-// limited, there is none.
 __device__ __forceinline__ int bin_below(float anchor, float x, float per_unit)
 {
-    return x > -INFINITY ? (int)fminf(anchor - bin_of(x, per_unit), (float)(kBins - 1)) : kBins - 1;
+    return (int)fminf(anchor - bin_of(x, per_unit), (float)(kBins - 1));
 }
 // bins per unit of x: 32 / T, and no more than 2^20, with which the last bin's weights are 0 still
 __device__ __forceinline__ float bins_per_unit(float T) { return fminf(32.0f / T, 0x1p20f); }
@@ -199,7 +198,7 @@ template <bool F32> __global__ __launch_bounds__(kThreads) void sample_bins_kern
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            if (b[j] < kBins - 1) {
+            if (b[j] < kBins - 1 && v[j] > -INFINITY) {
                 atomicAdd(reinterpret_cast<unsigned long long *>(&sums[b[j]]), (unsigned long long)w[j]);
                 if (count) atomicAdd(&counts[b[j]], 1u);
             }
@@ -318,7 +317,7 @@ template <bool F32, typename Do> __device__ __forceinline__ void each(const Samp
             logits8<F32>(a, r.row, i, (int)a.V, v);
             for (int j = 0; j < 8; ++j) {
                 const float x = seen(v[j], r.infinite);
-                if (bin_below(r.anchor, x, r.per_unit) != bin) continue;
+                if (x == -INFINITY || bin_below(r.anchor, x, r.per_unit) != bin) continue;
                 if (x != last) last = x, weight = r.weight(x);
                 what(place_of(key_of(x), (uint32_t)(i + j)), x, weight);
             }
@@ -540,7 +539,7 @@ template <bool F32> __global__ __launch_bounds__(kThreads) void sample_list_kern
                 v[j] = seen(v[j], r.infinite);
                 const int b = bin_below(r.anchor, v[j], r.per_unit);
                 const bool wanted = (uint32_t)(b - u0) <= uk || b == ks || (uint32_t)(b - ps) <= pk || (uint32_t)(b - ms) <= mk;
-                mine |= (uint32_t)wanted << j;
+                mine |= (uint32_t)(wanted && v[j] != -INFINITY) << j;
             }
         }
         if (!__any(mine)) continue;
