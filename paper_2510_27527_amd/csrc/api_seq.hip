@@ -199,6 +199,8 @@ int nvfp4_attn(const void *Q, int64_t ldq, int64_t N, int64_t Hq, const nvfp4_kv
     rc = make_dst(Out, NVFP4_OUT_BF16, ldo, N, Hq * c.D, &out);
     if (rc) return rc;
     if (!isfinite(scale) || !(scale > 0.0f)) return NVFP4_ERR_ENUM;
+    // The kernels load page 0 in the place of one that the cache does not have.  Where it has none at all there are no tokens either, whatever the tables say.
+    if (c.pages == 0) b.width = 0, b.prefix = 0;
     const int64_t need = N == 0 || b.B == 0 ? 0 : attn_workspace_bytes(N, (int)Hq, c.heads, c.D, b.B, (int64_t)b.width << c.page_log2, b.prefix);
     if (need < 0) return NVFP4_ERR_SHAPE;
     if (need && (!ws || ws_bytes < (size_t)need)) return NVFP4_ERR_WORKSPACE;
