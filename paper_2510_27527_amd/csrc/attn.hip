@@ -421,7 +421,19 @@ constexpr int kManyTiles = 256;
 // 20.1 / 20.6, 22.0 / 21.7, 23.7 / 22.4; eight up to 1000 in 8 bits 19.5 / 20.9, 20.6 / 22.1, 26.1 / 23.6.
 int rows_of_tile(int64_t rows) { return rows < 48 ? kTile : kWideRows; }
 
-Cut cut_of(int64_t N, int Hq, int heads, int B, int64_t tokens, int64_t prefix)
+// Sequences of whole tiles that nobody cuts can take the prefix themselves: no partial results, no join.  A tile's workgroup then walks the whole prefix alone, which is short against the partial
+// results, or there are workgroups enough to fill the GPU; else parts of the prefix are shared out.  Partial results of `groups` workgroups take the time of 300 + 9 groups tokens of a walk, and parts
+// need groups / 384 of the walk; with heads of more than 128 elements, one workgroup a CU, half of either.
+// us, through / in parts, four query heads a key head, 8 key heads of 128, a table of 256 own tokens.  50 new tokens of one sequence (16 workgroups) after 300 shared ones 21 / 29, 1000 40 / 31,
+// 64000 1768 / 124.  Two of 200 (112): 1000 44 / 68, 4000 122 / 102, 64000 1733 / 815.  Four of 256 (256): 4000 126 / 168, 16000 437 / 392.  Eight of 256 (512): 64000 2343 / 2538.  Heads of 256, one of
+// 200 (56): 600 66 / 75, 1200 108 / 97; four (224): 20000 1194 / 1699.
+bool parts_pay(int64_t groups, int D, int64_t prefix)
+{
+    const int64_t by = D > 128 ? 2 : 1;
+    return by * prefix * (384 - by * groups) > 384 * (300 + 9 * groups);
+}
+
+Cut cut_of(int64_t N, int Hq, int heads, int D, int B, int64_t tokens, int64_t prefix)
 {
     Cut p;
     const int64_t G = Hq / heads;
@@ -434,8 +446,7 @@ Cut cut_of(int64_t N, int Hq, int heads, int B, int64_t tokens, int64_t prefix)
     p.target = cut ? (int)((groups + heads - 1) / heads) : 0;
     const int64_t most = cut ? (units + p.min_units - 1) / p.min_units : 1;                // parts of a tile
     p.items = tiles * most < tiles + p.target ? tiles * most : tiles + p.target;           // every tile at least once, and the cuts
-    // Sequences of whole tiles that nobody cuts take the prefix themselves: no partial results, no join.  (Four prompts of up to 1000 tokens after 1000 shared ones: 100 us, 242 with parts.)
-    p.through = prefix > 0 && !cut && N * G >= (int64_t)B * kWideRows;
+    p.through = prefix > 0 && !cut && N * G >= (int64_t)B * kWideRows && !parts_pay(B * ((N * G / B + kWideRows - 1) / kWideRows) * heads, D, prefix);
     if (p.through) prefix = 0;
     p.slots = cut || prefix ? p.items : 0;
     p.prefix_rows = p.prefix_units = p.prefix_parts = 0;
@@ -481,7 +492,7 @@ template <int DP, bool BITS8> hipError_t run(const AttnArgs &a, const Cut &p, hi
 
 int64_t attn_workspace_bytes(int64_t N, int Hq, int heads, int D, int B, int64_t tokens, int64_t prefix)
 {
-    const Cut p = cut_of(N, Hq, heads, B, tokens, prefix);
+    const Cut p = cut_of(N, Hq, heads, D, B, tokens, prefix);
     if (p.items > kMaxGroups / heads || p.prefix_items > kMaxGroups / heads || (p.slots > 0 && N * Hq > kMaxGroups)) return -1;
     return (own_parts(p, heads) + prefix_parts(p, heads)) * (D * 4 + 8) + (p.slots > 0 ? (int64_t)B * 16 : 0);
 }
@@ -489,7 +500,7 @@ int64_t attn_workspace_bytes(int64_t N, int Hq, int heads, int D, int B, int64_t
 hipError_t launch_attn(const uint16_t *q, int64_t ldq, int64_t N, int Hq, const KvCache &c, const KvBatch &b, float scale, uint16_t *out, int64_t ldo, void *ws,
                        hipStream_t st)
 {
-    const Cut p = cut_of(N, Hq, c.heads, b.B, (int64_t)b.width << c.page_log2, b.prefix);
+    const Cut p = cut_of(N, Hq, c.heads, c.D, b.B, (int64_t)b.width << c.page_log2, b.prefix);
     const int64_t own = own_parts(p, c.heads), pre = prefix_parts(p, c.heads);
     float *const o = static_cast<float *>(ws);
     float2_t *const ml = reinterpret_cast<float2_t *>(o + (own + pre) * c.D);

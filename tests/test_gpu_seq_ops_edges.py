@@ -2,7 +2,10 @@
 import pytest
 import torch
 
+import seq_ops_reference as ref
+from block_ops_reference import within
 from test_gpu_block_ops import BF, draws, tj  # noqa: F401  (tj: the fixture)
+from test_gpu_seq_ops import run_attn
 
 pytestmark = pytest.mark.gpu
 
@@ -40,3 +43,16 @@ def test_a_cache_of_no_pages_has_no_tokens(tj, new, width, prefix, bits8):  # no
     # beside keys for 8 bits cosines and sines are made in 64 bits: 8 U of each of a pair's two elements on either side, and U of the sum
     off = 0.0 if not bits8 else 2.0 ** -24 * (2 * 8 * 2 + 2) * float(q.abs().max())
     assert float((qo - want)[placed].abs().max()) <= off
+
+
+# On either side of who takes the prefix: a short one, and many tiles, in front of their own tokens; a long one in parts.
+@pytest.mark.parametrize("case", [([0], [140], 4, 1, 64, 16, 300), ([0], [140], 4, 1, 64, 16, 420), ([0], [100], 2, 1, 128, 64, 1500), ([0, 30], [70, 65], 4, 2, 128, 32, 1111), ([3], [130], 1, 1, 208, 16, 700),
+                                  ([0] * 4, [64, 1, 63, 129], 2, 1, 64, 16, 900)], ids=lambda c: "-".join(str(v) for v in (len(c[0]), max(c[1])) + c[2:]))
+@pytest.mark.parametrize("bits8", [False, True])
+def test_prompts_after_prefixes_of_every_length(tj, case, bits8):  # noqa: F811
+    past, new, Hq, H, D, page, prefix = case
+    print("attn", case, bits8, flush=True)
+    bt, q, k, v, o, scale = run_attn(tj, case, bits8, 5)
+    want, bound = ref.attn(q.view(bt.N, Hq, D), k, v, bt, scale, Hq)
+    within(o.reshape(bt.N, Hq, D), want, bound, "out")
+    assert torch.equal(tj.attn(q, bt.cache, bt.kv, Hq), o)
