@@ -216,11 +216,12 @@ template <bool F32> __global__ __launch_bounds__(kThreads) void sample_bins_kern
     if (count) ws.counts[(int64_t)blockIdx.x * kBins + threadIdx.x] = counts[threadIdx.x];
 }
 
-// (weight, number of tokens) up to and with each thread's; all threads of the workgroup call it
-template <int WAVES> __device__ __forceinline__ void scan(double &w, uint32_t &c, double *lw, uint32_t *lc)
+// (Weight, number of tokens) up to and with each thread's; all threads of the workgroup call it.  In integers: a thread without tokens has the sum of the one in front of it, however the
+// additions are grouped, so that no sum is between the two and a place looked up by one always holds a token.
+template <int WAVES> __device__ __forceinline__ void scan(uint64_t &w, uint32_t &c, uint64_t *lw, uint32_t *lc)
 {
     for (int o = 1; o < 64; o <<= 1) {
-        const double x = __shfl_up(w, o, 64);
+        const uint64_t x = __shfl_up((unsigned long long)w, o, 64);
         const uint32_t y = __shfl_up(c, o, 64);
         if ((int)(threadIdx.x & 63) >= o) w += x, c += y;
     }
@@ -228,7 +229,7 @@ template <int WAVES> __device__ __forceinline__ void scan(double &w, uint32_t &c
     __syncthreads();
     if ((threadIdx.x & 63) == 63) lw[wave] = w, lc[wave] = c;
     __syncthreads();
-    double x = 0.0;
+    uint64_t x = 0;
     uint32_t y = 0;
 #pragma unroll
     for (int i = 0; i < WAVES; ++i)
@@ -252,7 +253,7 @@ struct Shared {
     uint64_t weights[kList];
     uint64_t sums[kCuts];
     uint32_t counts[kCuts];
-    double lw[kWaves];
+    uint64_t lw[kWaves];
     uint32_t lc[kWaves];
     uint64_t few[kFew], few_weight[kFew];
     double found[2];
@@ -375,19 +376,19 @@ template <bool F32, bool RANK> __device__ void locate(const SampleArgs &a, const
         give();
         __syncthreads();
         const uint32_t here = s.counts[threadIdx.x];
-        double w = (double)s.sums[threadIdx.x];
-        const double own = w;
+        const uint64_t own = s.sums[threadIdx.x];
+        uint64_t sum = own;
         uint32_t c = here;
-        scan<kChoose / 64>(w, c, s.lw, s.lc);
-        w += before;
+        scan<kChoose / 64>(sum, c, s.lw, s.lc);
+        const double w = before + (double)sum, start = before + (double)(sum - own);
         c += rank;
         // the cut in which the sum passes the target; the last one that weighs anything where none does
-        const bool passes = RANK ? (double)c > target : w > target, passed = RANK ? (double)(c - here) > target : w - own > target;
+        const bool passes = RANK ? (double)c > target : w > target, passed = RANK ? (double)(c - here) > target : start > target;
         if (here && passes && !passed) atomicMax(&s.cut, kCuts + (kCuts - (int)threadIdx.x));
-        else if (RANK ? here > 0 : own > 0.0) atomicMax(&s.cut, (int)threadIdx.x);
+        else if (RANK ? here > 0 : own > 0) atomicMax(&s.cut, (int)threadIdx.x);
         __syncthreads();
         const int cut = s.cut >= kCuts ? 2 * kCuts - s.cut : s.cut;
-        if ((int)threadIdx.x == cut) s.found[0] = w - own, s.n = c - here;
+        if ((int)threadIdx.x == cut) s.found[0] = start, s.n = c - here;
         __syncthreads();
         before = s.found[0];
         rank = s.n;
@@ -431,7 +432,8 @@ template <bool F32> __global__ __launch_bounds__(kThreads) void sample_list_kern
     __shared__ double ends[kBins];
     __shared__ uint32_t count_ends[kBins];
     __shared__ uint32_t keys[kSliceList], index[kSliceList];
-    __shared__ double lw[kWaves], factors[kMaxSlices];
+    __shared__ double factors[kMaxSlices];
+    __shared__ uint64_t lw[kWaves];
     __shared__ uint32_t lc[kWaves], n, base;
     __shared__ int bins[8];
     const int64_t row = blockIdx.x / slices;
@@ -467,16 +469,17 @@ template <bool F32> __global__ __launch_bounds__(kThreads) void sample_list_kern
         counts[i] = some && a.top_k ? ws.counts[at] : 0;
     }
     __syncthreads();
-    double w = 0.0;
+    uint64_t own = 0;
     uint32_t c = 0;
 #pragma unroll
     for (int i = 0; i < kMaxSlices; ++i) {
-        if (sums[i]) w += (double)sums[i] * factors[i];
+        if (sums[i]) own += (uint64_t)((double)sums[i] * factors[i]);
         c += counts[i];
     }
-    const double own = w;
+    uint64_t sum = own;
     const uint32_t own_count = c;
-    scan<kWaves>(w, c, lw, lc);
+    scan<kWaves>(sum, c, lw, lc);
+    const double w = (double)sum;
     ends[t] = w;
     count_ends[t] = c;
     __syncthreads();
@@ -484,7 +487,7 @@ template <bool F32> __global__ __launch_bounds__(kThreads) void sample_list_kern
     const uint32_t tokens = count_ends[kBins - 1];
     // bins[i]: the bin that a sum falls in, the last one with weight where it is beyond all
     const auto bin_at = [&](int i, double sum) {
-        if (own > 0.0 && begin <= sum && (sum < w || w >= total)) bins[i] = t;
+        if (own > 0 && begin <= sum && (sum < w || w >= total)) bins[i] = t;
     };
     const bool by_k = k >= 1 && (uint32_t)k < tokens, by_p = p < 1.0f, by_m = m > 0.0f;
     p = p > 0.0f ? p : 0.0f;
@@ -622,10 +625,9 @@ template <bool F32> __global__ __launch_bounds__(kChoose) void sample_choose_ker
             each<F32>(a, r, s, b, [&](uint64_t, float x, uint64_t weight) {
                 if (exp2(-(r.weight.top - (double)x) * r.weight.step) >= (double)m) sum += weight;
             });
-        double all = (double)sum;
         uint32_t none = 0;
-        scan<kChoose / 64>(all, none, s.lw, s.lc);
-        if (t == kChoose - 1) s.found[0] = all + (in.m0 ? s.ends[in.m0 - 1] : 0.0);
+        scan<kChoose / 64>(sum, none, s.lw, s.lc);
+        if (t == kChoose - 1) s.found[0] = (double)sum + (in.m0 ? s.ends[in.m0 - 1] : 0.0);
         __syncthreads();
         kept = fmin(kept, s.found[0]);
     }
