@@ -92,6 +92,7 @@ class Decoder:
 
 def answer(model, shared, prompts, steps, seed=0, **how):
     """`steps` tokens for each of the prompts (lists of tokens), which all follow the tokens of `shared`; [steps, prompts]."""
+    assert all(prompts), "prompts: one token each at least, whose hidden state the answer begins with"
     device = model.embedding.device
     g = torch.Generator(device=device).manual_seed(seed)
     pages = model.layers[0]["cache"].k.shape[0]
