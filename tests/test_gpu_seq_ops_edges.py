@@ -56,3 +56,41 @@ def test_prompts_after_prefixes_of_every_length(tj, case, bits8):  # noqa: F811
     want, bound = ref.attn(q.view(bt.N, Hq, D), k, v, bt, scale, Hq)
     within(o.reshape(bt.N, Hq, D), want, bound, "out")
     assert torch.equal(tj.attn(q, bt.cache, bt.kv, Hq), o)
+
+
+# Ascending starts that begin below the first row, end behind the last one, leave rows out at either end, or give sequences none; few rows and tiles of 128, one part and several
+@pytest.mark.parametrize("N,starts", [(3, (-7, 1, 2, 900)), (3, (0, 0, 2, 3)), (3, (1, 1, 1, 2)), (3, (-5, -1, 0, 2)), (3, (3, 3, 3, 3)), (3, (2, 7, 9, 70)), (3, (-(2 ** 31), -9, 1, 2 ** 31 - 1)), (3, (5, 9, 12, 70)),
+                                      (3, (-3, -2, -1, 0)), (150, (-50, 70, 4000, 4000)), (150, (10, 80, 80, 140)), (300, (-1, 299, 299, 2 ** 31 - 1))])
+@pytest.mark.parametrize("prefix,extra", [(0, 0), (0, 40), (50, 0), (700, 40)])
+def test_starts_that_reach_outside_the_rows(tj, N, starts, prefix, extra):  # noqa: F811
+    """Every sequence has the rows between its starts that there are, the last tokens of it; rows between no two starts are left as they were."""
+    B = tj.binding
+    Hq, H, D = 4, 2, 64
+    inside = [min(max(s, 0), N) for s in starts]
+    new = [b - a for a, b in zip(inside, inside[1:])]
+    bt = ref.Batch(tj, [30, 20, 10], new, H, D, 16, prefix=prefix, seed=3, extra_width=extra)
+    normal = draws(N + prefix)
+    T = len(bt.tokens())
+    k, v = bt.fill(normal(T, H, D), normal(T, H, D))
+    kv = tj.KVBatch(bt.kv.table, bt.kv.lens, torch.tensor(starts, dtype=torch.int32).cuda(), bt.kv.prefix_table, prefix)
+    print("starts", N, starts, prefix, extra, flush=True)
+    mine = torch.zeros(N, dtype=torch.bool)
+    mine[inside[0]:inside[-1]] = True
+    fresh = lambda width, dtype=BF: torch.full((N, width), -7.0, dtype=dtype, device="cuda")
+    q = normal(N, Hq * D).to(BF).cuda()
+    o = tj.attn(q, bt.cache, kv, Hq, Out=fresh(Hq * D))
+    assert (o[~mine] == -7.0).all()
+    want, bound = ref.attn(q[mine].view(-1, Hq, D), k, v, bt, D ** -0.5, Hq)
+    within(o[mine].view(-1, Hq, D), want, bound, "out")
+    lk, lv = tj.kv_load(bt.cache, kv, N, K=fresh(H * D), V=fresh(H * D))
+    at = [bt.index[(b, bt.past[b] + i)] for b, i in bt.rows]
+    for got, held in ((lk, k), (lv, v)):
+        assert (got[~mine] == -7.0).all() and torch.equal(got[mine].double().cpu(), held[at].reshape(-1, H * D))
+    x = normal(N, H * D).to(BF).cuda()
+    turn = tj.Rope(tj.rope_frequencies(D))
+    qo = tj.kv_append(x, x, bt.cache, kv, turn, Q=q, Qo=fresh(Hq * D, torch.float32), out_dtype=B.OUT_F32)
+    pos = torch.zeros(N, dtype=torch.int32)
+    pos[mine] = torch.tensor([prefix + bt.past[b] + i for b, i in bt.rows], dtype=torch.int32)
+    assert (qo[~mine] == -7.0).all() and torch.equal(qo[mine], tj.rope(q, pos.cuda(), turn, Hq, B.OUT_F32)[mine])
+    _, lv = tj.kv_load(bt.cache, kv, N, K=fresh(H * D), V=fresh(H * D))
+    assert (lv[~mine] == -7.0).all() and torch.equal(lv[mine], x[mine])
