@@ -223,7 +223,8 @@ template <int WAVES> __device__ __forceinline__ void scan(uint64_t &w, uint32_t 
     for (int o = 1; o < 64; o <<= 1) {
         const uint64_t x = __shfl_up((unsigned long long)w, o, 64);
         const uint32_t y = __shfl_up(c, o, 64);
-        if ((int)(threadIdx.x & 63) >= o) w += x, c += y;
+        const bool in = (int)(threadIdx.x & 63) >= o;
+        w += in ? x : 0, c += in ? y : 0;
     }
     const int wave = threadIdx.x >> 6;
     __syncthreads();
@@ -380,15 +381,17 @@ template <bool F32, bool RANK> __device__ void locate(const SampleArgs &a, const
         uint64_t sum = own;
         uint32_t c = here;
         scan<kChoose / 64>(sum, c, s.lw, s.lc);
-        const double w = before + (double)sum, start = before + (double)(sum - own);
         c += rank;
-        // the cut in which the sum passes the target; the last one that weighs anything where none does
-        const bool passes = RANK ? (double)c > target : w > target, passed = RANK ? (double)(c - here) > target : start > target;
-        if (here && passes && !passed) atomicMax(&s.cut, kCuts + (kCuts - (int)threadIdx.x));
-        else if (RANK ? here > 0 : own > 0) atomicMax(&s.cut, (int)threadIdx.x);
+        // The first cut with which the sum passes the target; the last one that weighs anything where none does.
+        const bool some = RANK ? here > 0 : own > 0;
+        const uint64_t any = __ballot(some), passes = __ballot(some && (RANK ? (double)c > target : before + (double)sum > target));
+        if ((threadIdx.x & 63) == 0) {
+            if (passes) atomicMax(&s.cut, 2 * kCuts - ((int)threadIdx.x + __ffsll((unsigned long long)passes) - 1));
+            else if (any) atomicMax(&s.cut, (int)threadIdx.x + 63 - __clzll((long long)any));
+        }
         __syncthreads();
         const int cut = s.cut >= kCuts ? 2 * kCuts - s.cut : s.cut;
-        if ((int)threadIdx.x == cut) s.found[0] = start, s.n = c - here;
+        if ((int)threadIdx.x == cut) s.found[0] = before + (double)(sum - own), s.n = c - here;
         __syncthreads();
         before = s.found[0];
         rank = s.n;
