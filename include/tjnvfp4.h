@@ -372,13 +372,13 @@ int nvfp4_gemv(const void *X, int64_t ldx, int64_t M, const nvfp4_tensor *W, voi
  *
  * What device memory holds (lengths, tables, positions, parameters of rows) is not looked at by the host: whatever it is, no call reads or writes outside its
  * arrays.  Where a length is negative or longer than its table, it is taken as 0 or as the table's room; a page that the cache does not have holds
- * no tokens: appending to it writes nothing, attention does not see it, loading gives zeros.
+ * no tokens: appending to it writes nothing, attention does not see it, loading gives zeros (in a cache of no pages, every one).
  */
 enum { NVFP4_ROPE_HALF = 0, NVFP4_ROPE_PAIRS = 1 };
 enum { NVFP4_KV_BF16 = 0, NVFP4_KV_8 = 1 };
 enum { NVFP4_ROPE_PLAIN = 0, NVFP4_ROPE_LINEAR = 1, NVFP4_ROPE_BASE = 2, NVFP4_ROPE_PARTS = 3 };
 
-/* Rotary positions of a head of D elements: pair j < R / 2 is turned by the angle position * freqs[j] (the product of the binary32 frequency and the integer, exact):
+/* Rotary positions of a head of D elements: pair j < R / 2 is turned by the angle position * freqs[j] (product and turns in binary64: off by up to 2^-51 of the angle):
  *   (a, b) -> scale (a cos - b sin, b cos + a sin)
  * NVFP4_ROPE_HALF: pair j is elements (j, R / 2 + j); NVFP4_ROPE_PAIRS: (2j, 2j + 1).  Elements from R on stay as they are. */
 typedef struct nvfp4_rotation {
@@ -418,7 +418,7 @@ typedef struct nvfp4_kvcache {
 
 /* A batch of B sequences and the rows of a call.  Rows starts[b] .. starts[b + 1] - 1 are the last tokens of sequence b, of whose own tokens the cache then has lens[b]
  * (the call's among them): row starts[b] + i is own token p = lens[b] - n_b + i.  Own token p lies in page table[b][p / page], slot p % page.  Before the own tokens every sequence has the
- * `prefix` tokens of the pages prefix_table[0 ..]: row positions are prefix + p.  starts NULL: one row each (N = B).  Rows that belong to no
+ * `prefix` tokens of the pages prefix_table[0 ..]: row positions are prefix + p.  starts NULL: one row each (N = B); a start below 0 counts as 0, one above N as N.  Rows that belong to no
  * sequence, and rows with p < 0 when they are appended or loaded, are left as they were.  Device memory, int32, 4-byte aligned. */
 typedef struct nvfp4_kvbatch {
     const int32_t *table;         /* [B][width] */
@@ -443,10 +443,11 @@ int nvfp4_kv_load(const nvfp4_kvcache *cache, const nvfp4_kvbatch *batch, int64_
  * Attention of the batch's rows Q [N x Hq D] (bf16) over the cache: head h of row (b, p) sees the prefix and own tokens 0 .. p through head h / (Hq / H) of keys and values,
  *   out = sum_t softmax_t(scale q . k_t) v_t        (zeros where it sees nothing)
  * Out [N x Hq D] bf16.  Scores and sums are binary32; the weights of the values are rounded to bf16 for the matrix instructions.  A NaN or infinity in a key or value stays with the
- * rows that see it.  The prefix is read once for all rows of a tile, whatever the number of sequences.
+ * rows that see it.  The prefix is read once for all rows of a tile, whatever the number of sequences.  How a call is cut goes by its sizes, averages over its sequences: a prompt beside single tokens
+ * of other sequences can take many times what they take in two calls.
  * Hq a multiple of H, N < 2^24, N * Hq <= 2^30, and less than 2^24 workgroups: one takes a key head of 16 rows (128 where a sequence, or for the prefix the batch, has 48 and more; a row is a
  * token and query head), or one token and query head where partial results are joined (a prefix in front of few rows each); SHAPE otherwise.  Out must not overlap Q.  scale finite and above 0.  ws: nvfp4_attn_workspace_bytes of the same sizes (16-byte aligned; from N, B, width and prefix alone, not from lengths, so that
- * one does for all steps of a batch).  Same inputs, same bits.  Errors: NULL, SHAPE, ENUM, ALIGN, MISMATCH, WORKSPACE.
+ * one does for all steps of a batch; 0: none is needed, or the call refuses these sizes).  Same inputs, same bits.  Errors: NULL, SHAPE, ENUM, ALIGN, MISMATCH, WORKSPACE.
  */
 int nvfp4_attn(const void *Q, int64_t ldq, int64_t N, int64_t Hq, const nvfp4_kvcache *cache, const nvfp4_kvbatch *batch, float scale, void *Out, int64_t ldo,
                void *ws, size_t ws_bytes, void *stream);

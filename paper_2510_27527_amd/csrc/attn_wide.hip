@@ -1,7 +1,7 @@
 // Attention on tiles of 128 rows: prompts, and many sequences' rows against a shared prefix.  (Formulas: attn_common.h.)
 //
-// 4 D flops and one exponential a (row, token) pair.  Four prompts up to 4096 tokens long (32 query heads, 8 key heads of 128): 327 us, 765 TFLOP/s; matrix instructions are busy 35 % of
-// the time, the vector ALU 45 %, waves wait 26 % of theirs.  The exponentials are not what bounds it: 388 us without them where it took 404 under a profiler.  The four waves of a workgroup have 32 rows
+// 4 D flops and one exponential a (row, token) pair.  Four prompts up to 4096 tokens long (32 query heads, 8 key heads of 128): 331 us, 755 TFLOP/s (385 and more in the first 30 ms after the
+// GPU was idle); matrix instructions are busy 35 % of the time, the vector ALU 44 %, waves wait 27 % of theirs.  Without the exponentials it takes 316 us.  The four waves of a workgroup have 32 rows
 // each and share tiles of 64 tokens in LDS, the next tile on its way in registers.  Products: scores^T [tokens x rows] = K Q^T and out^T [D x rows] += V^T P^T, 32 x 32 x 16
 // each; the tokens are dealt to the rows of a score tile so that a lane ends up with the weights that the second product takes from it.  Values lie in LDS as rows of tokens and are turned by the
 // transposing LDS reads.  8-bit caches become bf16 on their way into LDS, once for all four waves.
@@ -224,7 +224,7 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attn_wide_kernel(A
         }
         float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
         top = max32(top) * a.scale2;
-        // moved whenever it is exceeded: a row's largest weight is then 1, which bf16 holds exactly.  (Moved from 2^8 on only: 386 us instead of 398 for four prompts up to 4096 tokens, and
+        // Moved whenever it is exceeded: a row's largest weight is then 1, which bf16 holds exactly.  (Moved from 2^8 on only: 322 us instead of 332 for four prompts up to 4096 tokens, and
         // outputs 0.0022 off instead of 0.0018, where rounding the exact ones to bf16 gives 0.0016.)
         if (__any(top > m)) {
             const float to = fmaxf(m, top), old = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - to);

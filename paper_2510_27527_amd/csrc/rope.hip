@@ -4,8 +4,8 @@
 //
 // Bound by memory: every element is read once and written once.  A unit of work is eight pairs (16 elements, two 16-byte accesses each way)
 // or eight elements that stay as they are; cosines and sines are computed once per token and pair, in LDS, for all of the token's heads.
-// Medians: 16384 rows of 32 heads of 64 (bf16, 134 MB) 24.7 us, 5.4 TB/s; 1001 x 5 heads of 80 in binary32 3.7; appending one token 2.8, 256 tokens 5.0 (8 key heads of 128); 6253 tokens into
-// 8 bits 39, and read back as binary32 12.4.  In 8 bits several tokens a workgroup (47 to 75 us, where one took 42 to 46) and two units a thread at once (59 to 62) were slower.
+// Medians: 16384 rows of 32 heads of 64 (bf16, 134 MB) 24.5 us, 5.5 TB/s; 1001 x 5 heads of 80 in binary32 3.7; appending one token 2.8, 256 tokens 4.9 (32 query heads, 8 key heads of 128);
+// 6253 tokens into 8 bits 38, and read back as bf16 11.5; into bf16 42 (3.6 TB/s), read back 12 (4.2).  In 8 bits several tokens a workgroup (47 to 75 us, where one took 42 to 46) and two units a thread at once (59 to 62) were slower.
 #include "rowwise.h"
 #include "seq_ops.h"
 
