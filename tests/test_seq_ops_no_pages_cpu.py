@@ -14,11 +14,13 @@ HIP, WORKSPACE = -7, -4
 CALL = """
 import sys
 sys.path[:0] = [%r, %r]
+import torch
 import test_seq_ops_boundary_cpu as t
 import paper_2510_27527_amd.binding as B
 pages, N, width, prefix, kind = map(int, sys.argv[1:])
 c = t.cache(pages=pages, kind=kind, ke=t.FAKE, ve=t.FAKE)
 b = t.batch(Bn=N, width=width, prefix=prefix, prefix_table=t.FAKE)
+assert not torch.cuda.is_available()
 print(B.lib().nvfp4_attn(t.FAKE, 256, N, 4, c, b, 0.125, t.FAKE, 256, None, 0, None))
 """ % (ROOT, os.path.join(ROOT, "tests"))
 
